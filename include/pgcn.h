@@ -522,6 +522,156 @@ typedef struct {
 } pgcn_sage_bwd_args;
 int pgcn_sage_layer_bwd(const pgcn_partition *part, const pgcn_sage_bwd_args *args, hipStream_t stream);
 
+/* Activation applied after a group norm: u, max(u, 0), u / (1 + e^-u), u (1 + erf(u / sqrt 2)) / 2. */
+enum pgcn_act { PGCN_ACT_NONE = 0, PGCN_ACT_RELU = 1, PGCN_ACT_SILU = 2, PGCN_ACT_GELU = 3 };
+
+/*
+ * The operators below (top logits, distillation loss, group norm) take matrices in
+ * `dtype`: PGCN_F32 (fp32, ld % 4 == 0) or PGCN_BF16 (bf16 bits, ld % 8 == 0), 16-byte
+ * aligned.  They compute in fp32 (loss sums in fp64) and round a bf16 result once, to
+ * nearest even.  Columns past the matrix's width are neither used nor written, whatever
+ * they hold.  Outputs overlap no other buffer of the call (else PGCN_EINVAL).  A
+ * workspace is 16-byte aligned, of the size that the call's _workspace_size function
+ * gives (0 bytes: it may be NULL), may hold anything before the call and is the call's
+ * own until its work has ended.  A stream of another device than the current one is
+ * refused with PGCN_EINVAL, and so are more than 2^31 - 1 rows.  The _workspace_size
+ * functions return 0 for sizes that the call rejects.
+ */
+
+/* Largest number of listed classes, of classes, and of channels that they take. */
+#define PGCN_MAX_TOP 256
+#define PGCN_MAX_CLASSES 262144
+#define PGCN_MAX_CHANNELS 8192
+
+/*
+ * The `top` largest logits of every row: what a trained partition model keeps of its
+ * answers to teach another one (pgcn_distill_loss_fwd_bwd).
+ *     top_values[r, k], top_ids[r, k]: the k-th largest logit of row r and its class; of
+ *         equal logits (-0 equals +0) the lower class comes first;
+ *     tail_lse[r] = log sum of e^{Z[r, c] / temperature} over the classes not listed
+ * A logit of -inf marks a class that is no answer: it is never listed and adds nothing to
+ * the tail.  Where a row has fewer than `top` others, the slots left hold -inf and -1; a
+ * tail of nothing is -inf.  A NaN is never listed either and makes the row's tail NaN.
+ */
+typedef struct {
+  int32_t dtype;               /* pgcn_dtype of Z                                */
+  int32_t classes;             /* 1 .. PGCN_MAX_CLASSES                          */
+  int32_t top;                 /* 1 .. min(classes, PGCN_MAX_TOP)                */
+  float temperature;           /* > 0, with a finite reciprocal                  */
+  int64_t rows;
+  int64_t ld;                  /* stride of Z (elements)                         */
+  int64_t ld_top;              /* stride of top_values and top_ids, >= top       */
+  const void *Z;               /* [rows, ld]                                     */
+  float *top_values;           /* [rows, ld_top] out                             */
+  int32_t *top_ids;            /* [rows, ld_top] out                             */
+  float *tail_lse;             /* [rows] out or NULL                             */
+  void *workspace;
+  size_t workspace_bytes;
+} pgcn_top_logits_args;
+size_t pgcn_top_logits_workspace_size(int32_t dtype, int64_t rows, int32_t classes, int32_t top);
+int pgcn_top_logits(const pgcn_top_logits_args *args, hipStream_t stream);
+
+/*
+ * Loss of a student's logits Z against a teacher's top logits, with its gradient.  With
+ * T = temperature, row by row:
+ *     p_k  = e^{top_values[k] / T - L},  rho = e^{tail_lse - L},  L so that sum_k p_k + rho = 1
+ *     q    = softmax(Z / T),  s = sum of q over the classes not listed
+ *     loss = soft_scale * (sum_k p_k log(p_k / q_{top_ids[k]}) + rho log(rho / s))
+ *          + hard_scale * -log softmax(Z)[label]                  (summed over the rows)
+ *     J    = d loss / d Z
+ * tail_lse NULL: rho = 0, the listed classes share the whole of p.  A T^2 that keeps the
+ * gradient's size over temperatures belongs into soft_scale.
+ *   - A slot with id -1 (any negative one) or value -inf lists no probability; the latter's
+ *     class still counts as listed.  A class listed twice counts with its lowest slot.  A
+ *     row that lists none adds no soft term.
+ *   - labels NULL, or a label -1: no hard term (a node without a label).
+ *   - p log(p / q) is 0 where p is 0, also where q is 0 (a logit of -inf masks its class);
+ *     it is +inf where p > 0 and q = 0.
+ *   - An id or label >= classes (a label < -1 too) makes the loss NaN; the id is otherwise
+ *     ignored.  A row without any finite logit that has a soft or hard term makes it NaN.
+ *   - A NaN among a row's logits or listed values makes the loss and the row's J NaN.
+ * J: [rows, ld], the dtype and stride of Z.  loss_out: one device float, written (not
+ * accumulated), reduced in a fixed order.
+ */
+typedef struct {
+  int32_t dtype;               /* pgcn_dtype of Z and J                          */
+  int32_t classes;             /* 1 .. PGCN_MAX_CLASSES                          */
+  int32_t top;                 /* 1 .. min(classes, PGCN_MAX_TOP)                */
+  float temperature;           /* > 0, with a finite reciprocal                  */
+  int64_t rows;
+  int64_t ld;                  /* stride of Z and J (elements)                   */
+  int64_t ld_top;              /* stride of top_values and top_ids, >= top       */
+  float soft_scale, hard_scale;
+  const void *Z;               /* [rows, ld]                                     */
+  const float *top_values;     /* [rows, ld_top]                                 */
+  const int32_t *top_ids;      /* [rows, ld_top]                                 */
+  const float *tail_lse;       /* [rows] at the same temperature, or NULL        */
+  const int32_t *labels;       /* [rows] or NULL                                 */
+  void *J;                     /* [rows, ld] out                                 */
+  float *loss_out;             /* [1] out                                        */
+  void *workspace;
+  size_t workspace_bytes;
+} pgcn_distill_args;
+size_t pgcn_distill_workspace_size(int32_t dtype, int64_t rows, int32_t classes, int32_t top);
+int pgcn_distill_loss_fwd_bwd(const pgcn_distill_args *args, hipStream_t stream);
+
+/*
+ * Group normalisation of features-last rows with an activation, for use between a layer's
+ * product (relu = 0) and the next layer.  The rows [i sample_rows, (i + 1) sample_rows) are
+ * sample i: 1 row normalises every node by itself (groups = 1: layer norm), the
+ * partition's n_inner rows all its nodes together.  Per sample and group of channels /
+ * groups neighbouring channels:
+ *     mean, rstd = 1 / sqrt(variance + eps)    over the sample's rows and the group's channels
+ *     u = (X - mean) rstd gamma + beta ;  Y = act(u)
+ * gamma or beta NULL: 1 and 0.  mean and rstd ([samples, groups]) are kept for the backward;
+ * either may be NULL where none follows.
+ */
+typedef struct {
+  int32_t dtype;               /* pgcn_dtype of X and Y                          */
+  int32_t act;                 /* pgcn_act                                       */
+  int32_t channels;            /* 1 .. PGCN_MAX_CHANNELS                         */
+  int32_t groups;              /* divides channels                               */
+  int64_t samples, sample_rows;
+  int64_t ld_x, ld_y;
+  float eps;                   /* > 0                                            */
+  const void *X;               /* [samples * sample_rows, ld_x]                  */
+  const float *gamma, *beta;   /* [channels] or NULL                             */
+  void *Y;                     /* [samples * sample_rows, ld_y] out              */
+  float *mean, *rstd;          /* [samples, groups] out or NULL                  */
+  void *workspace;
+  size_t workspace_bytes;
+} pgcn_group_norm_fwd_args;
+int pgcn_group_norm_fwd(const pgcn_group_norm_fwd_args *args, hipStream_t stream);
+
+/*
+ * Its gradients, from the forward's input, mean and rstd, and the gradient J_out of Y:
+ *     du = J_out act'(u) ;  dbeta = sum du ;  dgamma = sum du xhat       over all rows
+ *     J_in = rstd (gamma du - mean(gamma du) - xhat mean(gamma du xhat))
+ * with xhat = (X - mean) rstd and the means over the sample's group.  ReLU's slope is
+ * 1[u > 0], with u formed as in the forward.  J_in, dgamma and dbeta may each be NULL.
+ * The sums over rows are reduced in a fixed order.
+ */
+typedef struct {
+  int32_t dtype;               /* pgcn_dtype of X, J_out and J_in                */
+  int32_t act;
+  int32_t channels;
+  int32_t groups;
+  int64_t samples, sample_rows;
+  int64_t ld_x, ld_j_out, ld_j_in;
+  const void *X;               /* [samples * sample_rows, ld_x]                  */
+  const void *J_out;           /* [samples * sample_rows, ld_j_out]              */
+  const float *gamma, *beta;   /* as in the forward                              */
+  const float *mean, *rstd;    /* [samples, groups]                              */
+  void *J_in;                  /* [samples * sample_rows, ld_j_in] out or NULL   */
+  float *dgamma, *dbeta;       /* [channels] out or NULL                         */
+  void *workspace;
+  size_t workspace_bytes;
+} pgcn_group_norm_bwd_args;
+int pgcn_group_norm_bwd(const pgcn_group_norm_bwd_args *args, hipStream_t stream);
+/* Bytes that pgcn_group_norm_fwd and pgcn_group_norm_bwd need (the larger of both). */
+size_t pgcn_group_norm_workspace_size(int32_t dtype, int32_t channels, int32_t groups, int64_t samples,
+                                      int64_t sample_rows);
+
 /* Refill of a stale buffer (Algorithm 1's send/receive threads; the paper runs
  * them on a second stream): an asynchronous copy of `bytes` bytes into device
  * memory `dst`, enqueued on `stream`.  flags = 0: device-to-device on the
@@ -560,7 +710,8 @@ enum pgcn_trace_kind {
   PGCN_TK_GEMM_DGRAD = 4, PGCN_TK_GEMM_WGRAD = 5, PGCN_TK_WGRAD_REDUCE = 6, PGCN_TK_EMA = 7,
   PGCN_TK_PACK = 8, PGCN_TK_ACCUM = 9, PGCN_TK_LOSS = 10, PGCN_TK_SGD = 11, PGCN_TK_REFILL = 12,
   PGCN_TK_GEMM_PACK = 13, PGCN_TK_DROPOUT = 14, PGCN_TK_ADAM = 15, PGCN_TK_MASK_SCALE = 16,
-  PGCN_TK_ACCUM_EMA = 17
+  PGCN_TK_ACCUM_EMA = 17, PGCN_TK_TOP_LOGITS = 18, PGCN_TK_DISTILL = 19, PGCN_TK_GROUP_NORM = 20,
+  PGCN_TK_GROUP_NORM_BWD = 21
 };
 int pgcn_trace_enable(int32_t capacity);
 int pgcn_trace_filter(uint32_t kind_mask);

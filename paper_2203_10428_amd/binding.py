@@ -29,6 +29,8 @@ PGCN_SOFTMAX_CE, PGCN_SIGMOID_BCE = 0, 1
 PGCN_REFILL_DMA, PGCN_REFILL_FROM_HOST = 1, 2
 PGCN_ORDER_AGG, PGCN_ORDER_TRANSFORM = 0, 1
 PGCN_NOALLOC_SCRATCH_BYTES = 32 << 20
+PGCN_ACT_NONE, PGCN_ACT_RELU, PGCN_ACT_SILU, PGCN_ACT_GELU = range(4)
+PGCN_MAX_TOP, PGCN_MAX_CLASSES, PGCN_MAX_CHANNELS = 256, 262144, 8192
 
 _vp = C.c_void_p
 _i32, _i64, _u32, _f32, _sz = C.c_int32, C.c_int64, C.c_uint32, C.c_float, C.c_size_t
@@ -86,6 +88,32 @@ class pgcn_sage_bwd_args(C.Structure):
                 ("J_bd_out", _vp), ("workspace", _vp), ("workspace_bytes", _sz), ("order", _i32), ("X_bd", _vp)]
 
 
+class pgcn_top_logits_args(C.Structure):
+    _fields_ = [("dtype", _i32), ("classes", _i32), ("top", _i32), ("temperature", _f32), ("rows", _i64), ("ld", _i64),
+                ("ld_top", _i64), ("Z", _vp), ("top_values", _vp), ("top_ids", _vp), ("tail_lse", _vp),
+                ("workspace", _vp), ("workspace_bytes", _sz)]
+
+
+class pgcn_distill_args(C.Structure):
+    _fields_ = [("dtype", _i32), ("classes", _i32), ("top", _i32), ("temperature", _f32), ("rows", _i64), ("ld", _i64),
+                ("ld_top", _i64), ("soft_scale", _f32), ("hard_scale", _f32), ("Z", _vp), ("top_values", _vp),
+                ("top_ids", _vp), ("tail_lse", _vp), ("labels", _vp), ("J", _vp), ("loss_out", _vp),
+                ("workspace", _vp), ("workspace_bytes", _sz)]
+
+
+class pgcn_group_norm_fwd_args(C.Structure):
+    _fields_ = [("dtype", _i32), ("act", _i32), ("channels", _i32), ("groups", _i32), ("samples", _i64),
+                ("sample_rows", _i64), ("ld_x", _i64), ("ld_y", _i64), ("eps", _f32), ("X", _vp), ("gamma", _vp),
+                ("beta", _vp), ("Y", _vp), ("mean", _vp), ("rstd", _vp), ("workspace", _vp), ("workspace_bytes", _sz)]
+
+
+class pgcn_group_norm_bwd_args(C.Structure):
+    _fields_ = [("dtype", _i32), ("act", _i32), ("channels", _i32), ("groups", _i32), ("samples", _i64),
+                ("sample_rows", _i64), ("ld_x", _i64), ("ld_j_out", _i64), ("ld_j_in", _i64), ("X", _vp),
+                ("J_out", _vp), ("gamma", _vp), ("beta", _vp), ("mean", _vp), ("rstd", _vp), ("J_in", _vp),
+                ("dgamma", _vp), ("dbeta", _vp), ("workspace", _vp), ("workspace_bytes", _sz)]
+
+
 # every symbol include/pgcn.h declares, with its ctypes signature
 SIGNATURES = {
     "pgcn_partition_setup": (_i32, [C.POINTER(pgcn_csr), C.POINTER(pgcn_boundary_map), _u32, C.POINTER(_vp)]),
@@ -109,6 +137,13 @@ SIGNATURES = {
     "pgcn_sage_layer_fwd": (_i32, [_vp, C.POINTER(pgcn_sage_fwd_args), _vp]),
     "pgcn_sage_layer_bwd": (_i32, [_vp, C.POINTER(pgcn_sage_bwd_args), _vp]),
     "pgcn_refill_async": (_i32, [_vp, _vp, _sz, _u32, _vp]),
+    "pgcn_top_logits_workspace_size": (_sz, [_i32, _i64, _i32, _i32]),
+    "pgcn_top_logits": (_i32, [C.POINTER(pgcn_top_logits_args), _vp]),
+    "pgcn_distill_workspace_size": (_sz, [_i32, _i64, _i32, _i32]),
+    "pgcn_distill_loss_fwd_bwd": (_i32, [C.POINTER(pgcn_distill_args), _vp]),
+    "pgcn_group_norm_workspace_size": (_sz, [_i32, _i32, _i32, _i64, _i64]),
+    "pgcn_group_norm_fwd": (_i32, [C.POINTER(pgcn_group_norm_fwd_args), _vp]),
+    "pgcn_group_norm_bwd": (_i32, [C.POINTER(pgcn_group_norm_bwd_args), _vp]),
     "pgcn_trace_enable": (_i32, [_i32]),
     "pgcn_trace_filter": (_i32, [C.c_uint32]),
     "pgcn_trace_collect": (_i32, [_vp, _vp, _vp, _i32, C.POINTER(_i32)]),
@@ -313,9 +348,72 @@ def pgcn_refill_async(dst, src, nbytes: int, flags: int = 0, stream=None):
     _check(lib.pgcn_refill_async(_ptr(dst), _ptr(src), nbytes, flags, _stream(stream)), "pgcn_refill_async")
 
 
+def _same_device(*xs):
+    """Tensors of a call without a partition handle have to be on the current device (a pointer given as an
+    int is the caller's word)."""
+    cur = -1
+    for x in xs:
+        if isinstance(x, torch.Tensor):
+            if not x.is_cuda:
+                raise ValueError("a tensor of the call is not in device memory")
+            if cur < 0:
+                cur = torch.cuda.current_device()
+            if x.get_device() != cur:
+                raise ValueError("a tensor of the call is on another device than the current one")
+
+
+def pgcn_top_logits_workspace_size(dtype: int, rows: int, classes: int, top: int) -> int:
+    return int(lib.pgcn_top_logits_workspace_size(dtype, rows, classes, top))
+
+
+def pgcn_top_logits(*, dtype, rows, classes, ld, top, ld_top, temperature, Z, top_values, top_ids, tail_lse,
+                    workspace=None, workspace_bytes=0, stream=None):
+    _same_device(Z, top_values, top_ids, tail_lse, workspace)
+    a = pgcn_top_logits_args(dtype, classes, top, temperature, rows, ld, ld_top, _ptr(Z), _ptr(top_values),
+                             _ptr(top_ids), _ptr(tail_lse), _ptr(workspace), workspace_bytes)
+    _check(lib.pgcn_top_logits(C.byref(a), _stream(stream)), "pgcn_top_logits")
+
+
+def pgcn_distill_workspace_size(dtype: int, rows: int, classes: int, top: int) -> int:
+    return int(lib.pgcn_distill_workspace_size(dtype, rows, classes, top))
+
+
+def pgcn_distill_loss_fwd_bwd(*, dtype, rows, classes, ld, top, ld_top, temperature, soft_scale, hard_scale, Z,
+                              top_values, top_ids, tail_lse, labels, J, loss_out, workspace, workspace_bytes,
+                              stream=None):
+    _same_device(Z, top_values, top_ids, tail_lse, labels, J, loss_out, workspace)
+    a = pgcn_distill_args(dtype, classes, top, temperature, rows, ld, ld_top, soft_scale, hard_scale, _ptr(Z),
+                          _ptr(top_values), _ptr(top_ids), _ptr(tail_lse), _ptr(labels), _ptr(J), _ptr(loss_out),
+                          _ptr(workspace), workspace_bytes)
+    _check(lib.pgcn_distill_loss_fwd_bwd(C.byref(a), _stream(stream)), "pgcn_distill_loss_fwd_bwd")
+
+
+def pgcn_group_norm_workspace_size(dtype: int, channels: int, groups: int, samples: int, sample_rows: int) -> int:
+    return int(lib.pgcn_group_norm_workspace_size(dtype, channels, groups, samples, sample_rows))
+
+
+def pgcn_group_norm_fwd(*, dtype, act, channels, groups, samples, sample_rows, ld_x, ld_y, eps, X, gamma, beta, Y,
+                        mean, rstd, workspace=None, workspace_bytes=0, stream=None):
+    _same_device(X, gamma, beta, Y, mean, rstd, workspace)
+    a = pgcn_group_norm_fwd_args(dtype, act, channels, groups, samples, sample_rows, ld_x, ld_y, eps, _ptr(X),
+                                 _ptr(gamma), _ptr(beta), _ptr(Y), _ptr(mean), _ptr(rstd), _ptr(workspace),
+                                 workspace_bytes)
+    _check(lib.pgcn_group_norm_fwd(C.byref(a), _stream(stream)), "pgcn_group_norm_fwd")
+
+
+def pgcn_group_norm_bwd(*, dtype, act, channels, groups, samples, sample_rows, ld_x, ld_j_out, ld_j_in, X, J_out,
+                        gamma, beta, mean, rstd, J_in, dgamma, dbeta, workspace=None, workspace_bytes=0,
+                        stream=None):
+    _same_device(X, J_out, gamma, beta, mean, rstd, J_in, dgamma, dbeta, workspace)
+    a = pgcn_group_norm_bwd_args(dtype, act, channels, groups, samples, sample_rows, ld_x, ld_j_out, ld_j_in, _ptr(X),
+                                 _ptr(J_out), _ptr(gamma), _ptr(beta), _ptr(mean), _ptr(rstd), _ptr(J_in),
+                                 _ptr(dgamma), _ptr(dbeta), _ptr(workspace), workspace_bytes)
+    _check(lib.pgcn_group_norm_bwd(C.byref(a), _stream(stream)), "pgcn_group_norm_bwd")
+
+
 TRACE_KINDS = ["agg_fwd", "agg_bwd", "agg_fixup", "gemm_fwd", "gemm_dgrad", "gemm_wgrad", "wgrad_reduce", "ema",
                "pack", "accum", "loss", "sgd", "refill", "gemm_pack", "dropout", "adam", "mask_scale",
-               "accum_ema"]
+               "accum_ema", "top_logits", "distill", "group_norm", "group_norm_bwd"]
 
 
 def pgcn_trace_enable(capacity: int):

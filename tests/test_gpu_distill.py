@@ -1,0 +1,455 @@
+"""Top logits and the distillation loss on the GPU against ``oracle.ops`` (float64).
+
+Bounds.  u = 2^-24.  Every exponent argument is a difference of two fp32 logits times an fp32
+1/T (itself rounded once): 3 roundings, so an argument A is off by at most 3 u |A|, and the
+exponential by that and 2 u more; sums of n positive terms with chains of at most 64 + 16
+additions (a lane's own, then lanes and waves) by 80 u of themselves, a running maximum's
+rescalings (at most one per addition, 4 u each) by 320 u; logarithms of them by as much in the
+absolute, and 2 u |log|.  With EPS = 512 u:
+    log p, log q, log s:       |error| <= 4 u (|A| + |log|) + EPS =: d
+    a probability p:           p (e^d - 1) <= 1.01 p d   (d <= 0.01 in these tests)
+The loss sums p (log p - log q): |error| <= p (d_p + d_q) + 1.01 p d_p |log p - log q|, and 16 u of the
+absolute sum; J the differences.  A bf16 J is rounded once more, by half a step: 2^-8 |J|.  Results
+below the smallest normal may be flushed: 2^-126 absolute.
+"""
+import numpy as np
+import pytest
+import torch
+
+from oracle import ops
+from paper_2203_10428_amd import binding as B
+
+pytestmark = pytest.mark.gpu
+
+U = 2.0 ** -24
+EPS = 512 * U
+NINF = float("-inf")
+CODE = {"f32": B.PGCN_F32, "bf16": B.PGCN_BF16}
+DT = {"f32": torch.float32, "bf16": torch.bfloat16}
+
+
+def matrix(x, dtype, pad=8, fill=float("nan")):
+    """A device matrix with a row stride of its own; the padding holds NaN, which no result may show."""
+    rows, cols = x.shape
+    ld = (cols + 7) // 8 * 8 + pad
+    m = torch.full((rows, ld), fill, dtype=DT[dtype], device="cuda")
+    m[:, :cols] = torch.from_numpy(np.ascontiguousarray(x, dtype=np.float32)).to("cuda").to(DT[dtype])
+    return m
+
+
+def top(Z, C, K, T, dtype, ld_top=None, tail=True, stream=None):
+    rows, ld_top = Z.shape[0], ld_top or K
+    v = torch.full((rows, ld_top), 7.0, device="cuda")
+    i = torch.full((rows, ld_top), 77, dtype=torch.int32, device="cuda")
+    t = torch.full((rows + 1,), 777.0, device="cuda") if tail else None
+    n = B.pgcn_top_logits_workspace_size(CODE[dtype], rows, C, K)
+    ws = torch.full((max(n, 16),), 255, dtype=torch.uint8, device="cuda")
+    B.pgcn_top_logits(dtype=CODE[dtype], rows=rows, classes=C, ld=Z.stride(0), top=K, ld_top=ld_top, temperature=T, Z=Z,
+                      top_values=v, top_ids=i, tail_lse=t, workspace=ws, workspace_bytes=ws.numel(), stream=stream)
+    torch.cuda.synchronize()
+    assert (v[:, K:] == 7.0).all() and (i[:, K:] == 77).all() and (t is None or t[rows] == 777.0)
+    return v[:, :K].cpu().numpy(), i[:, :K].cpu().numpy(), None if t is None else t[:rows].cpu().numpy()
+
+
+def log_error(A, log):
+    """d of the module notes: A the largest argument in use, log the logarithm itself."""
+    return 4 * U * (np.abs(A) + np.abs(log)) + EPS
+
+
+def check_top(Z, C, K, T, dtype, **kw):
+    z = Z[:, :C].float().cpu().numpy().astype(np.float64)
+    v, i, t = top(Z, C, K, T, dtype, **kw)
+    rv, ri, rt = ops.top_logits(z, K, T)
+    assert np.array_equal(i, ri)
+    assert np.array_equal(v.astype(np.float64), rv)
+    if t is None:
+        return
+    assert np.array_equal(np.isnan(t), np.isnan(rt)) and np.array_equal(t == NINF, rt == NINF)
+    on = np.isfinite(rt)
+    zz = np.where(np.isfinite(z), np.abs(z), 0.0).max(axis=1, initial=0.0)
+    assert (np.abs(t - rt)[on] <= log_error(4 * zz / T, rt)[on]).all()
+
+
+def logits(rng, rows, C, scale=2.5):
+    return scale * rng.standard_normal((rows, C))
+
+
+# sizes around the edges of the kernels: lanes, waves, vectors, registers, parts of a row
+SIZES = [(1, 1, 1), (5, 2, 2), (3, 8, 4), (257, 8, 8), (1000, 41, 8), (33, 47, 16), (70, 64, 64), (65, 65, 5), (19, 100, 100),
+         (9, 129, 7), (130, 256, 32), (4, 257, 200), (6, 1000, 256), (3, 2047, 64), (3, 2049, 17), (2, 8193, 50),
+         (3, 16385, 128), (2, 40000, 64), (1, 65537, 50), (1, 131073, 256), (17, 33000, 9)]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,C,K", SIZES)
+def test_top_logits_sizes(rows, C, K, dtype):
+    rng = np.random.default_rng(rows + C)
+    check_top(matrix(logits(rng, rows, C), dtype), C, K, 2.0, dtype, ld_top=K + 3)
+
+
+@pytest.mark.parametrize("C,K", [(41, 8), (100, 64), (300, 32), (5000, 64), (40000, 200), (131072, 256)])
+@pytest.mark.parametrize("kind", ["equal", "ties", "rising", "falling", "masked", "one_left", "none_left", "lowest", "inf", "zeros",
+                                  "last_block"])
+def test_top_logits_orders_and_masks(C, K, kind):
+    rng = np.random.default_rng(C)
+    z = logits(rng, 3, C)
+    if kind == "equal":
+        z[:] = 1.25
+    elif kind == "ties":
+        z = np.round(z)
+    elif kind == "rising":
+        z = np.tile(np.arange(C) / 64.0, (3, 1))
+    elif kind == "falling":
+        z = np.tile(-np.arange(C) / 64.0, (3, 1))
+    elif kind == "masked":
+        z[:, rng.random(C) < 0.9] = NINF
+    elif kind == "one_left":
+        z[:] = NINF
+        z[:, C - 1] = -3.0
+    elif kind == "none_left":
+        z[1] = NINF
+    elif kind == "lowest":
+        z[:, 1:] = float(np.finfo(np.float32).min)
+    elif kind == "inf":
+        z[0, C // 2] = np.inf
+        z[1, 0] = np.nan
+        z[2, C - 1] = np.nan
+    elif kind == "zeros":
+        z[:] = np.where(rng.random(z.shape) < 0.5, 0.0, -0.0)
+    else:
+        z[:, -min(C, 300):] += 50.0
+    check_top(matrix(z, "f32"), C, K, 1.0 if kind == "lowest" else 0.7, "f32")
+
+
+def test_top_logits_many_short_rows():
+    rng = np.random.default_rng(5)
+    for rows, C, K, dtype in ((70001, 41, 8, "f32"), (40003, 47, 16, "bf16"), (30001, 100, 4, "f32"), (20011, 30, 30, "f32")):
+        Z = matrix(np.round(logits(rng, rows, C), 1), dtype)
+        v, i, t = top(Z, C, K, 1.5, dtype)
+        z = Z[:, :C].float().cpu()
+        order = torch.sort(z, dim=1, descending=True, stable=True)
+        assert np.array_equal(i, order.indices[:, :K].int().numpy()) and np.array_equal(v, order.values[:, :K].numpy())
+        if K < C:
+            rt = torch.logsumexp(order.values[:, K:].double() / 1.5, 1).numpy()
+            assert (np.abs(t - rt) <= log_error(4 * 20.0 / 1.5, rt)).all()
+        else:
+            assert (t == NINF).all()
+
+
+def test_top_logits_without_a_tail():
+    rng = np.random.default_rng(6)
+    for rows, C, K in ((50, 41, 8), (3, 9000, 30), (1, 100003, 50)):
+        check_top(matrix(logits(rng, rows, C), "f32"), C, K, 1.0, "f32", tail=False)
+
+
+# ------------------------------------------------------------------ distill --
+
+def call(Z, C, v, i, tail, labels, T, soft, hard, dtype, stream=None, J=None, ws=None, loss=None):
+    rows = Z.shape[0]
+    J = torch.full_like(Z, 5.0) if J is None else J
+    loss = torch.full((2,), 7.0, device="cuda") if loss is None else loss
+    n = B.pgcn_distill_workspace_size(CODE[dtype], rows, C, v.shape[1])
+    ws = torch.full((max(n, 16),), 255, dtype=torch.uint8, device="cuda") if ws is None else ws
+    B.pgcn_distill_loss_fwd_bwd(dtype=CODE[dtype], rows=rows, classes=C, ld=Z.stride(0), top=v.shape[1], ld_top=v.stride(0),
+                                temperature=T, soft_scale=soft, hard_scale=hard, Z=Z, top_values=v, top_ids=i, tail_lse=tail,
+                                labels=labels, J=J, loss_out=loss, workspace=ws, workspace_bytes=ws.numel(), stream=stream)
+    return J, loss
+
+
+def row_bounds(z, v, i, tail, y, T, soft, hard):
+    """Bounds of one row's J (before its rounding to bf16) and loss, by the module notes."""
+    fin = np.where(np.isfinite(z), z, 0.0)
+    span = 2 * np.abs(fin).max()
+    listed = np.zeros(len(z), bool)
+    first = {}
+    for c, t in zip(i, v):
+        if c >= 0 and c not in first:
+            first[int(c)] = float(t)
+    listed[list(first)] = True
+    jb, lb = np.zeros(len(z)), 0.0
+    if any(t > NINF for t in first.values()):
+        A = span / T
+        lq = z / T - ops._lse(z / T)
+        q = np.exp(lq)
+        tt = np.array(list(first.values())) / T
+        tot = ops._lse(tt) if tail is None else ops._lse(np.append(tt, tail))
+        At = 2 * np.abs(tt[np.isfinite(tt)]).max() + (abs(tail) if tail is not None and np.isfinite(tail) else 0.0)
+        p, dp = np.zeros(len(z)), np.zeros(len(z))
+        for c, t in first.items():
+            if t == NINF:
+                continue
+            lp = t / T - tot
+            p[c], dp[c] = np.exp(lp), log_error(At, lp)
+            dq = log_error(A, lq[c])
+            lb += soft * (p[c] * (dp[c] + dq) + 1.01 * p[c] * (dp[c] + 16 * U) * abs(lp - lq[c]))
+        dq = np.where(np.isfinite(lq), log_error(A, np.where(np.isfinite(lq), lq, 0.0)), 0.0)
+        jb += soft / T * 1.01 * (q * dq + p * dp)
+        if tail is not None and tail > NINF:
+            lr = tail - tot
+            rho, dr = np.exp(lr), log_error(At, lr)
+            ls = ops._lse(z[~listed] / T) - ops._lse(z / T)
+            if np.isfinite(ls):
+                ds = log_error(A, ls)
+                lb += soft * (rho * (dr + ds) + 1.01 * rho * (dr + 16 * U) * abs(lr - ls))
+                within = np.exp(lq - ls)
+                jb += np.where(listed, 0.0, soft / T * within * (1.01 * (np.exp(ls) * ds + rho * dr) + (np.exp(ls) + rho) * dq))
+    if y >= 0:
+        l1 = z - ops._lse(z)
+        d1 = np.where(np.isfinite(l1), log_error(span, np.where(np.isfinite(l1), l1, 0.0)), 0.0)
+        jb += hard * 1.01 * np.exp(l1) * d1
+        jb[y] += hard * 2 * U
+        lb += hard * log_error(span, l1[y])
+    return jb, lb
+
+
+def check(Z, C, v, i, tail, labels, T, soft, hard, dtype):
+    J, loss = call(Z, C, v, i, tail, labels, T, soft, hard, dtype)
+    torch.cuda.synchronize()
+    assert (J[:, C:] == 5.0).all() and loss[1] == 7.0
+    z = Z[:, :C].float().cpu().numpy().astype(np.float64)
+    vn, ic = v.cpu().numpy().astype(np.float64), i.cpu().numpy()
+    tn = None if tail is None else tail.cpu().numpy().astype(np.float64)
+    yn = None if labels is None else labels.cpu().numpy()
+    soft, hard, T = float(np.float32(soft)), float(np.float32(hard)), float(np.float32(T))
+    ref_loss, ref = ops.distill(z, vn, ic, tn, yn, T, soft, hard)
+    j = J[:, :C].float().cpu().numpy().astype(np.float64)
+    lb = 0.0
+    for r in range(len(z)):
+        b, l = row_bounds(z[r], vn[r], ic[r], None if tn is None else tn[r], -1 if yn is None else int(yn[r]), T, soft, hard)
+        b = b + 4 * U * np.abs(ref[r]) + 2.0 ** -126
+        if dtype == "bf16":
+            b = b * (1 + 2.0 ** -8) + 2.0 ** -8 * np.abs(ref[r])
+        assert (np.abs(j[r] - ref[r]) <= b).all(), (r, np.abs(j[r] - ref[r]).max())
+        lb += l
+    got = float(loss[0])
+    if np.isinf(ref_loss):
+        assert got == ref_loss
+    else:
+        assert abs(got - ref_loss) <= lb + 2 * U * abs(ref_loss) + len(z) * 2.0 ** -126, (got, ref_loss, lb)
+
+
+def teacher(rng, z, K, T, none=0.1):
+    """Top logits of perturbed rows, as the entry point lists them; some rows list nothing."""
+    v, i, tail = ops.top_logits(z + np.where(np.isfinite(z), rng.standard_normal(z.shape), 0.0), K, T)
+    i[rng.random(len(z)) < none] = -1
+    return v, i, tail
+
+
+def put(v, i, tail, ld=None):
+    K = v.shape[1]
+    vt = torch.full((len(v), ld or K), float("nan"), device="cuda")
+    it = torch.full((len(v), ld or K), 1 << 30, dtype=torch.int32, device="cuda")
+    vt[:, :K] = torch.from_numpy(v.astype(np.float32)).cuda()
+    it[:, :K] = torch.from_numpy(i.astype(np.int32)).cuda()
+    return vt[:, :K], it[:, :K], None if tail is None else torch.from_numpy(tail.astype(np.float32)).cuda()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,C,K", SIZES)
+def test_distill_sizes(rows, C, K, dtype):
+    rng = np.random.default_rng(rows * 7 + C)
+    T = [1.0, 2.0, 0.6][(rows + C) % 3]
+    Z = matrix(logits(rng, rows, C), dtype)
+    z = Z[:, :C].float().cpu().numpy().astype(np.float64)
+    v, i, tail = put(*teacher(rng, z, K, T), ld=K + 1)
+    y = torch.from_numpy(rng.integers(-1, C, rows).astype(np.int32)).cuda()
+    check(Z, C, v, i, tail, y, T, 0.8 * T * T / rows, 0.3 / rows, dtype)
+    check(Z, C, v, i, None, None, T, 1.0, 0.0, dtype)
+
+
+@pytest.mark.parametrize("rows,C,K", [(40, 41, 8), (12, 300, 60), (3, 5000, 64), (2, 70000, 40)])
+@pytest.mark.parametrize("kind", ["masked", "sure", "far", "all_absent", "repeats", "inf_slots", "offset", "label_in_list", "lowest",
+                                  "covers_all"])
+def test_distill_masks_and_lists(rows, C, K, kind):
+    rng = np.random.default_rng(C + K)
+    z, T = logits(rng, rows, C).astype(np.float32).astype(np.float64), 1.3
+    y = rng.integers(-1, C, rows)
+    if kind == "masked":
+        off = rng.random(C) < 0.6
+        off[0] = False
+        z[:, off] = NINF
+        y = np.where(off[y], 0, y)
+    elif kind == "sure":                    # the student is sure: s is far below 1, not lost
+        z[:, 0] = 40.0
+    elif kind == "far":                     # the rest underflows relative to the listed classes
+        z[:, 1] = 150.0
+    v, i, tail = teacher(rng, z, K, T, none=0.2)
+    if kind == "sure" or kind == "far":
+        tail = np.where(np.isfinite(tail), np.maximum(tail, v[:, 0] / T - 1.0), tail)
+    elif kind == "all_absent":
+        i[:] = -1
+        v[:] = np.nan
+    elif kind == "repeats":
+        i[:, K // 2] = i[:, 0]
+        i[:, K - 1] = i[:, 0]
+    elif kind == "inf_slots":
+        v[:, K // 2:] = NINF
+        v[0] = NINF
+    elif kind == "offset":
+        v, tail = v + 300.0, tail + 300.0 / T
+    elif kind == "label_in_list":
+        y = np.where(i[:, K - 1] >= 0, i[:, K - 1], 0)
+    elif kind == "lowest":                  # a mask of the type's lowest value
+        z[:, C // 2:] = float(np.finfo(np.float32).min)
+        z[1, :] = float(np.finfo(np.float32).min)
+        y = np.where(y >= C // 2, 0, y)
+        i = np.where(i >= C // 2, -1, i)
+    elif kind == "covers_all" and C <= 300:
+        v, i, tail = teacher(rng, z, min(C, 256), T, none=0.2)
+    Z = matrix(z, "f32")
+    v, i, tail = put(v, i, tail)
+    y = torch.from_numpy(y.astype(np.int32)).cuda()
+    if kind == "lowest":                    # the row of lowest values alone: no loss bound, its span is not a number
+        J, loss = call(Z, C, v, i, None, y, T, 1.0, 1.0, "f32")
+        assert torch.isfinite(J[:, :C]).all() and torch.isfinite(loss[0])
+        keep = [r for r in range(rows) if r != 1]
+        ref = ops.distill(np.where(z < -1e30, NINF, z)[keep], v.cpu().numpy()[keep].astype(np.float64), i.cpu().numpy()[keep], None,
+                          y.cpu().numpy()[keep], float(np.float32(T)), 1.0, 1.0)[1]
+        assert np.abs(J[keep, :C].cpu().numpy() - ref).max() <= 2 * EPS
+        return
+    check(Z, C, v, i, tail, y, T, 0.9, 0.4, "f32")
+    check(Z, C, v, i, tail, None, T, 0.9, 0.4, "f32")
+
+
+@pytest.mark.parametrize("rows,C,K", [(20, 41, 8), (5, 700, 8), (2, 40000, 8), (1, 200000, 8)])
+def test_distill_poison(rows, C, K):
+    """What the interface says of ids and labels out of range, NaN, and rows without a finite logit."""
+    rng = np.random.default_rng(C)
+    z = logits(rng, rows, C)
+    tv, ti, tail = put(*teacher(rng, z, K, 1.0, none=0.0))
+    y = torch.zeros(rows, dtype=torch.int32, device="cuda")
+    args = (tail, y, 1.0, 1.0, 1.0, "f32")
+
+    def run(z_=None, v=tv, i=ti, lab=y):
+        J, loss = call(matrix(z if z_ is None else z_, "f32"), C, v, i, tail, lab, 1.0, 1.0, 1.0, "f32")
+        torch.cuda.synchronize()
+        return J[:, :C], float(loss[0])
+
+    J0, l0 = run()
+    assert np.isfinite(l0) and torch.isfinite(J0).all()
+    i2 = ti.clone()
+    i2[0, 3] = C
+    J, l = run(i=i2)
+    assert np.isnan(l) and torch.isfinite(J).all()
+    for bad in (C, C + 5, -2):
+        y2 = y.clone()
+        y2[rows - 1] = bad
+        J, l = run(lab=y2)
+        assert np.isnan(l) and torch.isfinite(J).all()
+    z2 = z.copy()
+    z2[rows - 1, C - 1] = np.nan
+    J, l = run(z_=z2)
+    assert np.isnan(l) and torch.isnan(J[rows - 1]).all()
+    assert rows == 1 or torch.equal(J[:rows - 1], J0[:rows - 1])
+    v2 = tv.clone()
+    v2[0, 1] = float("nan")
+    J, l = run(v=v2)
+    assert np.isnan(l) and torch.isnan(J[0]).all()
+    z3 = z.copy()
+    z3[0] = NINF
+    assert np.isnan(run(z_=z3)[1])
+    i3, y3 = ti.clone(), y.clone()          # ... and without a term it adds nothing
+    i3[0], y3[0] = -1, -1
+    J, l = run(z_=z3, i=i3, lab=y3)
+    assert np.isfinite(l) and (J[0] == 0).all()
+
+
+def test_distill_no_rows():
+    loss = torch.full((1,), 3.0, device="cuda")
+    B.pgcn_distill_loss_fwd_bwd(dtype=B.PGCN_F32, rows=0, classes=41, ld=48, top=8, ld_top=8, temperature=1.0, soft_scale=1.0,
+                                hard_scale=1.0, Z=None, top_values=None, top_ids=None, tail_lse=None, labels=None, J=None,
+                                loss_out=loss, workspace=None, workspace_bytes=0)
+    torch.cuda.synchronize()
+    assert float(loss[0]) == 0.0
+
+
+@pytest.mark.parametrize("rows,C,K", [(3001, 41, 8), (64, 9000, 40), (2, 131071, 64)])
+def test_distill_is_reproducible_on_any_stream_and_in_a_graph(rows, C, K):
+    """Equal inputs give equal bits: again, on another stream, with another workspace content, and replayed
+    from a graph between eager calls."""
+    rng = np.random.default_rng(3)
+    Z = matrix(logits(rng, rows, C), "f32")
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    v = torch.empty(rows, K, device="cuda")
+    i = torch.empty(rows, K, dtype=torch.int32, device="cuda")
+    tail = torch.empty(rows, device="cuda")
+    n = max(16, B.pgcn_top_logits_workspace_size(B.PGCN_F32, rows, C, K), B.pgcn_distill_workspace_size(B.PGCN_F32, rows, C, K))
+    ws = torch.zeros(n, dtype=torch.uint8, device="cuda")
+    J, loss = torch.empty_like(Z), torch.empty(2, device="cuda")
+    S = matrix(logits(rng, rows, C), "f32")
+    y = torch.from_numpy(rng.integers(-1, C, rows).astype(np.int32)).cuda()
+
+    def run(stream):
+        B.pgcn_top_logits(dtype=B.PGCN_F32, rows=rows, classes=C, ld=Z.stride(0), top=K, ld_top=K, temperature=2.0, Z=Z, top_values=v,
+                          top_ids=i, tail_lse=tail, workspace=ws, workspace_bytes=n, stream=stream)
+        call(S, C, v, i, tail, y, 2.0, 0.5, 0.5, "f32", stream, J, ws, loss)
+
+    run(torch.cuda.current_stream())
+    torch.cuda.synchronize()
+    want = [t.clone() for t in (v, i, tail, J[:, :C], loss[:1])]
+
+    def same():
+        torch.cuda.synchronize()
+        got = (v, i, tail, J[:, :C], loss[:1])
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+        for t in (v, tail, J, loss):
+            t.fill_(9.0)
+        i.zero_()
+        ws.fill_(255)
+        torch.cuda.synchronize()
+
+    same()
+    run(side)
+    same()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=side):
+        run(torch.cuda.current_stream())
+    for _ in range(3):
+        g.replay()
+        same()
+        run(torch.cuda.current_stream())
+        same()
+
+
+def test_two_calls_at_once():
+    """Two streams, a workspace each."""
+    rng = np.random.default_rng(4)
+    sets = []
+    for k in range(2):
+        Z = matrix(logits(rng, 5000, 41), "f32")
+        z = Z[:, :41].cpu().numpy().astype(np.float64)
+        sets.append((Z, *put(*teacher(rng, z, 8, 1.0)), torch.cuda.Stream()))
+    want = []
+    for Z, v, i, tail, _ in sets:
+        J, loss = call(Z, 41, v, i, tail, None, 1.0, 1.0, 0.0, "f32")
+        torch.cuda.synchronize()
+        want.append((J[:, :41].clone(), loss.clone()))
+    bufs = [(torch.full_like(s[0], 5.0), torch.full((2,), 7.0, device="cuda"),
+             torch.zeros(B.pgcn_distill_workspace_size(B.PGCN_F32, 5000, 41, 8), dtype=torch.uint8, device="cuda")) for s in sets]
+    torch.cuda.synchronize()
+    for _ in range(4):
+        for (Z, v, i, tail, st), (J, loss, ws) in zip(sets, bufs):
+            call(Z, 41, v, i, tail, None, 1.0, 1.0, 0.0, "f32", st, J, ws, loss)
+    torch.cuda.synchronize()
+    for (J, loss, _), (rj, rl) in zip(bufs, want):
+        assert torch.equal(J[:, :41], rj) and torch.equal(loss, rl)
+
+
+def test_a_student_learns_its_teachers_list():
+    """The gradient against differences of the loss itself (fp32 logits, a step far above their rounding)."""
+    rng = np.random.default_rng(8)
+    z = logits(rng, 1, 41, 1.0).astype(np.float32)
+    v, i, tail = put(*teacher(rng, z.astype(np.float64), 8, 2.0, none=0.0))
+    y = torch.tensor([3], dtype=torch.int32, device="cuda")
+    J = call(matrix(z, "f32"), 41, v, i, tail, y, 2.0, 1.0, 1.0, "f32")[0][0, :41].cpu().numpy()
+    h = 2.0 ** -6
+    for c in range(0, 41, 5):
+        d = []
+        for s in (h, -h):
+            zz = z.copy()
+            zz[0, c] += s
+            d.append(float(call(matrix(zz, "f32"), 41, v, i, tail, y, 2.0, 1.0, 1.0, "f32")[1][0]))
+        # a log-sum's third derivative is below 1, and there are three: h^2 / 2; each loss is off by
+        # at most d_p + d_q of the soft and d of the hard term, below 4 EPS here, and J by less than that
+        assert abs((d[0] - d[1]) / (2 * h) - J[c]) <= h * h / 2 + 4 * EPS / h + 4 * EPS
