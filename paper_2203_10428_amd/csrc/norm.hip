@@ -21,24 +21,55 @@ constexpr int kThreads = 256;
 
 // ------------------------------------------------------------ activations --
 
-template <int kAct>
-__device__ __forceinline__ float act(float u) {
-  if (kAct == PGCN_ACT_RELU) return u > 0.f || u != u ? u : 0.f;      // a NaN stays one
-  if (kAct == PGCN_ACT_SILU) return u / (1.0f + __expf(-u));
-  if (kAct == PGCN_ACT_GELU) return 0.5f * u * (1.0f + erff(u * 0.70710678118654752f));
-  return u;
+__device__ __forceinline__ float sigmoid(float u) { return __builtin_amdgcn_rcpf(1.0f + __expf(-u)); }
+
+// The normal distribution's Phi(u) and e^{-u^2 / 2}: erfc by Hastings' fifth-degree form
+// (Abramowitz and Stegun 7.1.26, within 1.5e-7), taken on the side where nothing cancels.
+__device__ __forceinline__ float normal_cdf(float u, float &e) {
+  const float x = fabsf(u) * 0.70710678118654752f, t = __builtin_amdgcn_rcpf(1.0f + 0.3275911f * x);
+  e = __expf(-x * x);
+  const float tail = 0.5f * e * t * (0.254829592f + t * (-0.284496736f + t * (1.421413741f + t * (-1.453152027f + t * 1.061405429f))));
+  return u < 0.f ? tail : 1.0f - tail;
 }
 
-template <int kAct>
-__device__ __forceinline__ float act_slope(float u) {
-  if (kAct == PGCN_ACT_RELU) return u > 0.f ? 1.f : 0.f;
-  if (kAct == PGCN_ACT_SILU) {
-    const float g = 1.0f / (1.0f + __expf(-u));
-    return g * (1.0f + u * (1.0f - g));
+// y = act(u), the choice once for a whole array
+template <int N>
+__device__ __forceinline__ void activate(float (&u)[N], int act) {
+  if (act == PGCN_ACT_RELU) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) u[i] = u[i] <= 0.f ? 0.f : u[i];      // a NaN stays one
+  } else if (act == PGCN_ACT_SILU) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) u[i] *= sigmoid(u[i]);
+  } else if (act == PGCN_ACT_GELU) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      float e;
+      u[i] *= normal_cdf(u[i], e);
+    }
   }
-  if (kAct == PGCN_ACT_GELU)
-    return 0.5f * (1.0f + erff(u * 0.70710678118654752f)) + u * __expf(-0.5f * u * u) * 0.39894228040143268f;
-  return 1.f;
+}
+
+// j *= act'(u)
+template <int N>
+__device__ __forceinline__ void times_slope(float (&j)[N], const float (&u)[N], int act) {
+  if (act == PGCN_ACT_RELU) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) j[i] = u[i] > 0.f ? j[i] : 0.f;
+  } else if (act == PGCN_ACT_SILU) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const float g = sigmoid(u[i]);
+      j[i] *= g * (1.0f + u[i] * (1.0f - g));
+    }
+  } else if (act == PGCN_ACT_GELU) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      float e;
+      const float c = normal_cdf(u[i], e);
+      j[i] *= c + u[i] * e * 0.39894228040143268f;
+    }
+  }
 }
 
 __device__ __forceinline__ float normed(float x, float mu, float r) {
@@ -181,7 +212,7 @@ __global__ __launch_bounds__(kThreads) void moments_kernel(pgcn_group_norm_fwd_a
 }
 
 // Joins a sample's chunks, normalises `per` of its rows.
-template <class T, int kAct>
+template <class T>
 __global__ __launch_bounds__(kThreads) void normalise_kernel(pgcn_group_norm_fwd_args a, Cut cut, int64_t per, int blocks,
                                                              int sh, const float2 *part) {
   extern __shared__ float lds[];                        // mean, 1 / deviation: [2][groups]
@@ -219,14 +250,15 @@ __global__ __launch_bounds__(kThreads) void normalise_kernel(pgcn_group_norm_fwd
       float x[T::E];
       T::unpack(*reinterpret_cast<const typename T::raw *>((const typename T::type *)a.X + (row0 + r) * a.ld_x + vec * T::E), x);
 #pragma unroll
-      for (int e = 0; e < T::E; ++e) x[e] = act<kAct>(affine(normed(x[e], mu[e], rs[e]), ga[e], be[e]));
+      for (int e = 0; e < T::E; ++e) x[e] = affine(normed(x[e], mu[e], rs[e]), ga[e], be[e]);
+      activate(x, a.act);
       store_some<T>((typename T::type *)a.Y + (row0 + r) * a.ld_y + vec * T::E, x, f - vec * T::E);
     }
   }
 }
 
 // Sums of du and du xhat for every channel over one chunk of one sample: part[block][2][channels].
-template <class T, int kAct>
+template <class T>
 __global__ __launch_bounds__(kThreads) void grad_sums_kernel(pgcn_group_norm_bwd_args a, Cut cut, int sh, float *part) {
   __shared__ float red[2][kThreads * 8];
   const int f = a.channels, cg = f / a.groups, vecs = (f + T::E - 1) / T::E, lx = 1 << sh, ty = kThreads >> sh;
@@ -251,11 +283,17 @@ __global__ __launch_bounds__(kThreads) void grad_sums_kernel(pgcn_group_norm_bwd
         float x[T::E], j[T::E];
         T::unpack(*reinterpret_cast<const typename T::raw *>((const typename T::type *)a.X + (row0 + r) * a.ld_x + vec * T::E), x);
         T::unpack(*reinterpret_cast<const typename T::raw *>((const typename T::type *)a.J_out + (row0 + r) * a.ld_j_out + vec * T::E), j);
+        float u[T::E];
 #pragma unroll
         for (int e = 0; e < T::E; ++e) {
-          const float xh = normed(x[e], mu[e], rs[e]), du = j[e] * act_slope<kAct>(affine(xh, ga[e], be[e]));
-          s1[e] += du;
-          s2[e] += du * xh;
+          x[e] = normed(x[e], mu[e], rs[e]);
+          u[e] = affine(x[e], ga[e], be[e]);
+        }
+        times_slope(j, u, a.act);
+#pragma unroll
+        for (int e = 0; e < T::E; ++e) {
+          s1[e] += j[e];
+          s2[e] += j[e] * x[e];
         }
       }
     }
@@ -300,25 +338,25 @@ __global__ __launch_bounds__(kThreads) void add_chunks_kernel(const float *part,
 
 // Sums over the samples: dbeta from the first half of sums[sample][2][channels], dgamma from the second.
 __global__ __launch_bounds__(kThreads) void param_grads_kernel(const float *sums, int64_t samples, int f, float *dgamma, float *dbeta) {
-  __shared__ float red[kThreads];
+  __shared__ double red[kThreads];
   const int i = blockIdx.x * 32 + (threadIdx.x & 31), slot = threadIdx.x >> 5;
-  float s = 0.f;
+  double s = 0.0;                                       // thousands of terms in one chain
   if (i < 2 * f)
-    for (int64_t b = slot; b < samples; b += kThreads / 32) s += sums[b * 2 * f + i];
+    for (int64_t b = slot; b < samples; b += kThreads / 32) s += (double)sums[b * 2 * f + i];
   red[threadIdx.x] = s;
   __syncthreads();
   if (slot == 0 && i < 2 * f) {
     for (int k = 1; k < kThreads / 32; ++k) s += red[threadIdx.x + 32 * k];
     if (i < f) {
-      if (dbeta) dbeta[i] = s;
+      if (dbeta) dbeta[i] = (float)s;
     } else if (dgamma) {
-      dgamma[i - f] = s;
+      dgamma[i - f] = (float)s;
     }
   }
 }
 
 // dX of `per` rows of a sample, from the sample's channel sums.
-template <class T, int kAct>
+template <class T>
 __global__ __launch_bounds__(kThreads) void grad_rows_kernel(pgcn_group_norm_bwd_args a, int64_t per, int blocks, int sh,
                                                              const float *sums) {
   extern __shared__ float lds[];                        // c1, c2: [2][groups]
@@ -356,12 +394,273 @@ __global__ __launch_bounds__(kThreads) void grad_rows_kernel(pgcn_group_norm_bwd
       float x[T::E], j[T::E];
       T::unpack(*reinterpret_cast<const typename T::raw *>((const typename T::type *)a.X + (row0 + r) * a.ld_x + vec * T::E), x);
       T::unpack(*reinterpret_cast<const typename T::raw *>((const typename T::type *)a.J_out + (row0 + r) * a.ld_j_out + vec * T::E), j);
+      float u[T::E];
 #pragma unroll
       for (int e = 0; e < T::E; ++e) {
-        const float xh = normed(x[e], mu[e], rs[e]), du = j[e] * act_slope<kAct>(affine(xh, ga[e], be[e]));
-        x[e] = rs[e] * (ga[e] * du - c1[e] - xh * c2[e]);
+        x[e] = normed(x[e], mu[e], rs[e]);
+        u[e] = affine(x[e], ga[e], be[e]);
       }
+      times_slope(j, u, a.act);
+#pragma unroll
+      for (int e = 0; e < T::E; ++e) x[e] = rs[e] * (ga[e] * j[e] - c1[e] - x[e] * c2[e]);
       store_some<T>((typename T::type *)a.J_in + (row0 + r) * a.ld_j_in + vec * T::E, x, f - vec * T::E);
+    }
+  }
+}
+
+// ------------------------------------------------- one row to a sample ----
+//
+// kLanes threads hold a row, kVecs 16-byte vectors each (vector lane + kLanes i), so that X (and
+// J) cross the memory once and both passes over the row stay in registers.  A workgroup walks
+// rows at a fixed stride: gamma, beta and the backward's channel sums stay in registers too.
+// How a group's sum is formed:
+enum class Sum {
+  ROW,     // one group: all the row's threads
+  LANES,   // groups of 2^k neighbouring vectors: shuffles inside them
+  LDS      // any other: the row's values through LDS, a team of lanes for each group
+};
+
+struct RowShape {
+  int f, groups, cg, vecs;
+  int span;            // LANES: vectors of a group
+  int team;            // LDS: lanes of a team
+  uint32_t magic;      // c / cg = umulhi(c, magic) for c < 2^13; 0: cg is 1
+};
+
+__device__ __forceinline__ int group_of(const RowShape &sp, int c) { return sp.magic ? (int)__umulhi((uint32_t)c, sp.magic) : c; }
+
+template <int kLanes>
+__device__ __forceinline__ void row_sync() {
+  if (kLanes > 64) {
+    __syncthreads();
+  } else {                       // the row's threads are lanes of one wave, whose LDS accesses keep their order
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+  }
+}
+
+// Sums of w over every group, to every element of it: out[i][e], or out[i][0] for the vector.
+// `lds`: the row's own f + groups floats (LDS), or kThreads / 64 floats (ROW over several waves).
+template <class T, int kLanes, int kVecs, Sum kSum, int kOut>
+__device__ __forceinline__ void group_sums(const float (&w)[kVecs][T::E], float (&out)[kVecs][kOut], const RowShape &sp, float *lds) {
+  const int lane = threadIdx.x % kLanes;
+  if (kSum == Sum::LDS) {
+    float *res = lds + (sp.f + 3) / 4 * 4;
+    row_sync<kLanes>();
+#pragma unroll
+    for (int i = 0; i < kVecs; ++i)
+#pragma unroll
+      for (int e = 0; e < T::E; ++e) {
+        const int c = (lane + kLanes * i) * T::E + e;
+        if (c < sp.f) lds[c] = w[i][e];
+      }
+    row_sync<kLanes>();
+    const int t = lane & (sp.team - 1), teams = kLanes / sp.team;
+    for (int g0 = 0; g0 < sp.groups; g0 += teams) {                   // the same rounds for every lane
+      const int g = g0 + lane / sp.team;
+      float s = 0.f;
+      if (g < sp.groups)
+        for (int c = t; c < sp.cg; c += sp.team) s += lds[g * sp.cg + c];
+      for (int o = sp.team / 2; o > 0; o >>= 1) s += __shfl_xor(s, o, 64);
+      if (t == 0 && g < sp.groups) res[g] = s;
+    }
+    row_sync<kLanes>();
+#pragma unroll
+    for (int i = 0; i < kVecs; ++i)
+#pragma unroll
+      for (int e = 0; e < kOut; ++e) {
+        const int c = (lane + kLanes * i) * T::E + e;
+        out[i][e] = res[group_of(sp, c < sp.f ? c : 0)];
+      }
+    return;
+  }
+  float s[kVecs];
+#pragma unroll
+  for (int i = 0; i < kVecs; ++i) {
+    float h[T::E / 2];
+#pragma unroll
+    for (int e = 0; e < T::E / 2; ++e) h[e] = w[i][e] + w[i][e + T::E / 2];
+    s[i] = T::E == 4 ? h[0] + h[1] : (h[0] + h[T::E / 4]) + (h[1] + h[T::E / 2 - 1]);
+  }
+  if (kSum == Sum::ROW) {
+    float r = s[0];
+#pragma unroll
+    for (int i = 1; i < kVecs; ++i) r += s[i];
+#pragma unroll
+    for (int o = (kLanes < 64 ? kLanes : 64) / 2; o > 0; o >>= 1) r += __shfl_xor(r, o, 64);
+    if (kLanes > 64) {
+      __syncthreads();
+      if (threadIdx.x % 64 == 0) lds[threadIdx.x / 64] = r;
+      __syncthreads();
+      r = (lds[0] + lds[1]) + (lds[2] + lds[3]);
+    }
+#pragma unroll
+    for (int i = 0; i < kVecs; ++i) out[i][0] = r;
+  } else {
+    for (int o = 1; o < sp.span; o <<= 1)
+#pragma unroll
+      for (int i = 0; i < kVecs; ++i) s[i] += __shfl_xor(s[i], o, 64);
+#pragma unroll
+    for (int i = 0; i < kVecs; ++i) out[i][0] = s[i];
+  }
+}
+
+template <class T, int kVecs>
+__device__ __forceinline__ void load_params(const float *p, float other, int f, int v0, int step, float (&out)[kVecs][T::E]) {
+#pragma unroll
+  for (int i = 0; i < kVecs; ++i)
+#pragma unroll
+    for (int e = 0; e < T::E; ++e) {
+      const int c = (v0 + step * i) * T::E + e;
+      out[i][e] = p && c < f ? p[c] : other;
+    }
+}
+
+template <class T, int kVecs>
+__device__ __forceinline__ void load_row(const void *base, int64_t off, int vecs, int v0, int step, float (&x)[kVecs][T::E]) {
+  const typename T::type *p = (const typename T::type *)base + off;
+#pragma unroll
+  for (int i = 0; i < kVecs; ++i) {
+    typename T::raw r = {};
+    if (v0 + step * i < vecs) r = *reinterpret_cast<const typename T::raw *>(p + (v0 + step * i) * T::E);
+    T::unpack(r, x[i]);
+  }
+}
+
+template <class T, int kLanes, int kVecs, Sum kSum>
+__global__ __launch_bounds__(kThreads) void rows_fwd_kernel(pgcn_group_norm_fwd_args a, RowShape sp, int lds_row) {
+  extern __shared__ float lds_all[];
+  constexpr int kOut = kSum == Sum::LDS ? T::E : 1;
+  const int lane = threadIdx.x % kLanes, slot = threadIdx.x / kLanes;
+  float *lds = lds_all + slot * lds_row;
+  float ga[kVecs][T::E], be[kVecs][T::E];
+  load_params<T>(a.gamma, 1.f, sp.f, lane, kLanes, ga);
+  load_params<T>(a.beta, 0.f, sp.f, lane, kLanes, be);
+  const float inv_n = 1.0f / (float)sp.cg;
+  for (int64_t r = (int64_t)blockIdx.x * (kThreads / kLanes) + slot; r < a.samples; r += (int64_t)gridDim.x * (kThreads / kLanes)) {
+    float x[kVecs][T::E], w[kVecs][T::E], mu[kVecs][kOut], rs[kVecs][kOut];
+    load_row<T>(a.X, r * a.ld_x, sp.vecs, lane, kLanes, x);
+#pragma unroll
+    for (int i = 0; i < kVecs; ++i)
+#pragma unroll
+      for (int e = 0; e < T::E; ++e) w[i][e] = x[i][e] = (lane + kLanes * i) * T::E + e < sp.f ? x[i][e] : 0.f;
+    group_sums<T, kLanes, kVecs, kSum>(w, mu, sp, lds);
+#pragma unroll
+    for (int i = 0; i < kVecs; ++i) {
+#pragma unroll
+      for (int e = 0; e < kOut; ++e) mu[i][e] *= inv_n;
+#pragma unroll
+      for (int e = 0; e < T::E; ++e) {
+        const float d = x[i][e] - mu[i][e % kOut];
+        w[i][e] = (lane + kLanes * i) * T::E + e < sp.f ? d * d : 0.f;
+      }
+    }
+    group_sums<T, kLanes, kVecs, kSum>(w, rs, sp, lds);
+#pragma unroll
+    for (int i = 0; i < kVecs; ++i) {
+      const int c0 = (lane + kLanes * i) * T::E;
+#pragma unroll
+      for (int e = 0; e < kOut; ++e) rs[i][e] = 1.0f / sqrtf(rs[i][e] * inv_n + a.eps);
+      if (c0 < sp.f) {
+        // the thread with a group's first channel writes its statistics
+#pragma unroll
+        for (int e = 0; e < kOut; ++e) {
+          const int c = c0 + e, g = group_of(sp, c);
+          if (c < sp.f && g * sp.cg == c) {
+            if (a.mean) a.mean[r * sp.groups + g] = mu[i][e];
+            if (a.rstd) a.rstd[r * sp.groups + g] = rs[i][e];
+          }
+        }
+#pragma unroll
+        for (int e = 0; e < T::E; ++e) x[i][e] = affine(normed(x[i][e], mu[i][e % kOut], rs[i][e % kOut]), ga[i][e], be[i][e]);
+        activate(x[i], a.act);
+        store_some<T>((typename T::type *)a.Y + r * a.ld_y + c0, x[i], sp.f - c0);
+      }
+    }
+  }
+}
+
+// The backward of those rows; a workgroup's channel sums go to part[workgroup][2][channels].
+template <class T, int kLanes, int kVecs, Sum kSum>
+__global__ __launch_bounds__(kThreads) void rows_bwd_kernel(pgcn_group_norm_bwd_args a, RowShape sp, int lds_row, float *part) {
+  extern __shared__ float lds_all[];
+  constexpr int kOut = kSum == Sum::LDS ? T::E : 1;
+  const int lane = threadIdx.x % kLanes, slot = threadIdx.x / kLanes;
+  float *lds = lds_all + slot * lds_row;
+  float ga[kVecs][T::E], be[kVecs][T::E], s1[kVecs][T::E] = {}, s2[kVecs][T::E] = {};
+  load_params<T>(a.gamma, 1.f, sp.f, lane, kLanes, ga);
+  load_params<T>(a.beta, 0.f, sp.f, lane, kLanes, be);
+  const float inv_n = 1.0f / (float)sp.cg;
+  for (int64_t r = (int64_t)blockIdx.x * (kThreads / kLanes) + slot; r < a.samples; r += (int64_t)gridDim.x * (kThreads / kLanes)) {
+    float x[kVecs][T::E], j[kVecs][T::E], w[kVecs][T::E], c1[kVecs][kOut], c2[kVecs][kOut], rs[kVecs][kOut];
+    load_row<T>(a.X, r * a.ld_x, sp.vecs, lane, kLanes, x);
+    load_row<T>(a.J_out, r * a.ld_j_out, sp.vecs, lane, kLanes, j);
+#pragma unroll
+    for (int i = 0; i < kVecs; ++i) {
+      const int c0 = (lane + kLanes * i) * T::E;
+      float mu[kOut], u[T::E];
+#pragma unroll
+      for (int e = 0; e < kOut; ++e) {
+        const int64_t g = r * sp.groups + group_of(sp, c0 + e < sp.f ? c0 + e : 0);
+        mu[e] = a.mean[g];
+        rs[i][e] = a.rstd[g];
+      }
+#pragma unroll
+      for (int e = 0; e < T::E; ++e) {
+        x[i][e] = normed(x[i][e], mu[e % kOut], rs[i][e % kOut]);
+        u[e] = affine(x[i][e], ga[i][e], be[i][e]);
+      }
+      times_slope(j[i], u, a.act);
+#pragma unroll
+      for (int e = 0; e < T::E; ++e) {
+        const bool in = c0 + e < sp.f;
+        x[i][e] = in ? x[i][e] : 0.f;
+        j[i][e] = in ? j[i][e] : 0.f;
+        s1[i][e] += j[i][e];
+        s2[i][e] += j[i][e] * x[i][e];
+        j[i][e] *= ga[i][e];
+        w[i][e] = j[i][e] * x[i][e];
+      }
+    }
+    if (!a.J_in) continue;
+    group_sums<T, kLanes, kVecs, kSum>(j, c1, sp, lds);
+    group_sums<T, kLanes, kVecs, kSum>(w, c2, sp, lds);
+#pragma unroll
+    for (int i = 0; i < kVecs; ++i) {
+      const int c0 = (lane + kLanes * i) * T::E;
+#pragma unroll
+      for (int e = 0; e < T::E; ++e)
+        x[i][e] = rs[i][e % kOut] * (j[i][e] - c1[i][e % kOut] * inv_n - x[i][e] * (c2[i][e % kOut] * inv_n));
+      if (c0 < sp.f) store_some<T>((typename T::type *)a.J_in + r * a.ld_j_in + c0, x[i], sp.f - c0);
+    }
+  }
+  if (!part) return;
+  // join the workgroup's row slots (fixed order), each half of the sums in turn
+  constexpr int kSlots = kThreads / kLanes;
+  float *p = part + (int64_t)blockIdx.x * 2 * sp.f;
+#pragma unroll
+  for (int half = 0; half < 2; ++half) {
+#pragma unroll
+    for (int i = 0; i < kVecs; ++i) {
+      float v[T::E];
+#pragma unroll
+      for (int e = 0; e < T::E; ++e) v[e] = half ? s2[i][e] : s1[i][e];
+      if (kSlots > 1) {
+        __syncthreads();
+#pragma unroll
+        for (int e = 0; e < T::E; ++e) lds_all[e * kThreads + threadIdx.x] = v[e];
+        __syncthreads();
+        if (slot == 0) {
+#pragma unroll
+          for (int e = 0; e < T::E; ++e)
+            for (int k = 1; k < kSlots; ++k) v[e] += lds_all[e * kThreads + k * kLanes + lane];
+        }
+      }
+      const int c0 = (lane + kLanes * i) * T::E;
+      if (slot == 0)
+#pragma unroll
+        for (int e = 0; e < T::E; ++e)
+          if (c0 + e < sp.f) p[half * sp.f + c0 + e] = v[e];
     }
   }
 }
@@ -383,26 +682,126 @@ Shape shape_of(int32_t dtype, int32_t channels, int64_t samples, int64_t sample_
   return s;
 }
 
-template <class T, int kAct>
-int fwd(const pgcn_group_norm_fwd_args &a, hipStream_t s) {
+// part[n][2][channels] summed over n.
+int launch_param_grads(const float *part, int64_t n, int channels, float *dgamma, float *dbeta, hipStream_t s) {
+  hipLaunchKernelGGL(param_grads_kernel, dim3((unsigned)((2 * channels + 31) / 32)), dim3(kThreads), 0, s, part, n, channels, dgamma,
+                     dbeta);
+  PGCN_HIP(hipGetLastError());
+  return PGCN_OK;
+}
+
+// ---- launches: rows --------------------------------------------------------
+
+bool is_pow2(int x) { return (x & (x - 1)) == 0; }
+
+RowShape row_shape(int32_t dtype, int32_t f, int32_t groups, int lanes) {
+  const int e = dtype == PGCN_BF16 ? BF16::E : F32::E;
+  RowShape sp;
+  sp.f = f;
+  sp.groups = groups;
+  sp.cg = f / groups;
+  sp.vecs = (f + e - 1) / e;
+  sp.span = sp.cg % e == 0 ? sp.cg / e : 0;
+  sp.team = 1;
+  while (sp.team < 64 && 2 * sp.team * groups <= lanes) sp.team *= 2;
+  sp.magic = sp.cg > 1 ? (uint32_t)(((uint64_t(1) << 32) + sp.cg - 1) / sp.cg) : 0;
+  return sp;
+}
+
+// Threads and vectors a row: the fewest lanes that hold it in one vector each, a wave up to 4,
+// then a workgroup.
+void row_threads(int vecs, int &lanes, int &per) {
+  lanes = vecs <= 16 ? 16 : vecs <= 32 ? 32 : vecs <= 256 ? 64 : kThreads;
+  per = 1;
+  while (lanes * per < vecs) per *= 2;
+}
+
+constexpr int kRowBlocksFwd = 2048, kRowBlocksBwd = 1024;
+
+unsigned row_blocks(int64_t rows, int lanes, int most) {
+  const int64_t n = kThreads / lanes, b = (rows + n - 1) / n;
+  return (unsigned)std::min<int64_t>(b, most);
+}
+
+template <class T, int kLanes, int kVecs, Sum kSum>
+int rows_fwd_go(const pgcn_group_norm_fwd_args &a, const RowShape &sp, hipStream_t s) {
+  const int row = kSum == Sum::LDS ? (sp.f + 3) / 4 * 4 + (sp.groups + 3) / 4 * 4 : 4;
+  hipLaunchKernelGGL((rows_fwd_kernel<T, kLanes, kVecs, kSum>), dim3(row_blocks(a.samples, kLanes, kRowBlocksFwd)), dim3(kThreads),
+                     (size_t)(kThreads / kLanes) * row * 4, s, a, sp, row);
+  PGCN_HIP(hipGetLastError());
+  return PGCN_OK;
+}
+
+template <class T, int kLanes, int kVecs, Sum kSum>
+int rows_bwd_go(const pgcn_group_norm_bwd_args &a, const RowShape &sp, hipStream_t s) {
+  const int row = kSum == Sum::LDS ? (sp.f + 3) / 4 * 4 + (sp.groups + 3) / 4 * 4 : 4;
+  const unsigned blocks = row_blocks(a.samples, kLanes, kRowBlocksBwd);
+  float *part = a.dgamma || a.dbeta ? (float *)a.workspace : nullptr;
+  if (!part && !a.J_in) return PGCN_OK;
+  const size_t lds = std::max((size_t)(kThreads / kLanes) * row, (size_t)(kThreads * T::E)) * 4;
+  hipLaunchKernelGGL((rows_bwd_kernel<T, kLanes, kVecs, kSum>), dim3(blocks), dim3(kThreads), lds, s, a, sp, row, part);
+  PGCN_HIP(hipGetLastError());
+  return part ? launch_param_grads(part, blocks, a.channels, a.dgamma, a.dbeta, s) : PGCN_OK;
+}
+
+#define PGCN_ROW_SHAPES(go, T, a, s)                                                                              \
+  int lanes, per;                                                                                                 \
+  row_threads((a.channels + T::E - 1) / T::E, lanes, per);                                                        \
+  const RowShape sp = row_shape(a.dtype, a.channels, a.groups, lanes);                                            \
+  const int how = sp.groups == 1 ? 0 : sp.span > 0 && is_pow2(sp.span) && sp.span <= lanes && lanes <= 64 ? 1 : 2; \
+  switch (lanes * 100 + per * 10 + how) {                                                                         \
+    case 1610: return go<T, 16, 1, Sum::ROW>(a, sp, s);                                                           \
+    case 1611: return go<T, 16, 1, Sum::LANES>(a, sp, s);                                                         \
+    case 1612: return go<T, 16, 1, Sum::LDS>(a, sp, s);                                                           \
+    case 3210: return go<T, 32, 1, Sum::ROW>(a, sp, s);                                                           \
+    case 3211: return go<T, 32, 1, Sum::LANES>(a, sp, s);                                                         \
+    case 3212: return go<T, 32, 1, Sum::LDS>(a, sp, s);                                                           \
+    case 6410: return go<T, 64, 1, Sum::ROW>(a, sp, s);                                                           \
+    case 6411: return go<T, 64, 1, Sum::LANES>(a, sp, s);                                                         \
+    case 6412: return go<T, 64, 1, Sum::LDS>(a, sp, s);                                                           \
+    case 6420: return go<T, 64, 2, Sum::ROW>(a, sp, s);                                                           \
+    case 6421: return go<T, 64, 2, Sum::LANES>(a, sp, s);                                                         \
+    case 6422: return go<T, 64, 2, Sum::LDS>(a, sp, s);                                                           \
+    case 6440: return go<T, 64, 4, Sum::ROW>(a, sp, s);                                                           \
+    case 6441: return go<T, 64, 4, Sum::LANES>(a, sp, s);                                                         \
+    case 6442: return go<T, 64, 4, Sum::LDS>(a, sp, s);                                                           \
+    case 25620: return go<T, 256, 2, Sum::ROW>(a, sp, s);                                                         \
+    case 25622: return go<T, 256, 2, Sum::LDS>(a, sp, s);                                                         \
+    case 25640: return go<T, 256, 4, Sum::ROW>(a, sp, s);                                                         \
+    case 25642: return go<T, 256, 4, Sum::LDS>(a, sp, s);                                                         \
+    case 25680: return go<T, 256, 8, Sum::ROW>(a, sp, s);                                                         \
+    default: return go<T, 256, 8, Sum::LDS>(a, sp, s);                                                            \
+  }
+
+template <class T>
+int rows_fwd(const pgcn_group_norm_fwd_args &a, hipStream_t s) {
+  PGCN_ROW_SHAPES(rows_fwd_go, T, a, s)
+}
+template <class T>
+int rows_bwd(const pgcn_group_norm_bwd_args &a, hipStream_t s) {
+  PGCN_ROW_SHAPES(rows_bwd_go, T, a, s)
+}
+
+template <class T>
+int fwd_chunks(const pgcn_group_norm_fwd_args &a, hipStream_t s) {
   const Shape sp = shape_of(a.dtype, a.channels, a.samples, a.sample_rows);
   float2 *part = (float2 *)a.workspace;
   hipLaunchKernelGGL(moments_kernel<T>, dim3((unsigned)(a.samples * sp.stat.chunks)), dim3(kThreads), 8 * (size_t)a.channels, s,
                      a, sp.stat, sp.sh, part);
   PGCN_HIP(hipGetLastError());
-  hipLaunchKernelGGL((normalise_kernel<T, kAct>), dim3((unsigned)(a.samples * sp.apply.chunks)), dim3(kThreads), 8 * (size_t)a.groups,
+  hipLaunchKernelGGL(normalise_kernel<T>, dim3((unsigned)(a.samples * sp.apply.chunks)), dim3(kThreads), 8 * (size_t)a.groups,
                      s, a, sp.stat, sp.apply.per, sp.apply.chunks, sp.sh, part);
   PGCN_HIP(hipGetLastError());
   return PGCN_OK;
 }
 
-template <class T, int kAct>
-int bwd(const pgcn_group_norm_bwd_args &a, hipStream_t s) {
+template <class T>
+int bwd_chunks(const pgcn_group_norm_bwd_args &a, hipStream_t s) {
   const Shape sp = shape_of(a.dtype, a.channels, a.samples, a.sample_rows);
   const int w = 2 * a.channels;
   float *part = (float *)a.workspace, *sums = part;
   if (a.samples > 0) {
-    hipLaunchKernelGGL((grad_sums_kernel<T, kAct>), dim3((unsigned)(a.samples * sp.stat.chunks)), dim3(kThreads), 0, s, a, sp.stat,
+    hipLaunchKernelGGL(grad_sums_kernel<T>, dim3((unsigned)(a.samples * sp.stat.chunks)), dim3(kThreads), 0, s, a, sp.stat,
                        sp.sh, part);
     PGCN_HIP(hipGetLastError());
     if (sp.stat.chunks > 1) {
@@ -414,12 +813,11 @@ int bwd(const pgcn_group_norm_bwd_args &a, hipStream_t s) {
     }
   }
   if (a.dgamma || a.dbeta) {
-    hipLaunchKernelGGL(param_grads_kernel, dim3((unsigned)((w + 31) / 32)), dim3(kThreads), 0, s, sums, a.samples, a.channels,
-                       a.dgamma, a.dbeta);
-    PGCN_HIP(hipGetLastError());
+    const int rc = launch_param_grads(sums, a.samples, a.channels, a.dgamma, a.dbeta, s);
+    if (rc) return rc;
   }
   if (a.J_in && a.samples > 0) {
-    hipLaunchKernelGGL((grad_rows_kernel<T, kAct>), dim3((unsigned)(a.samples * sp.apply.chunks)), dim3(kThreads),
+    hipLaunchKernelGGL(grad_rows_kernel<T>, dim3((unsigned)(a.samples * sp.apply.chunks)), dim3(kThreads),
                        8 * (size_t)a.groups, s, a, sp.apply.per, sp.apply.chunks, sp.sh, sums);
     PGCN_HIP(hipGetLastError());
   }
@@ -430,33 +828,29 @@ int bwd(const pgcn_group_norm_bwd_args &a, hipStream_t s) {
 
 size_t group_norm_workspace(int32_t dtype, int32_t channels, int32_t groups, int64_t samples, int64_t sample_rows) {
   if (samples == 0) return 0;
+  if (sample_rows == 1) {
+    int lanes, per;
+    const int e = dtype == PGCN_BF16 ? BF16::E : F32::E;
+    row_threads((channels + e - 1) / e, lanes, per);
+    return 8 * (size_t)channels * row_blocks(samples, lanes, kRowBlocksBwd);
+  }
   const Shape sp = shape_of(dtype, channels, samples, sample_rows);
   const size_t f = 8 * (size_t)samples * (size_t)sp.stat.chunks * (size_t)groups;
   const size_t b = 8 * (size_t)channels * (size_t)samples * (size_t)(sp.stat.chunks + 1);
   return std::max(f, b);
 }
 
-#define PGCN_BY_TYPE(fn, a, s)                                               \
-  switch ((a.dtype == PGCN_BF16 ? 4 : 0) + a.act) {                          \
-    case 0: return fn<F32, PGCN_ACT_NONE>(a, s);                             \
-    case 1: return fn<F32, PGCN_ACT_RELU>(a, s);                             \
-    case 2: return fn<F32, PGCN_ACT_SILU>(a, s);                             \
-    case 3: return fn<F32, PGCN_ACT_GELU>(a, s);                             \
-    case 4: return fn<BF16, PGCN_ACT_NONE>(a, s);                            \
-    case 5: return fn<BF16, PGCN_ACT_RELU>(a, s);                            \
-    case 6: return fn<BF16, PGCN_ACT_SILU>(a, s);                            \
-    default: return fn<BF16, PGCN_ACT_GELU>(a, s);                           \
-  }
-
 int launch_group_norm_fwd(const pgcn_group_norm_fwd_args &a, hipStream_t s) {
   if (a.samples == 0) return PGCN_OK;
   TraceScope ts(PGCN_TK_GROUP_NORM, s);
-  PGCN_BY_TYPE(fwd, a, s)
+  if (a.sample_rows == 1) return a.dtype == PGCN_BF16 ? rows_fwd<BF16>(a, s) : rows_fwd<F32>(a, s);
+  return a.dtype == PGCN_BF16 ? fwd_chunks<BF16>(a, s) : fwd_chunks<F32>(a, s);
 }
 
 int launch_group_norm_bwd(const pgcn_group_norm_bwd_args &a, hipStream_t s) {
   TraceScope ts(PGCN_TK_GROUP_NORM_BWD, s);
-  PGCN_BY_TYPE(bwd, a, s)
+  if (a.sample_rows == 1 && a.samples > 0) return a.dtype == PGCN_BF16 ? rows_bwd<BF16>(a, s) : rows_bwd<F32>(a, s);
+  return a.dtype == PGCN_BF16 ? bwd_chunks<BF16>(a, s) : bwd_chunks<F32>(a, s);
 }
 
 }  // namespace pgcn
