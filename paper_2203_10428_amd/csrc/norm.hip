@@ -101,29 +101,38 @@ __device__ __forceinline__ Moments join(const Moments &a, const Moments &b) {
   return r;
 }
 
-// How a sample's rows are cut: `chunks` ranges of `per` rows (the last may be shorter), so that
-// few long samples fill the chip too.
+// ---------------------------------------------- samples of many rows -------
+//
+// Two launches: the first leaves each chunk's group statistics, the second joins a sample's
+// chunks in every workgroup and writes the rows.  Few long samples are cut into enough chunks
+// to fill the chip.
+//
+// A workgroup's threads: lx side by side on a row's vectors (all of them where a row has at most
+// 256), ty row slots above one another, the rest idle.
 struct Cut {
-  int64_t per;
+  int vecs, lx, ty;
+  int64_t per;           // rows of a chunk (the last may be shorter)
   int chunks;
+  int64_t out_per;       // rows of a workgroup of the second launch
+  int out_blocks;
 };
 
-// Column layout of a workgroup: 1 << sh lanes side by side on a row's vectors, the rest on rows.
-int column_shift(int vecs) {
-  int sh = 0;
-  while (sh < 8 && (1 << sh) < vecs) ++sh;
-  return sh;
-}
+constexpr int kBatch = 4;              // rows that a thread loads together
+constexpr int kChunkBlocks = 1024;     // workgroups of a launch, about: 4 for each compute unit
 
-constexpr int kMaxChunks = 256;
-
-Cut cut_rows(int64_t samples, int64_t sample_rows, int64_t min_rows) {
-  samples = std::max<int64_t>(1, samples);
-  int64_t want = std::max<int64_t>(1, 1024 / samples);
-  want = std::min<int64_t>(std::min<int64_t>(want, kMaxChunks), (sample_rows + min_rows - 1) / min_rows);
+Cut cut_rows(int32_t dtype, int32_t channels, int64_t samples, int64_t sample_rows) {
+  const int e = dtype == PGCN_BF16 ? BF16::E : F32::E;
   Cut c;
-  c.per = (sample_rows + want - 1) / want;
+  c.vecs = (channels + e - 1) / e;
+  const int tiles = (c.vecs + kThreads - 1) / kThreads;
+  c.lx = (c.vecs + tiles - 1) / tiles;
+  c.ty = kThreads / c.lx;
+  const int64_t least = (int64_t)kBatch * c.ty, most = std::max<int64_t>(1, kChunkBlocks / std::max<int64_t>(1, samples));
+  const int64_t parts = std::min(most, (sample_rows + least - 1) / least);
+  c.per = (sample_rows + parts - 1) / parts;
   c.chunks = (int)((sample_rows + c.per - 1) / c.per);
+  c.out_per = c.per;
+  c.out_blocks = c.chunks;
   return c;
 }
 
@@ -132,52 +141,141 @@ __device__ __forceinline__ int64_t chunk_rows(int64_t sample_rows, int64_t per, 
   return left < per ? left : per;
 }
 
-// Moments of every group over one chunk of one sample.  part[(sample chunks + chunk) groups + g] = (mu, M2).
+// One value for every group, formed by teams of lanes: value(g, lane of the team, team size)
+// gives a lane's part, which the team adds up; done(g, sum) is called once a group.
+template <class Value, class Done>
+__device__ __forceinline__ void for_groups(int groups, Value value, Done done) {
+  int team = 1;
+  while (team < 64 && 2 * team * groups <= kThreads) team *= 2;
+  const int t = threadIdx.x & (team - 1), teams = kThreads / team;
+  for (int g0 = 0; g0 < groups; g0 += teams) {
+    const int g = g0 + threadIdx.x / team;
+    float s = g < groups ? value(g, t, team) : 0.f;
+    for (int o = team / 2; o > 0; o >>= 1) s += __shfl_xor(s, o, 64);
+    if (g < groups && t == 0) done(g, s);
+  }
+}
+
+// Joins the chunks' (mean, M2) or adds up their sums, one result for each of the groups:
+// done(g, joined).  Threads side by side take neighbouring groups, the others every ty-th chunk.
+template <class Done>
+__device__ __forceinline__ void join_chunks(const float2 *part, int chunks, int groups, int64_t sample_rows, int64_t per, int cg,
+                                            Moments *red, Done done) {
+  const int wide = groups < kThreads ? groups : kThreads, deep = kThreads / wide;
+  const int tx = threadIdx.x % wide, slot = threadIdx.x / wide;
+  for (int g0 = 0; g0 < groups; g0 += wide) {
+    const int g = g0 + tx;
+    Moments m;
+    if (g < groups && slot < deep)
+      for (int c = slot; c < chunks; c += deep) {
+        const float2 p = part[(int64_t)c * groups + g];
+        m = join(m, Moments{(float)chunk_rows(sample_rows, per, c) * (float)cg, p.x, p.y});
+      }
+    __syncthreads();
+    red[threadIdx.x].n = m.n;
+    red[threadIdx.x].mu = m.mu;
+    red[threadIdx.x].m2 = m.m2;
+    __syncthreads();
+    for (int n = deep; n > 1; n = (n + 1) / 2) {
+      const int half = (n + 1) / 2;
+      if (slot + half < n) red[threadIdx.x] = join(red[threadIdx.x], red[threadIdx.x + half * wide]);
+      __syncthreads();
+    }
+    if (slot == 0 && g < groups) done(g, red[threadIdx.x]);
+  }
+}
+
+template <class Done>
+__device__ __forceinline__ void add_chunks(const float2 *part, int chunks, int groups, float2 *red, Done done) {
+  const int wide = groups < kThreads ? groups : kThreads, deep = kThreads / wide;
+  const int tx = threadIdx.x % wide, slot = threadIdx.x / wide;
+  for (int g0 = 0; g0 < groups; g0 += wide) {
+    const int g = g0 + tx;
+    float2 m = make_float2(0.f, 0.f);
+    if (g < groups && slot < deep)
+      for (int c = slot; c < chunks; c += deep) {
+        const float2 p = part[(int64_t)c * groups + g];
+        m.x += p.x;
+        m.y += p.y;
+      }
+    __syncthreads();
+    red[threadIdx.x] = m;
+    __syncthreads();
+    for (int n = deep; n > 1; n = (n + 1) / 2) {
+      const int half = (n + 1) / 2;
+      if (slot + half < n) {
+        red[threadIdx.x].x += red[threadIdx.x + half * wide].x;
+        red[threadIdx.x].y += red[threadIdx.x + half * wide].y;
+      }
+      __syncthreads();
+    }
+    if (slot == 0 && g < groups) done(g, red[threadIdx.x]);
+  }
+}
+
+// Moments of every group over one chunk of one sample: part[(sample chunks + chunk) groups + g] = (mu, M2).
 template <class T>
-__global__ __launch_bounds__(kThreads) void moments_kernel(pgcn_group_norm_fwd_args a, Cut cut, int sh, float2 *part) {
-  extern __shared__ float lds[];                        // channel mean, channel M2: [2][channels]
-  __shared__ float red[2][kThreads * 8];
-  const int f = a.channels, vecs = (f + T::E - 1) / T::E, lx = 1 << sh, ty = kThreads >> sh;
-  const int tx = threadIdx.x & (lx - 1), slot = threadIdx.x >> sh;
+__global__ __launch_bounds__(kThreads) void moments_kernel(pgcn_group_norm_fwd_args a, Cut cut, float2 *part) {
+  extern __shared__ float lds[];                        // channel mean, channel M2: [2][channels], then the group means
+  __shared__ float red[2][T::E][kThreads];
+  __shared__ int cnt[kThreads];
+  const int f = a.channels, tx = threadIdx.x % cut.lx, slot = threadIdx.x / cut.lx;
   const int64_t sample = blockIdx.x / cut.chunks;
   const int chunk = (int)(blockIdx.x - sample * cut.chunks);
   const int64_t rows = chunk_rows(a.sample_rows, cut.per, chunk);
   const typename T::type *x0 = (const typename T::type *)a.X + (sample * a.sample_rows + (int64_t)chunk * cut.per) * a.ld_x;
 
-  for (int v0 = 0; v0 < vecs; v0 += lx) {
+  for (int v0 = 0; v0 < cut.vecs; v0 += cut.lx) {
     const int vec = v0 + tx;
     float mu[T::E] = {}, m2[T::E] = {};
     int n = 0;
-    if (vec < vecs) {
-      for (int64_t r = slot; r < rows; r += ty) {
-        float x[T::E];
-        T::unpack(*reinterpret_cast<const typename T::raw *>(x0 + r * a.ld_x + vec * T::E), x);
-        ++n;
-        const float w = 1.0f / (float)n;
+    if (vec < cut.vecs && slot < cut.ty) {
+      for (int64_t r = slot; r < rows; r += kBatch * cut.ty) {
+        // a batch's own moments first, then one join: fewer steps in the chain
+        typename T::raw raw[kBatch];
+        int k = 0;
 #pragma unroll
-        for (int e = 0; e < T::E; ++e) {                // Welford's recurrence
-          const float d = x[e] - mu[e];
-          mu[e] += d * w;
-          m2[e] += d * (x[e] - mu[e]);
-        }
-      }
-    }
-    // join the row slots, halving them; slot s has seen ceil((rows - s) / ty) rows
-    for (int half = ty / 2; half > 0; half >>= 1) {
+        for (int b = 0; b < kBatch; ++b)
+          if (r + b * cut.ty < rows) {
+            raw[b] = *reinterpret_cast<const typename T::raw *>(x0 + (r + b * cut.ty) * a.ld_x + vec * T::E);
+            k = b + 1;
+          }
+        float x[kBatch][T::E];
 #pragma unroll
-      for (int e = 0; e < T::E; ++e) {
-        red[0][threadIdx.x * T::E + e] = mu[e];
-        red[1][threadIdx.x * T::E + e] = m2[e];
-      }
-      __shared__ int cnt[kThreads];
-      cnt[threadIdx.x] = n;
-      __syncthreads();
-      if (slot < half) {
-        const int o = threadIdx.x + half * lx;
-        const int no = cnt[o];
+        for (int b = 0; b < kBatch; ++b) T::unpack(raw[b < k ? b : 0], x[b]);
+        const float inv_k = 1.0f / (float)k, w = (float)k / (float)(n + k), wn = (float)n * w;
 #pragma unroll
         for (int e = 0; e < T::E; ++e) {
-          const Moments m = join(Moments{(float)n, mu[e], m2[e]}, Moments{(float)no, red[0][o * T::E + e], red[1][o * T::E + e]});
+          float s = 0.f, q = 0.f;
+#pragma unroll
+          for (int b = 0; b < kBatch; ++b) s += b < k ? x[b][e] : 0.f;
+          const float bm = s * inv_k;
+#pragma unroll
+          for (int b = 0; b < kBatch; ++b) {
+            const float d = x[b][e] - bm;
+            q += b < k ? d * d : 0.f;
+          }
+          const float d = bm - mu[e];
+          mu[e] += d * w;
+          m2[e] += q + d * d * wn;
+        }
+        n += k;
+      }
+    }
+    for (int left = cut.ty; left > 1; left = (left + 1) / 2) {      // join the row slots
+      const int half = (left + 1) / 2;
+#pragma unroll
+      for (int e = 0; e < T::E; ++e) {
+        red[0][e][threadIdx.x] = mu[e];
+        red[1][e][threadIdx.x] = m2[e];
+      }
+      cnt[threadIdx.x] = n;
+      __syncthreads();
+      if (slot + half < left) {
+        const int o = threadIdx.x + half * cut.lx, no = cnt[o];
+#pragma unroll
+        for (int e = 0; e < T::E; ++e) {
+          const Moments m = join(Moments{(float)n, mu[e], m2[e]}, Moments{(float)no, red[0][e][o], red[1][e][o]});
           mu[e] = m.mu;
           m2[e] = m.m2;
         }
@@ -185,7 +283,7 @@ __global__ __launch_bounds__(kThreads) void moments_kernel(pgcn_group_norm_fwd_a
       }
       __syncthreads();
     }
-    if (slot == 0 && vec < vecs) {
+    if (slot == 0 && vec < cut.vecs) {
 #pragma unroll
       for (int e = 0; e < T::E; ++e)
         if (vec * T::E + e < f) {
@@ -197,35 +295,33 @@ __global__ __launch_bounds__(kThreads) void moments_kernel(pgcn_group_norm_fwd_a
   __syncthreads();
   // a group's channels all have `rows` elements: mu is their average, M2 gains their spread
   const int cg = f / a.groups;
-  for (int g = threadIdx.x; g < a.groups; g += kThreads) {
+  float *mean = lds + 2 * f;
+  for_groups(a.groups, [&](int g, int t, int team) {
     float s = 0.f;
-    for (int c = 0; c < cg; ++c) s += lds[g * cg + c];
-    const float mu = s / (float)cg;
-    float m2 = 0.f, d2 = 0.f;
-    for (int c = 0; c < cg; ++c) {
-      const float d = lds[g * cg + c] - mu;
-      m2 += lds[f + g * cg + c];
-      d2 += d * d;
+    for (int c = t; c < cg; c += team) s += lds[g * cg + c];
+    return s;
+  }, [&](int g, float s) { mean[g] = s / (float)cg; });
+  __syncthreads();
+  for_groups(a.groups, [&](int g, int t, int team) {
+    float s = 0.f;
+    for (int c = t; c < cg; c += team) {
+      const float d = lds[g * cg + c] - mean[g];
+      s += lds[f + g * cg + c] + d * d * (float)rows;
     }
-    part[(int64_t)blockIdx.x * a.groups + g] = make_float2(mu, m2 + d2 * (float)rows);
-  }
+    return s;
+  }, [&](int g, float s) { part[(int64_t)blockIdx.x * a.groups + g] = make_float2(mean[g], s); });
 }
 
-// Joins a sample's chunks, normalises `per` of its rows.
+// Joins a sample's chunks, normalises `out_per` of its rows.
 template <class T>
-__global__ __launch_bounds__(kThreads) void normalise_kernel(pgcn_group_norm_fwd_args a, Cut cut, int64_t per, int blocks,
-                                                             int sh, const float2 *part) {
+__global__ __launch_bounds__(kThreads) void normalise_kernel(pgcn_group_norm_fwd_args a, Cut cut, const float2 *part) {
   extern __shared__ float lds[];                        // mean, 1 / deviation: [2][groups]
-  const int f = a.channels, cg = f / a.groups, vecs = (f + T::E - 1) / T::E, lx = 1 << sh, ty = kThreads >> sh;
-  const int tx = threadIdx.x & (lx - 1), slot = threadIdx.x >> sh;
-  const int64_t sample = blockIdx.x / blocks;
-  const int block = (int)(blockIdx.x - sample * blocks);
-  for (int g = threadIdx.x; g < a.groups; g += kThreads) {
-    Moments m;
-    for (int c = 0; c < cut.chunks; ++c) {
-      const float2 p = part[(sample * cut.chunks + c) * a.groups + g];
-      m = join(m, Moments{(float)chunk_rows(a.sample_rows, cut.per, c) * (float)cg, p.x, p.y});
-    }
+  __shared__ float red_[3 * kThreads];
+  const int f = a.channels, cg = f / a.groups, tx = threadIdx.x % cut.lx, slot = threadIdx.x / cut.lx;
+  const int64_t sample = blockIdx.x / cut.out_blocks;
+  const int block = (int)(blockIdx.x - sample * cut.out_blocks);
+  join_chunks(part + sample * cut.chunks * a.groups, cut.chunks, a.groups, a.sample_rows, cut.per, cg, (Moments *)red_,
+              [&](int g, const Moments &m) {
     const float r = 1.0f / sqrtf(m.m2 / m.n + a.eps);
     lds[g] = m.mu;
     lds[a.groups + g] = r;
@@ -233,10 +329,11 @@ __global__ __launch_bounds__(kThreads) void normalise_kernel(pgcn_group_norm_fwd
       if (a.mean) a.mean[sample * a.groups + g] = m.mu;
       if (a.rstd) a.rstd[sample * a.groups + g] = r;
     }
-  }
+  });
   __syncthreads();
-  const int64_t rows = chunk_rows(a.sample_rows, per, block), row0 = sample * a.sample_rows + (int64_t)block * per;
-  for (int vec = tx; vec < vecs; vec += lx) {
+  if (slot >= cut.ty) return;
+  const int64_t rows = chunk_rows(a.sample_rows, cut.out_per, block), row0 = sample * a.sample_rows + (int64_t)block * cut.out_per;
+  for (int vec = tx; vec < cut.vecs; vec += cut.lx) {
     float mu[T::E], rs[T::E], ga[T::E], be[T::E];
 #pragma unroll
     for (int e = 0; e < T::E; ++e) {
@@ -246,103 +343,144 @@ __global__ __launch_bounds__(kThreads) void normalise_kernel(pgcn_group_norm_fwd
       ga[e] = a.gamma ? a.gamma[c] : 1.f;
       be[e] = a.beta ? a.beta[c] : 0.f;
     }
-    for (int64_t r = slot; r < rows; r += ty) {
-      float x[T::E];
-      T::unpack(*reinterpret_cast<const typename T::raw *>((const typename T::type *)a.X + (row0 + r) * a.ld_x + vec * T::E), x);
+    for (int64_t r = slot; r < rows; r += kBatch * cut.ty) {
+      typename T::raw raw[kBatch];
 #pragma unroll
-      for (int e = 0; e < T::E; ++e) x[e] = affine(normed(x[e], mu[e], rs[e]), ga[e], be[e]);
-      activate(x, a.act);
-      store_some<T>((typename T::type *)a.Y + (row0 + r) * a.ld_y + vec * T::E, x, f - vec * T::E);
+      for (int b = 0; b < kBatch; ++b)
+        if (r + b * cut.ty < rows)
+          raw[b] = *reinterpret_cast<const typename T::raw *>((const typename T::type *)a.X + (row0 + r + b * cut.ty) * a.ld_x + vec * T::E);
+#pragma unroll
+      for (int b = 0; b < kBatch; ++b) {
+        if (r + b * cut.ty >= rows) break;
+        float x[T::E];
+        T::unpack(raw[b], x);
+#pragma unroll
+        for (int e = 0; e < T::E; ++e) x[e] = affine(normed(x[e], mu[e], rs[e]), ga[e], be[e]);
+        activate(x, a.act);
+        store_some<T>((typename T::type *)a.Y + (row0 + r + b * cut.ty) * a.ld_y + vec * T::E, x, f - vec * T::E);
+      }
     }
   }
 }
 
-// Sums of du and du xhat for every channel over one chunk of one sample: part[block][2][channels].
+// xhat -> x, du -> j of one vector.
 template <class T>
-__global__ __launch_bounds__(kThreads) void grad_sums_kernel(pgcn_group_norm_bwd_args a, Cut cut, int sh, float *part) {
-  __shared__ float red[2][kThreads * 8];
-  const int f = a.channels, cg = f / a.groups, vecs = (f + T::E - 1) / T::E, lx = 1 << sh, ty = kThreads >> sh;
-  const int tx = threadIdx.x & (lx - 1), slot = threadIdx.x >> sh;
-  const int64_t sample = blockIdx.x / cut.chunks;
-  const int chunk = (int)(blockIdx.x - sample * cut.chunks);
-  const int64_t rows = chunk_rows(a.sample_rows, cut.per, chunk), row0 = sample * a.sample_rows + (int64_t)chunk * cut.per;
-  for (int v0 = 0; v0 < vecs; v0 += lx) {
-    const int vec = v0 + tx;
-    float s1[T::E] = {}, s2[T::E] = {};
-    if (vec < vecs) {
-      float mu[T::E], rs[T::E], ga[T::E], be[T::E];
+__device__ __forceinline__ void grad_vector(const typename T::raw &xr, const typename T::raw &jr, const float (&mu)[T::E],
+                                            const float (&rs)[T::E], const float (&ga)[T::E], const float (&be)[T::E], int act,
+                                            float (&x)[T::E], float (&j)[T::E]) {
+  float u[T::E];
+  T::unpack(xr, x);
+  T::unpack(jr, j);
 #pragma unroll
-      for (int e = 0; e < T::E; ++e) {
-        const int c = vec * T::E + e < f ? vec * T::E + e : f - 1;
-        mu[e] = a.mean[sample * a.groups + c / cg];
-        rs[e] = a.rstd[sample * a.groups + c / cg];
-        ga[e] = a.gamma ? a.gamma[c] : 1.f;
-        be[e] = a.beta ? a.beta[c] : 0.f;
-      }
-      for (int64_t r = slot; r < rows; r += ty) {
-        float x[T::E], j[T::E];
-        T::unpack(*reinterpret_cast<const typename T::raw *>((const typename T::type *)a.X + (row0 + r) * a.ld_x + vec * T::E), x);
-        T::unpack(*reinterpret_cast<const typename T::raw *>((const typename T::type *)a.J_out + (row0 + r) * a.ld_j_out + vec * T::E), j);
-        float u[T::E];
+  for (int e = 0; e < T::E; ++e) {
+    x[e] = normed(x[e], mu[e], rs[e]);
+    u[e] = affine(x[e], ga[e], be[e]);
+  }
+  times_slope(j, u, act);
+}
+
+// Sums over one chunk of one sample: of gamma du and gamma du xhat for every group,
+// part[sample][chunk][groups].  A workgroup walks chunks and adds up du and du xhat for every
+// channel over all of its own, channel_part[block][2][channels] (null: not wanted), so that many
+// short samples leave few of them.
+template <class T>
+__global__ __launch_bounds__(kThreads) void grad_sums_kernel(pgcn_group_norm_bwd_args a, Cut cut, float2 *part, float *channel_part) {
+  extern __shared__ float lds[];                        // [2][channels]
+  __shared__ float red[2][T::E][kThreads];
+  const int f = a.channels, cg = f / a.groups, tx = threadIdx.x % cut.lx, slot = threadIdx.x / cut.lx;
+  for (int64_t unit = blockIdx.x; unit < a.samples * cut.chunks; unit += gridDim.x) {
+    const int64_t sample = unit / cut.chunks;
+    const int chunk = (int)(unit - sample * cut.chunks);
+    const int64_t rows = chunk_rows(a.sample_rows, cut.per, chunk), row0 = sample * a.sample_rows + (int64_t)chunk * cut.per;
+    for (int v0 = 0; v0 < cut.vecs; v0 += cut.lx) {
+      const int vec = v0 + tx;
+      float s1[T::E] = {}, s2[T::E] = {};
+      if (vec < cut.vecs && slot < cut.ty) {
+        float mu[T::E], rs[T::E], ga[T::E], be[T::E];
 #pragma unroll
         for (int e = 0; e < T::E; ++e) {
-          x[e] = normed(x[e], mu[e], rs[e]);
-          u[e] = affine(x[e], ga[e], be[e]);
+          const int c = vec * T::E + e < f ? vec * T::E + e : f - 1;
+          mu[e] = a.mean[sample * a.groups + c / cg];
+          rs[e] = a.rstd[sample * a.groups + c / cg];
+          ga[e] = a.gamma ? a.gamma[c] : 1.f;
+          be[e] = a.beta ? a.beta[c] : 0.f;
         }
-        times_slope(j, u, a.act);
+        for (int64_t r = slot; r < rows; r += kBatch * cut.ty) {
+          typename T::raw xr[kBatch], jr[kBatch];
+#pragma unroll
+          for (int b = 0; b < kBatch; ++b)
+            if (r + b * cut.ty < rows) {
+              xr[b] = *reinterpret_cast<const typename T::raw *>((const typename T::type *)a.X + (row0 + r + b * cut.ty) * a.ld_x + vec * T::E);
+              jr[b] = *reinterpret_cast<const typename T::raw *>((const typename T::type *)a.J_out + (row0 + r + b * cut.ty) * a.ld_j_out + vec * T::E);
+            }
+#pragma unroll
+          for (int b = 0; b < kBatch; ++b) {
+            if (r + b * cut.ty >= rows) break;
+            float x[T::E], j[T::E];
+            grad_vector<T>(xr[b], jr[b], mu, rs, ga, be, a.act, x, j);
+#pragma unroll
+            for (int e = 0; e < T::E; ++e) {
+              s1[e] += j[e];
+              s2[e] += j[e] * x[e];
+            }
+          }
+        }
+      }
+      for (int left = cut.ty; left > 1; left = (left + 1) / 2) {
+        const int half = (left + 1) / 2;
 #pragma unroll
         for (int e = 0; e < T::E; ++e) {
-          s1[e] += j[e];
-          s2[e] += j[e] * x[e];
+          red[0][e][threadIdx.x] = s1[e];
+          red[1][e][threadIdx.x] = s2[e];
+        }
+        __syncthreads();
+        if (slot + half < left) {
+#pragma unroll
+          for (int e = 0; e < T::E; ++e) {
+            s1[e] += red[0][e][threadIdx.x + half * cut.lx];
+            s2[e] += red[1][e][threadIdx.x + half * cut.lx];
+          }
+        }
+        __syncthreads();
+      }
+      if (slot == 0 && vec < cut.vecs) {
+        float *p = channel_part ? channel_part + (int64_t)blockIdx.x * 2 * f : nullptr;
+#pragma unroll
+        for (int e = 0; e < T::E; ++e) {
+          const int c = vec * T::E + e;
+          if (c >= f) break;
+          const float ga = a.gamma ? a.gamma[c] : 1.f;
+          lds[c] = ga * s1[e];
+          lds[f + c] = ga * s2[e];
+          if (p) {
+            const bool first = unit == blockIdx.x;
+            p[c] = first ? s1[e] : p[c] + s1[e];
+            p[f + c] = first ? s2[e] : p[f + c] + s2[e];
+          }
         }
       }
     }
-    for (int half = ty / 2; half > 0; half >>= 1) {
-#pragma unroll
-      for (int e = 0; e < T::E; ++e) {
-        red[0][threadIdx.x * T::E + e] = s1[e];
-        red[1][threadIdx.x * T::E + e] = s2[e];
-      }
-      __syncthreads();
-      if (slot < half) {
-#pragma unroll
-        for (int e = 0; e < T::E; ++e) {
-          s1[e] += red[0][(threadIdx.x + half * lx) * T::E + e];
-          s2[e] += red[1][(threadIdx.x + half * lx) * T::E + e];
-        }
-      }
-      __syncthreads();
-    }
-    if (slot == 0 && vec < vecs) {
-      float *p = part + (int64_t)blockIdx.x * 2 * f + vec * T::E;
-#pragma unroll
-      for (int e = 0; e < T::E; ++e)
-        if (vec * T::E + e < f) {
-          p[e] = s1[e];
-          p[f + e] = s2[e];
-        }
-    }
+    __syncthreads();
+    for (int h = 0; h < 2; ++h)
+      for_groups(a.groups, [&](int g, int t, int team) {
+        float s = 0.f;
+        for (int c = t; c < cg; c += team) s += lds[h * f + g * cg + c];
+        return s;
+      }, [&](int g, float s) { (&part[unit * a.groups + g].x)[h] = s; });
+    __syncthreads();
   }
 }
 
-// sums[sample][i] = sum over the sample's chunks of part[sample][chunk][i], i < width.
-__global__ __launch_bounds__(kThreads) void add_chunks_kernel(const float *part, int chunks, int64_t entries, int width, float *sums) {
-  const int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-  if (i >= entries) return;
-  const int64_t b = i / width;
-  const float *p = part + b * chunks * width + (i - b * width);
-  float s = 0.f;
-  for (int c = 0; c < chunks; ++c) s += p[(int64_t)c * width];
-  sums[i] = s;
-}
-
-// Sums over the samples: dbeta from the first half of sums[sample][2][channels], dgamma from the second.
-__global__ __launch_bounds__(kThreads) void param_grads_kernel(const float *sums, int64_t samples, int f, float *dgamma, float *dbeta) {
+// Sums over n of part[n][2][channels], 32 of the 2 channels values to a workgroup: the first half
+// is dbeta, the second dgamma.
+__device__ void param_grads(const float *part, int64_t n, int f, int block, float *dgamma, float *dbeta) {
   __shared__ double red[kThreads];
-  const int i = blockIdx.x * 32 + (threadIdx.x & 31), slot = threadIdx.x >> 5;
+  const int i = block * 32 + (threadIdx.x & 31), slot = threadIdx.x >> 5;
   double s = 0.0;                                       // thousands of terms in one chain
-  if (i < 2 * f)
-    for (int64_t b = slot; b < samples; b += kThreads / 32) s += (double)sums[b * 2 * f + i];
+  if (i < 2 * f) {
+#pragma unroll 8
+    for (int64_t b = slot; b < n; b += kThreads / 32) s += (double)part[b * 2 * f + i];
+  }
   red[threadIdx.x] = s;
   __syncthreads();
   if (slot == 0 && i < 2 * f) {
@@ -355,30 +493,33 @@ __global__ __launch_bounds__(kThreads) void param_grads_kernel(const float *sums
   }
 }
 
-// dX of `per` rows of a sample, from the sample's channel sums.
+__global__ __launch_bounds__(kThreads) void param_grads_kernel(const float *part, int64_t n, int f, float *dgamma, float *dbeta) {
+  param_grads(part, n, f, blockIdx.x, dgamma, dbeta);
+}
+
+// dX of `out_per` rows of a sample, from its chunks' group sums; the last `param_blocks`
+// workgroups add up the channel sums instead.
 template <class T>
-__global__ __launch_bounds__(kThreads) void grad_rows_kernel(pgcn_group_norm_bwd_args a, int64_t per, int blocks, int sh,
-                                                             const float *sums) {
+__global__ __launch_bounds__(kThreads) void grad_rows_kernel(pgcn_group_norm_bwd_args a, Cut cut, const float2 *part,
+                                                             const float *channel_part, int sum_blocks, int row_blocks) {
   extern __shared__ float lds[];                        // c1, c2: [2][groups]
-  const int f = a.channels, cg = f / a.groups, vecs = (f + T::E - 1) / T::E, lx = 1 << sh, ty = kThreads >> sh;
-  const int tx = threadIdx.x & (lx - 1), slot = threadIdx.x >> sh;
-  const int64_t sample = blockIdx.x / blocks;
-  const int block = (int)(blockIdx.x - sample * blocks);
-  const float inv_n = 1.0f / ((float)a.sample_rows * (float)cg);
-  for (int g = threadIdx.x; g < a.groups; g += kThreads) {
-    const float *p = sums + sample * 2 * f + g * cg;
-    float c1 = 0.f, c2 = 0.f;
-    for (int c = 0; c < cg; ++c) {
-      const float ga = a.gamma ? a.gamma[g * cg + c] : 1.f;
-      c1 += ga * p[c];
-      c2 += ga * p[f + c];
-    }
-    lds[g] = c1 * inv_n;
-    lds[a.groups + g] = c2 * inv_n;
+  __shared__ float2 red[kThreads];
+  if ((int)blockIdx.x >= row_blocks) {
+    param_grads(channel_part, sum_blocks, a.channels, blockIdx.x - row_blocks, a.dgamma, a.dbeta);
+    return;
   }
+  const int f = a.channels, cg = f / a.groups, tx = threadIdx.x % cut.lx, slot = threadIdx.x / cut.lx;
+  const int64_t sample = blockIdx.x / cut.out_blocks;
+  const int block = (int)(blockIdx.x - sample * cut.out_blocks);
+  const float inv_n = 1.0f / ((float)a.sample_rows * (float)cg);
+  add_chunks(part + sample * cut.chunks * a.groups, cut.chunks, a.groups, red, [&](int g, const float2 &s) {
+    lds[g] = s.x * inv_n;
+    lds[a.groups + g] = s.y * inv_n;
+  });
   __syncthreads();
-  const int64_t rows = chunk_rows(a.sample_rows, per, block), row0 = sample * a.sample_rows + (int64_t)block * per;
-  for (int vec = tx; vec < vecs; vec += lx) {
+  if (slot >= cut.ty) return;
+  const int64_t rows = chunk_rows(a.sample_rows, cut.out_per, block), row0 = sample * a.sample_rows + (int64_t)block * cut.out_per;
+  for (int vec = tx; vec < cut.vecs; vec += cut.lx) {
     float mu[T::E], rs[T::E], ga[T::E], be[T::E], c1[T::E], c2[T::E];
 #pragma unroll
     for (int e = 0; e < T::E; ++e) {
@@ -390,20 +531,23 @@ __global__ __launch_bounds__(kThreads) void grad_rows_kernel(pgcn_group_norm_bwd
       c1[e] = lds[c / cg];
       c2[e] = lds[a.groups + c / cg];
     }
-    for (int64_t r = slot; r < rows; r += ty) {
-      float x[T::E], j[T::E];
-      T::unpack(*reinterpret_cast<const typename T::raw *>((const typename T::type *)a.X + (row0 + r) * a.ld_x + vec * T::E), x);
-      T::unpack(*reinterpret_cast<const typename T::raw *>((const typename T::type *)a.J_out + (row0 + r) * a.ld_j_out + vec * T::E), j);
-      float u[T::E];
+    for (int64_t r = slot; r < rows; r += kBatch * cut.ty) {
+      typename T::raw xr[kBatch], jr[kBatch];
 #pragma unroll
-      for (int e = 0; e < T::E; ++e) {
-        x[e] = normed(x[e], mu[e], rs[e]);
-        u[e] = affine(x[e], ga[e], be[e]);
+      for (int b = 0; b < kBatch; ++b)
+        if (r + b * cut.ty < rows) {
+          xr[b] = *reinterpret_cast<const typename T::raw *>((const typename T::type *)a.X + (row0 + r + b * cut.ty) * a.ld_x + vec * T::E);
+          jr[b] = *reinterpret_cast<const typename T::raw *>((const typename T::type *)a.J_out + (row0 + r + b * cut.ty) * a.ld_j_out + vec * T::E);
+        }
+#pragma unroll
+      for (int b = 0; b < kBatch; ++b) {
+        if (r + b * cut.ty >= rows) break;
+        float x[T::E], j[T::E];
+        grad_vector<T>(xr[b], jr[b], mu, rs, ga, be, a.act, x, j);
+#pragma unroll
+        for (int e = 0; e < T::E; ++e) x[e] = rs[e] * (ga[e] * j[e] - c1[e] - x[e] * c2[e]);
+        store_some<T>((typename T::type *)a.J_in + (row0 + r + b * cut.ty) * a.ld_j_in + vec * T::E, x, f - vec * T::E);
       }
-      times_slope(j, u, a.act);
-#pragma unroll
-      for (int e = 0; e < T::E; ++e) x[e] = rs[e] * (ga[e] * j[e] - c1[e] - x[e] * c2[e]);
-      store_some<T>((typename T::type *)a.J_in + (row0 + r) * a.ld_j_in + vec * T::E, x, f - vec * T::E);
     }
   }
 }
@@ -665,23 +809,6 @@ __global__ __launch_bounds__(kThreads) void rows_bwd_kernel(pgcn_group_norm_bwd_
   }
 }
 
-struct Shape {
-  int vecs, sh;
-  Cut stat, apply;
-};
-
-Shape shape_of(int32_t dtype, int32_t channels, int64_t samples, int64_t sample_rows) {
-  const int e = dtype == PGCN_BF16 ? BF16::E : F32::E;
-  Shape s;
-  s.vecs = (channels + e - 1) / e;
-  s.sh = column_shift(s.vecs);
-  const int64_t ty = kThreads >> s.sh;
-  s.stat = cut_rows(samples, sample_rows, 8 * ty);
-  s.apply.per = 8 * ty;
-  s.apply.chunks = (int)((sample_rows + s.apply.per - 1) / s.apply.per);
-  return s;
-}
-
 // part[n][2][channels] summed over n.
 int launch_param_grads(const float *part, int64_t n, int channels, float *dgamma, float *dbeta, hipStream_t s) {
   hipLaunchKernelGGL(param_grads_kernel, dim3((unsigned)((2 * channels + 31) / 32)), dim3(kThreads), 0, s, part, n, channels, dgamma,
@@ -782,45 +909,45 @@ int rows_bwd(const pgcn_group_norm_bwd_args &a, hipStream_t s) {
   PGCN_ROW_SHAPES(rows_bwd_go, T, a, s)
 }
 
+// ---- launches: samples of many rows ----------------------------------------
+
 template <class T>
-int fwd_chunks(const pgcn_group_norm_fwd_args &a, hipStream_t s) {
-  const Shape sp = shape_of(a.dtype, a.channels, a.samples, a.sample_rows);
+int chunks_fwd(const pgcn_group_norm_fwd_args &a, hipStream_t s) {
+  const Cut cut = cut_rows(a.dtype, a.channels, a.samples, a.sample_rows);
   float2 *part = (float2 *)a.workspace;
-  hipLaunchKernelGGL(moments_kernel<T>, dim3((unsigned)(a.samples * sp.stat.chunks)), dim3(kThreads), 8 * (size_t)a.channels, s,
-                     a, sp.stat, sp.sh, part);
+  hipLaunchKernelGGL(moments_kernel<T>, dim3((unsigned)(a.samples * cut.chunks)), dim3(kThreads),
+                     4 * (2 * (size_t)a.channels + (size_t)a.groups), s, a, cut, part);
   PGCN_HIP(hipGetLastError());
-  hipLaunchKernelGGL(normalise_kernel<T>, dim3((unsigned)(a.samples * sp.apply.chunks)), dim3(kThreads), 8 * (size_t)a.groups,
-                     s, a, sp.stat, sp.apply.per, sp.apply.chunks, sp.sh, part);
+  hipLaunchKernelGGL(normalise_kernel<T>, dim3((unsigned)(a.samples * cut.out_blocks)), dim3(kThreads), 8 * (size_t)a.groups, s, a, cut,
+                     part);
   PGCN_HIP(hipGetLastError());
   return PGCN_OK;
 }
 
+// Bytes of the chunks' group sums, before their channel sums.
+size_t group_part_bytes(const Cut &cut, int32_t groups, int64_t samples) {
+  return align_up(8 * (size_t)samples * (size_t)cut.chunks * (size_t)groups, 16);
+}
+
+int chunk_sum_blocks(const Cut &cut, int64_t samples) { return (int)std::min<int64_t>(samples * cut.chunks, kChunkBlocks); }
+
 template <class T>
-int bwd_chunks(const pgcn_group_norm_bwd_args &a, hipStream_t s) {
-  const Shape sp = shape_of(a.dtype, a.channels, a.samples, a.sample_rows);
-  const int w = 2 * a.channels;
-  float *part = (float *)a.workspace, *sums = part;
-  if (a.samples > 0) {
-    hipLaunchKernelGGL(grad_sums_kernel<T>, dim3((unsigned)(a.samples * sp.stat.chunks)), dim3(kThreads), 0, s, a, sp.stat,
-                       sp.sh, part);
-    PGCN_HIP(hipGetLastError());
-    if (sp.stat.chunks > 1) {
-      sums = part + a.samples * sp.stat.chunks * w;
-      const int64_t entries = a.samples * w;
-      hipLaunchKernelGGL(add_chunks_kernel, dim3((unsigned)((entries + kThreads - 1) / kThreads)), dim3(kThreads), 0, s, part,
-                         sp.stat.chunks, entries, w, sums);
-      PGCN_HIP(hipGetLastError());
-    }
-  }
-  if (a.dgamma || a.dbeta) {
-    const int rc = launch_param_grads(sums, a.samples, a.channels, a.dgamma, a.dbeta, s);
-    if (rc) return rc;
-  }
-  if (a.J_in && a.samples > 0) {
-    hipLaunchKernelGGL(grad_rows_kernel<T>, dim3((unsigned)(a.samples * sp.apply.chunks)), dim3(kThreads),
-                       8 * (size_t)a.groups, s, a, sp.apply.per, sp.apply.chunks, sp.sh, sums);
-    PGCN_HIP(hipGetLastError());
-  }
+int chunks_bwd(const pgcn_group_norm_bwd_args &a, hipStream_t s) {
+  const Cut cut = cut_rows(a.dtype, a.channels, a.samples, a.sample_rows);
+  const bool params = a.dgamma || a.dbeta;
+  if (a.samples == 0) return params ? launch_param_grads(nullptr, 0, a.channels, a.dgamma, a.dbeta, s) : PGCN_OK;
+  if (!params && !a.J_in) return PGCN_OK;
+  float2 *part = (float2 *)a.workspace;
+  float *channel_part = params ? (float *)((char *)a.workspace + group_part_bytes(cut, a.groups, a.samples)) : nullptr;
+  const int sum_blocks = chunk_sum_blocks(cut, a.samples);
+  hipLaunchKernelGGL(grad_sums_kernel<T>, dim3((unsigned)sum_blocks), dim3(kThreads), 8 * (size_t)a.channels, s, a, cut,
+                     part, channel_part);
+  PGCN_HIP(hipGetLastError());
+  const unsigned row_blocks = a.J_in ? (unsigned)(a.samples * cut.out_blocks) : 0;
+  const unsigned param_blocks = params ? (unsigned)((2 * a.channels + 31) / 32) : 0;
+  hipLaunchKernelGGL(grad_rows_kernel<T>, dim3(row_blocks + param_blocks), dim3(kThreads), 8 * (size_t)a.groups, s, a, cut, part,
+                     channel_part, sum_blocks, (int)row_blocks);
+  PGCN_HIP(hipGetLastError());
   return PGCN_OK;
 }
 
@@ -834,23 +961,21 @@ size_t group_norm_workspace(int32_t dtype, int32_t channels, int32_t groups, int
     row_threads((channels + e - 1) / e, lanes, per);
     return 8 * (size_t)channels * row_blocks(samples, lanes, kRowBlocksBwd);
   }
-  const Shape sp = shape_of(dtype, channels, samples, sample_rows);
-  const size_t f = 8 * (size_t)samples * (size_t)sp.stat.chunks * (size_t)groups;
-  const size_t b = 8 * (size_t)channels * (size_t)samples * (size_t)(sp.stat.chunks + 1);
-  return std::max(f, b);
+  const Cut cut = cut_rows(dtype, channels, samples, sample_rows);
+  return group_part_bytes(cut, groups, samples) + 8 * (size_t)channels * (size_t)chunk_sum_blocks(cut, samples);
 }
 
 int launch_group_norm_fwd(const pgcn_group_norm_fwd_args &a, hipStream_t s) {
   if (a.samples == 0) return PGCN_OK;
   TraceScope ts(PGCN_TK_GROUP_NORM, s);
   if (a.sample_rows == 1) return a.dtype == PGCN_BF16 ? rows_fwd<BF16>(a, s) : rows_fwd<F32>(a, s);
-  return a.dtype == PGCN_BF16 ? fwd_chunks<BF16>(a, s) : fwd_chunks<F32>(a, s);
+  return a.dtype == PGCN_BF16 ? chunks_fwd<BF16>(a, s) : chunks_fwd<F32>(a, s);
 }
 
 int launch_group_norm_bwd(const pgcn_group_norm_bwd_args &a, hipStream_t s) {
   TraceScope ts(PGCN_TK_GROUP_NORM_BWD, s);
   if (a.sample_rows == 1 && a.samples > 0) return a.dtype == PGCN_BF16 ? rows_bwd<BF16>(a, s) : rows_bwd<F32>(a, s);
-  return a.dtype == PGCN_BF16 ? bwd_chunks<BF16>(a, s) : bwd_chunks<F32>(a, s);
+  return a.dtype == PGCN_BF16 ? chunks_bwd<BF16>(a, s) : chunks_bwd<F32>(a, s);
 }
 
 }  // namespace pgcn

@@ -156,7 +156,8 @@ def check_backward(x, f, G, samples, R, kind, dtype, eps=1e-5, affine=True, seed
 SHAPES = [(1, 1, 1, 1), (1, 1, 32, 4), (37, 1, 8, 2), (1000, 1, 256, 1), (513, 1, 256, 8), (70, 1, 602, 1), (33, 1, 602, 14), (65, 1, 41, 1),
           (50, 1, 300, 4), (9, 1, 300, 100), (21, 1, 512, 512), (5, 1, 2048, 1), (7, 1, 2052, 3), (3, 1, 8192, 32), (2, 1, 8191, 1),
           (2, 7, 16, 4), (3, 64, 320, 32), (5, 33, 60, 5), (1, 5000, 256, 8), (2, 1025, 7, 1), (40, 3, 130, 13), (1, 3001, 1, 1),
-          (4, 256, 1000, 8), (600, 2, 24, 3), (2, 500, 2100, 7), (1, 40, 8192, 2), (17, 100, 4, 2)]
+          (4, 256, 1000, 8), (600, 2, 24, 3), (2, 500, 2100, 7), (1, 40, 8192, 2), (17, 100, 4, 2), (2, 9, 8192, 8192),
+          (1500, 5, 16, 2), (1, 3000, 257, 257), (1, 2000, 24, 3)]
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
