@@ -101,6 +101,10 @@ __device__ __forceinline__ Moments join(const Moments &a, const Moments &b) {
   return r;
 }
 
+// The group of a channel, c / cg: c < 2^13 makes the high word of c ceil(2^32 / cg) exact.
+uint32_t group_magic(int cg) { return cg > 1 ? (uint32_t)(((uint64_t(1) << 32) + cg - 1) / cg) : 0; }
+__device__ __forceinline__ int group_of(uint32_t magic, int c) { return magic ? (int)__umulhi((uint32_t)c, magic) : c; }
+
 // ---------------------------------------------- samples of many rows -------
 //
 // Two launches: the first leaves each chunk's group statistics, the second joins a sample's
@@ -115,24 +119,32 @@ struct Cut {
   int chunks;
   int64_t out_per;       // rows of a workgroup of the second launch
   int out_blocks;
+  uint32_t magic;        // of groups, see group_of
 };
 
 constexpr int kBatch = 4;              // rows that a thread loads together
-constexpr int kChunkBlocks = 1024;     // workgroups of a launch, about: 4 for each compute unit
+// Workgroups of the two launches, about.  More chunks are more statistics for every workgroup of
+// the second one to join.  us of both launches, 1 x 58,000 x 256 fp32 forward and 8 x 4,096 x 320
+// bf16 backward: 512 and 512 39.3, 37.4; 512 and 1,024 37.3, 37.5; 1,024 and 1,024 39.3, 42.6.
+constexpr int kStatBlocks = 512, kOutBlocks = 1024;
 
-Cut cut_rows(int32_t dtype, int32_t channels, int64_t samples, int64_t sample_rows) {
+Cut cut_rows(int32_t dtype, int32_t channels, int32_t groups, int64_t samples, int64_t sample_rows) {
   const int e = dtype == PGCN_BF16 ? BF16::E : F32::E;
   Cut c;
   c.vecs = (channels + e - 1) / e;
+  c.magic = group_magic(channels / groups);
   const int tiles = (c.vecs + kThreads - 1) / kThreads;
   c.lx = (c.vecs + tiles - 1) / tiles;
   c.ty = kThreads / c.lx;
-  const int64_t least = (int64_t)kBatch * c.ty, most = std::max<int64_t>(1, kChunkBlocks / std::max<int64_t>(1, samples));
-  const int64_t parts = std::min(most, (sample_rows + least - 1) / least);
-  c.per = (sample_rows + parts - 1) / parts;
+  const int64_t least = (int64_t)kBatch * c.ty, n = std::max<int64_t>(1, samples);
+  auto cut = [&](int blocks) {           // rows of a part, whole batches
+    const int64_t parts = std::min(std::max<int64_t>(1, blocks / n), (sample_rows + least - 1) / least);
+    return ((sample_rows + parts - 1) / parts + least - 1) / least * least;
+  };
+  c.per = cut(kStatBlocks);
   c.chunks = (int)((sample_rows + c.per - 1) / c.per);
-  c.out_per = c.per;
-  c.out_blocks = c.chunks;
+  c.out_per = cut(kOutBlocks);
+  c.out_blocks = (int)((sample_rows + c.out_per - 1) / c.out_per);
   return c;
 }
 
@@ -156,48 +168,29 @@ __device__ __forceinline__ void for_groups(int groups, Value value, Done done) {
   }
 }
 
-// Joins the chunks' (mean, M2) or adds up their sums, one result for each of the groups:
-// done(g, joined).  Threads side by side take neighbouring groups, the others every ty-th chunk.
-template <class Done>
-__device__ __forceinline__ void join_chunks(const float2 *part, int chunks, int groups, int64_t sample_rows, int64_t per, int cg,
-                                            Moments *red, Done done) {
-  const int wide = groups < kThreads ? groups : kThreads, deep = kThreads / wide;
-  const int tx = threadIdx.x % wide, slot = threadIdx.x / wide;
-  for (int g0 = 0; g0 < groups; g0 += wide) {
-    const int g = g0 + tx;
-    Moments m;
-    if (g < groups && slot < deep)
-      for (int c = slot; c < chunks; c += deep) {
-        const float2 p = part[(int64_t)c * groups + g];
-        m = join(m, Moments{(float)chunk_rows(sample_rows, per, c) * (float)cg, p.x, p.y});
-      }
-    __syncthreads();
-    red[threadIdx.x].n = m.n;
-    red[threadIdx.x].mu = m.mu;
-    red[threadIdx.x].m2 = m.m2;
-    __syncthreads();
-    for (int n = deep; n > 1; n = (n + 1) / 2) {
-      const int half = (n + 1) / 2;
-      if (slot + half < n) red[threadIdx.x] = join(red[threadIdx.x], red[threadIdx.x + half * wide]);
-      __syncthreads();
-    }
-    if (slot == 0 && g < groups) done(g, red[threadIdx.x]);
-  }
-}
+// A group's chunks joined: `total(g, x, y)` gets the sums over the chunks of value(n, part).x and
+// .y in fp64, n the elements of the chunk.  Threads side by side take neighbouring groups, the
+// others every deep-th chunk.
+struct Sum2 {
+  double x, y;
+};
 
-template <class Done>
-__device__ __forceinline__ void add_chunks(const float2 *part, int chunks, int groups, float2 *red, Done done) {
+template <class Value, class Total>
+__device__ __forceinline__ void join_chunks(const float2 *part, int chunks, int groups, int64_t sample_rows, int64_t per, int cg,
+                                            Sum2 *red, Value value, Total total) {
   const int wide = groups < kThreads ? groups : kThreads, deep = kThreads / wide;
   const int tx = threadIdx.x % wide, slot = threadIdx.x / wide;
   for (int g0 = 0; g0 < groups; g0 += wide) {
     const int g = g0 + tx;
-    float2 m = make_float2(0.f, 0.f);
-    if (g < groups && slot < deep)
+    Sum2 m = {0.0, 0.0};
+    if (g < groups && slot < deep) {
+#pragma unroll 8
       for (int c = slot; c < chunks; c += deep) {
-        const float2 p = part[(int64_t)c * groups + g];
-        m.x += p.x;
-        m.y += p.y;
+        const Sum2 v = value((double)chunk_rows(sample_rows, per, c) * (double)cg, part[(int64_t)c * groups + g]);
+        m.x += v.x;
+        m.y += v.y;
       }
+    }
     __syncthreads();
     red[threadIdx.x] = m;
     __syncthreads();
@@ -209,7 +202,7 @@ __device__ __forceinline__ void add_chunks(const float2 *part, int chunks, int g
       }
       __syncthreads();
     }
-    if (slot == 0 && g < groups) done(g, red[threadIdx.x]);
+    if (slot == 0 && g < groups) total(g, red[threadIdx.x]);
   }
 }
 
@@ -230,36 +223,48 @@ __global__ __launch_bounds__(kThreads) void moments_kernel(pgcn_group_norm_fwd_a
     float mu[T::E] = {}, m2[T::E] = {};
     int n = 0;
     if (vec < cut.vecs && slot < cut.ty) {
-      for (int64_t r = slot; r < rows; r += kBatch * cut.ty) {
+      const typename T::type *p = x0 + slot * a.ld_x + vec * T::E;
+      const int64_t step = cut.ty * a.ld_x;
+      int64_t r = slot;
+      for (; r + (kBatch - 1) * cut.ty < rows; r += kBatch * cut.ty, p += kBatch * step) {
         // a batch's own moments first, then one join: fewer steps in the chain
         typename T::raw raw[kBatch];
-        int k = 0;
 #pragma unroll
-        for (int b = 0; b < kBatch; ++b)
-          if (r + b * cut.ty < rows) {
-            raw[b] = *reinterpret_cast<const typename T::raw *>(x0 + (r + b * cut.ty) * a.ld_x + vec * T::E);
-            k = b + 1;
-          }
+        for (int b = 0; b < kBatch; ++b) raw[b] = *reinterpret_cast<const typename T::raw *>(p + b * step);
         float x[kBatch][T::E];
 #pragma unroll
-        for (int b = 0; b < kBatch; ++b) T::unpack(raw[b < k ? b : 0], x[b]);
-        const float inv_k = 1.0f / (float)k, w = (float)k / (float)(n + k), wn = (float)n * w;
+        for (int b = 0; b < kBatch; ++b) T::unpack(raw[b], x[b]);
+        const float w = (float)kBatch * __builtin_amdgcn_rcpf((float)(n + kBatch)), wn = (float)n * w;
 #pragma unroll
         for (int e = 0; e < T::E; ++e) {
-          float s = 0.f, q = 0.f;
+          const float bm = ((x[0][e] + x[1][e]) + (x[2][e] + x[3][e])) * (1.0f / kBatch), d = bm - mu[e];
+          float q = 0.f;
 #pragma unroll
-          for (int b = 0; b < kBatch; ++b) s += b < k ? x[b][e] : 0.f;
-          const float bm = s * inv_k;
-#pragma unroll
-          for (int b = 0; b < kBatch; ++b) {
-            const float d = x[b][e] - bm;
-            q += b < k ? d * d : 0.f;
-          }
-          const float d = bm - mu[e];
+          for (int b = 0; b < kBatch; ++b) q += (x[b][e] - bm) * (x[b][e] - bm);
           mu[e] += d * w;
           m2[e] += q + d * d * wn;
         }
-        n += k;
+        n += kBatch;
+      }
+      if (r < rows) {                                                // what is left, loaded together too
+        typename T::raw raw[kBatch - 1];
+#pragma unroll
+        for (int b = 0; b < kBatch - 1; ++b)
+          raw[b] = *reinterpret_cast<const typename T::raw *>(r + b * cut.ty < rows ? p + b * step : p);
+#pragma unroll
+        for (int b = 0; b < kBatch - 1; ++b) {
+          if (r + b * cut.ty >= rows) break;
+          float x[T::E];
+          T::unpack(raw[b], x);
+          const float w = __builtin_amdgcn_rcpf((float)(n + 1)), wn = (float)n * w;
+#pragma unroll
+          for (int e = 0; e < T::E; ++e) {
+            const float d = x[e] - mu[e];
+            mu[e] += d * w;
+            m2[e] += d * d * wn;
+          }
+          ++n;
+        }
       }
     }
     for (int left = cut.ty; left > 1; left = (left + 1) / 2) {      // join the row slots
@@ -316,17 +321,21 @@ __global__ __launch_bounds__(kThreads) void moments_kernel(pgcn_group_norm_fwd_a
 template <class T>
 __global__ __launch_bounds__(kThreads) void normalise_kernel(pgcn_group_norm_fwd_args a, Cut cut, const float2 *part) {
   extern __shared__ float lds[];                        // mean, 1 / deviation: [2][groups]
-  __shared__ float red_[3 * kThreads];
+  __shared__ Sum2 red[kThreads];
   const int f = a.channels, cg = f / a.groups, tx = threadIdx.x % cut.lx, slot = threadIdx.x / cut.lx;
   const int64_t sample = blockIdx.x / cut.out_blocks;
   const int block = (int)(blockIdx.x - sample * cut.out_blocks);
-  join_chunks(part + sample * cut.chunks * a.groups, cut.chunks, a.groups, a.sample_rows, cut.per, cg, (Moments *)red_,
-              [&](int g, const Moments &m) {
-    const float r = 1.0f / sqrtf(m.m2 / m.n + a.eps);
-    lds[g] = m.mu;
+  const double n = (double)a.sample_rows * (double)cg;
+  // sums of x and of squares: fp64 leaves 29 bits of the variance where the mean is 4,096 deviations away
+  join_chunks(part + sample * cut.chunks * a.groups, cut.chunks, a.groups, a.sample_rows, cut.per, cg, red,
+              [](double k, const float2 &p) { return Sum2{k * (double)p.x, (double)p.y + k * (double)p.x * (double)p.x}; },
+              [&](int g, const Sum2 &t) {
+    const double mu = t.x / n, var = (t.y - t.x * mu) / n;
+    const float r = 1.0f / sqrtf((float)(var > 0.0 || var != var ? var : 0.0) + a.eps);
+    lds[g] = (float)mu;
     lds[a.groups + g] = r;
     if (block == 0) {
-      if (a.mean) a.mean[sample * a.groups + g] = m.mu;
+      if (a.mean) a.mean[sample * a.groups + g] = (float)mu;
       if (a.rstd) a.rstd[sample * a.groups + g] = r;
     }
   });
@@ -337,28 +346,40 @@ __global__ __launch_bounds__(kThreads) void normalise_kernel(pgcn_group_norm_fwd
     float mu[T::E], rs[T::E], ga[T::E], be[T::E];
 #pragma unroll
     for (int e = 0; e < T::E; ++e) {
-      const int c = vec * T::E + e < f ? vec * T::E + e : f - 1;
-      mu[e] = lds[c / cg];
-      rs[e] = lds[a.groups + c / cg];
+      const int c = vec * T::E + e < f ? vec * T::E + e : f - 1, g = group_of(cut.magic, c);
+      mu[e] = lds[g];
+      rs[e] = lds[a.groups + g];
       ga[e] = a.gamma ? a.gamma[c] : 1.f;
       be[e] = a.beta ? a.beta[c] : 0.f;
     }
-    for (int64_t r = slot; r < rows; r += kBatch * cut.ty) {
+    const typename T::type *p = (const typename T::type *)a.X + (row0 + slot) * a.ld_x + vec * T::E;
+    typename T::type *y = (typename T::type *)a.Y + (row0 + slot) * a.ld_y + vec * T::E;
+    const int64_t step = cut.ty * a.ld_x, step_y = cut.ty * a.ld_y;
+    const int left = f - vec * T::E;
+    auto one = [&](const typename T::raw &raw, typename T::type *to) {
+      float x[T::E];
+      T::unpack(raw, x);
+#pragma unroll
+      for (int e = 0; e < T::E; ++e) x[e] = affine(normed(x[e], mu[e], rs[e]), ga[e], be[e]);
+      activate(x, a.act);
+      store_some<T>(to, x, left);
+    };
+    int64_t r = slot;
+    for (; r + (kBatch - 1) * cut.ty < rows; r += kBatch * cut.ty, p += kBatch * step, y += kBatch * step_y) {
       typename T::raw raw[kBatch];
 #pragma unroll
-      for (int b = 0; b < kBatch; ++b)
-        if (r + b * cut.ty < rows)
-          raw[b] = *reinterpret_cast<const typename T::raw *>((const typename T::type *)a.X + (row0 + r + b * cut.ty) * a.ld_x + vec * T::E);
+      for (int b = 0; b < kBatch; ++b) raw[b] = *reinterpret_cast<const typename T::raw *>(p + b * step);
 #pragma unroll
-      for (int b = 0; b < kBatch; ++b) {
-        if (r + b * cut.ty >= rows) break;
-        float x[T::E];
-        T::unpack(raw[b], x);
+      for (int b = 0; b < kBatch; ++b) one(raw[b], y + b * step_y);
+    }
+    if (r < rows) {
+      typename T::raw raw[kBatch - 1];
 #pragma unroll
-        for (int e = 0; e < T::E; ++e) x[e] = affine(normed(x[e], mu[e], rs[e]), ga[e], be[e]);
-        activate(x, a.act);
-        store_some<T>((typename T::type *)a.Y + (row0 + r + b * cut.ty) * a.ld_y + vec * T::E, x, f - vec * T::E);
-      }
+      for (int b = 0; b < kBatch - 1; ++b)
+        raw[b] = *reinterpret_cast<const typename T::raw *>(r + b * cut.ty < rows ? p + b * step : p);
+#pragma unroll
+      for (int b = 0; b < kBatch - 1; ++b)
+        if (r + b * cut.ty < rows) one(raw[b], y + b * step_y);
     }
   }
 }
@@ -399,31 +420,46 @@ __global__ __launch_bounds__(kThreads) void grad_sums_kernel(pgcn_group_norm_bwd
         float mu[T::E], rs[T::E], ga[T::E], be[T::E];
 #pragma unroll
         for (int e = 0; e < T::E; ++e) {
-          const int c = vec * T::E + e < f ? vec * T::E + e : f - 1;
-          mu[e] = a.mean[sample * a.groups + c / cg];
-          rs[e] = a.rstd[sample * a.groups + c / cg];
+          const int c = vec * T::E + e < f ? vec * T::E + e : f - 1, g = group_of(cut.magic, c);
+          mu[e] = a.mean[sample * a.groups + g];
+          rs[e] = a.rstd[sample * a.groups + g];
           ga[e] = a.gamma ? a.gamma[c] : 1.f;
           be[e] = a.beta ? a.beta[c] : 0.f;
         }
-        for (int64_t r = slot; r < rows; r += kBatch * cut.ty) {
+        const typename T::type *p = (const typename T::type *)a.X + (row0 + slot) * a.ld_x + vec * T::E;
+        const typename T::type *q = (const typename T::type *)a.J_out + (row0 + slot) * a.ld_j_out + vec * T::E;
+        const int64_t step = cut.ty * a.ld_x, step_j = cut.ty * a.ld_j_out;
+        auto one = [&](const typename T::raw &xr, const typename T::raw &jr) {
+          float x[T::E], j[T::E];
+          grad_vector<T>(xr, jr, mu, rs, ga, be, a.act, x, j);
+#pragma unroll
+          for (int e = 0; e < T::E; ++e) {
+            s1[e] += j[e];
+            s2[e] += j[e] * x[e];
+          }
+        };
+        int64_t r = slot;
+        for (; r + (kBatch - 1) * cut.ty < rows; r += kBatch * cut.ty, p += kBatch * step, q += kBatch * step_j) {
           typename T::raw xr[kBatch], jr[kBatch];
 #pragma unroll
-          for (int b = 0; b < kBatch; ++b)
-            if (r + b * cut.ty < rows) {
-              xr[b] = *reinterpret_cast<const typename T::raw *>((const typename T::type *)a.X + (row0 + r + b * cut.ty) * a.ld_x + vec * T::E);
-              jr[b] = *reinterpret_cast<const typename T::raw *>((const typename T::type *)a.J_out + (row0 + r + b * cut.ty) * a.ld_j_out + vec * T::E);
-            }
-#pragma unroll
           for (int b = 0; b < kBatch; ++b) {
-            if (r + b * cut.ty >= rows) break;
-            float x[T::E], j[T::E];
-            grad_vector<T>(xr[b], jr[b], mu, rs, ga, be, a.act, x, j);
-#pragma unroll
-            for (int e = 0; e < T::E; ++e) {
-              s1[e] += j[e];
-              s2[e] += j[e] * x[e];
-            }
+            xr[b] = *reinterpret_cast<const typename T::raw *>(p + b * step);
+            jr[b] = *reinterpret_cast<const typename T::raw *>(q + b * step_j);
           }
+#pragma unroll
+          for (int b = 0; b < kBatch; ++b) one(xr[b], jr[b]);
+        }
+        if (r < rows) {
+          typename T::raw xr[kBatch - 1], jr[kBatch - 1];
+#pragma unroll
+          for (int b = 0; b < kBatch - 1; ++b) {
+            const bool in = r + b * cut.ty < rows;
+            xr[b] = *reinterpret_cast<const typename T::raw *>(in ? p + b * step : p);
+            jr[b] = *reinterpret_cast<const typename T::raw *>(in ? q + b * step_j : q);
+          }
+#pragma unroll
+          for (int b = 0; b < kBatch - 1; ++b)
+            if (r + b * cut.ty < rows) one(xr[b], jr[b]);
         }
       }
       for (int left = cut.ty; left > 1; left = (left + 1) / 2) {
@@ -503,7 +539,7 @@ template <class T>
 __global__ __launch_bounds__(kThreads) void grad_rows_kernel(pgcn_group_norm_bwd_args a, Cut cut, const float2 *part,
                                                              const float *channel_part, int sum_blocks, int row_blocks) {
   extern __shared__ float lds[];                        // c1, c2: [2][groups]
-  __shared__ float2 red[kThreads];
+  __shared__ Sum2 red[kThreads];
   if ((int)blockIdx.x >= row_blocks) {
     param_grads(channel_part, sum_blocks, a.channels, blockIdx.x - row_blocks, a.dgamma, a.dbeta);
     return;
@@ -511,10 +547,12 @@ __global__ __launch_bounds__(kThreads) void grad_rows_kernel(pgcn_group_norm_bwd
   const int f = a.channels, cg = f / a.groups, tx = threadIdx.x % cut.lx, slot = threadIdx.x / cut.lx;
   const int64_t sample = blockIdx.x / cut.out_blocks;
   const int block = (int)(blockIdx.x - sample * cut.out_blocks);
-  const float inv_n = 1.0f / ((float)a.sample_rows * (float)cg);
-  add_chunks(part + sample * cut.chunks * a.groups, cut.chunks, a.groups, red, [&](int g, const float2 &s) {
-    lds[g] = s.x * inv_n;
-    lds[a.groups + g] = s.y * inv_n;
+  const double inv_n = 1.0 / ((double)a.sample_rows * (double)cg);
+  join_chunks(part + sample * cut.chunks * a.groups, cut.chunks, a.groups, a.sample_rows, cut.per, cg, red,
+              [](double, const float2 &p) { return Sum2{(double)p.x, (double)p.y}; },
+              [&](int g, const Sum2 &t) {
+    lds[g] = (float)(t.x * inv_n);
+    lds[a.groups + g] = (float)(t.y * inv_n);
   });
   __syncthreads();
   if (slot >= cut.ty) return;
@@ -523,31 +561,48 @@ __global__ __launch_bounds__(kThreads) void grad_rows_kernel(pgcn_group_norm_bwd
     float mu[T::E], rs[T::E], ga[T::E], be[T::E], c1[T::E], c2[T::E];
 #pragma unroll
     for (int e = 0; e < T::E; ++e) {
-      const int c = vec * T::E + e < f ? vec * T::E + e : f - 1;
-      mu[e] = a.mean[sample * a.groups + c / cg];
-      rs[e] = a.rstd[sample * a.groups + c / cg];
+      const int c = vec * T::E + e < f ? vec * T::E + e : f - 1, g = group_of(cut.magic, c);
+      mu[e] = a.mean[sample * a.groups + g];
+      rs[e] = a.rstd[sample * a.groups + g];
       ga[e] = a.gamma ? a.gamma[c] : 1.f;
       be[e] = a.beta ? a.beta[c] : 0.f;
-      c1[e] = lds[c / cg];
-      c2[e] = lds[a.groups + c / cg];
+      c1[e] = lds[g];
+      c2[e] = lds[a.groups + g];
     }
-    for (int64_t r = slot; r < rows; r += kBatch * cut.ty) {
+    const typename T::type *p = (const typename T::type *)a.X + (row0 + slot) * a.ld_x + vec * T::E;
+    const typename T::type *q = (const typename T::type *)a.J_out + (row0 + slot) * a.ld_j_out + vec * T::E;
+    typename T::type *y = (typename T::type *)a.J_in + (row0 + slot) * a.ld_j_in + vec * T::E;
+    const int64_t step = cut.ty * a.ld_x, step_j = cut.ty * a.ld_j_out, step_y = cut.ty * a.ld_j_in;
+    const int left = f - vec * T::E;
+    auto one = [&](const typename T::raw &xr, const typename T::raw &jr, typename T::type *to) {
+      float x[T::E], j[T::E];
+      grad_vector<T>(xr, jr, mu, rs, ga, be, a.act, x, j);
+#pragma unroll
+      for (int e = 0; e < T::E; ++e) x[e] = rs[e] * (ga[e] * j[e] - c1[e] - x[e] * c2[e]);
+      store_some<T>(to, x, left);
+    };
+    int64_t r = slot;
+    for (; r + (kBatch - 1) * cut.ty < rows; r += kBatch * cut.ty, p += kBatch * step, q += kBatch * step_j, y += kBatch * step_y) {
       typename T::raw xr[kBatch], jr[kBatch];
 #pragma unroll
-      for (int b = 0; b < kBatch; ++b)
-        if (r + b * cut.ty < rows) {
-          xr[b] = *reinterpret_cast<const typename T::raw *>((const typename T::type *)a.X + (row0 + r + b * cut.ty) * a.ld_x + vec * T::E);
-          jr[b] = *reinterpret_cast<const typename T::raw *>((const typename T::type *)a.J_out + (row0 + r + b * cut.ty) * a.ld_j_out + vec * T::E);
-        }
-#pragma unroll
       for (int b = 0; b < kBatch; ++b) {
-        if (r + b * cut.ty >= rows) break;
-        float x[T::E], j[T::E];
-        grad_vector<T>(xr[b], jr[b], mu, rs, ga, be, a.act, x, j);
-#pragma unroll
-        for (int e = 0; e < T::E; ++e) x[e] = rs[e] * (ga[e] * j[e] - c1[e] - x[e] * c2[e]);
-        store_some<T>((typename T::type *)a.J_in + (row0 + r + b * cut.ty) * a.ld_j_in + vec * T::E, x, f - vec * T::E);
+        xr[b] = *reinterpret_cast<const typename T::raw *>(p + b * step);
+        jr[b] = *reinterpret_cast<const typename T::raw *>(q + b * step_j);
       }
+#pragma unroll
+      for (int b = 0; b < kBatch; ++b) one(xr[b], jr[b], y + b * step_y);
+    }
+    if (r < rows) {
+      typename T::raw xr[kBatch - 1], jr[kBatch - 1];
+#pragma unroll
+      for (int b = 0; b < kBatch - 1; ++b) {
+        const bool in = r + b * cut.ty < rows;
+        xr[b] = *reinterpret_cast<const typename T::raw *>(in ? p + b * step : p);
+        jr[b] = *reinterpret_cast<const typename T::raw *>(in ? q + b * step_j : q);
+      }
+#pragma unroll
+      for (int b = 0; b < kBatch - 1; ++b)
+        if (r + b * cut.ty < rows) one(xr[b], jr[b], y + b * step_y);
     }
   }
 }
@@ -568,10 +623,8 @@ struct RowShape {
   int f, groups, cg, vecs;
   int span;            // LANES: vectors of a group
   int team;            // LDS: lanes of a team
-  uint32_t magic;      // c / cg = umulhi(c, magic) for c < 2^13; 0: cg is 1
+  uint32_t magic;      // of groups, see group_of
 };
-
-__device__ __forceinline__ int group_of(const RowShape &sp, int c) { return sp.magic ? (int)__umulhi((uint32_t)c, sp.magic) : c; }
 
 template <int kLanes>
 __device__ __forceinline__ void row_sync() {
@@ -614,7 +667,7 @@ __device__ __forceinline__ void group_sums(const float (&w)[kVecs][T::E], float 
 #pragma unroll
       for (int e = 0; e < kOut; ++e) {
         const int c = (lane + kLanes * i) * T::E + e;
-        out[i][e] = res[group_of(sp, c < sp.f ? c : 0)];
+        out[i][e] = res[group_of(sp.magic, c < sp.f ? c : 0)];
       }
     return;
   }
@@ -709,7 +762,7 @@ __global__ __launch_bounds__(kThreads) void rows_fwd_kernel(pgcn_group_norm_fwd_
         // the thread with a group's first channel writes its statistics
 #pragma unroll
         for (int e = 0; e < kOut; ++e) {
-          const int c = c0 + e, g = group_of(sp, c);
+          const int c = c0 + e, g = group_of(sp.magic, c);
           if (c < sp.f && g * sp.cg == c) {
             if (a.mean) a.mean[r * sp.groups + g] = mu[i][e];
             if (a.rstd) a.rstd[r * sp.groups + g] = rs[i][e];
@@ -745,7 +798,7 @@ __global__ __launch_bounds__(kThreads) void rows_bwd_kernel(pgcn_group_norm_bwd_
       float mu[kOut], u[T::E];
 #pragma unroll
       for (int e = 0; e < kOut; ++e) {
-        const int64_t g = r * sp.groups + group_of(sp, c0 + e < sp.f ? c0 + e : 0);
+        const int64_t g = r * sp.groups + group_of(sp.magic, c0 + e < sp.f ? c0 + e : 0);
         mu[e] = a.mean[g];
         rs[i][e] = a.rstd[g];
       }
@@ -831,7 +884,7 @@ RowShape row_shape(int32_t dtype, int32_t f, int32_t groups, int lanes) {
   sp.span = sp.cg % e == 0 ? sp.cg / e : 0;
   sp.team = 1;
   while (sp.team < 64 && 2 * sp.team * groups <= lanes) sp.team *= 2;
-  sp.magic = sp.cg > 1 ? (uint32_t)(((uint64_t(1) << 32) + sp.cg - 1) / sp.cg) : 0;
+  sp.magic = group_magic(sp.cg);
   return sp;
 }
 
@@ -913,7 +966,7 @@ int rows_bwd(const pgcn_group_norm_bwd_args &a, hipStream_t s) {
 
 template <class T>
 int chunks_fwd(const pgcn_group_norm_fwd_args &a, hipStream_t s) {
-  const Cut cut = cut_rows(a.dtype, a.channels, a.samples, a.sample_rows);
+  const Cut cut = cut_rows(a.dtype, a.channels, a.groups, a.samples, a.sample_rows);
   float2 *part = (float2 *)a.workspace;
   hipLaunchKernelGGL(moments_kernel<T>, dim3((unsigned)(a.samples * cut.chunks)), dim3(kThreads),
                      4 * (2 * (size_t)a.channels + (size_t)a.groups), s, a, cut, part);
@@ -929,11 +982,11 @@ size_t group_part_bytes(const Cut &cut, int32_t groups, int64_t samples) {
   return align_up(8 * (size_t)samples * (size_t)cut.chunks * (size_t)groups, 16);
 }
 
-int chunk_sum_blocks(const Cut &cut, int64_t samples) { return (int)std::min<int64_t>(samples * cut.chunks, kChunkBlocks); }
+int chunk_sum_blocks(const Cut &cut, int64_t samples) { return (int)std::min<int64_t>(samples * cut.chunks, kStatBlocks); }
 
 template <class T>
 int chunks_bwd(const pgcn_group_norm_bwd_args &a, hipStream_t s) {
-  const Cut cut = cut_rows(a.dtype, a.channels, a.samples, a.sample_rows);
+  const Cut cut = cut_rows(a.dtype, a.channels, a.groups, a.samples, a.sample_rows);
   const bool params = a.dgamma || a.dbeta;
   if (a.samples == 0) return params ? launch_param_grads(nullptr, 0, a.channels, a.dgamma, a.dbeta, s) : PGCN_OK;
   if (!params && !a.J_in) return PGCN_OK;
@@ -961,7 +1014,7 @@ size_t group_norm_workspace(int32_t dtype, int32_t channels, int32_t groups, int
     row_threads((channels + e - 1) / e, lanes, per);
     return 8 * (size_t)channels * row_blocks(samples, lanes, kRowBlocksBwd);
   }
-  const Cut cut = cut_rows(dtype, channels, samples, sample_rows);
+  const Cut cut = cut_rows(dtype, channels, groups, samples, sample_rows);
   return group_part_bytes(cut, groups, samples) + 8 * (size_t)channels * (size_t)chunk_sum_blocks(cut, samples);
 }
 
