@@ -19,7 +19,7 @@ LIB = os.path.join(PKG, "libpgcn.so")
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 
 SOURCES = ["setup.cpp", "api.cpp", "trace.cpp", "aggregate.hip", "gemm.hip", "gemm_nk.hip", "elementwise.hip", "noalloc.hip",
-           "ops.cpp", "distill.hip", "norm.hip"]
+           "ops.cpp", "top.hip", "distill.hip", "norm.hip"]
 
 COMMON = ["-O3", "-fPIC", "-std=c++17", "--offload-arch=gfx950",
           "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",

@@ -1,5 +1,4 @@
-// Top logits of a row, and the loss of a student's logits against a teacher's top logits
-// with its gradient.
+// The loss of a student's logits against a teacher's top logits, with its gradient.
 //
 // With z a row of the student's logits, T the temperature, (y_k, t_k) the teacher's listed
 // classes and logits and b the log-sum of its other logits at T:
@@ -9,7 +8,12 @@
 //     d KL / d z_c = (q_c - p_c) / T            where c is listed
 //                    q_c (1 - rho / s) / T      elsewhere
 // The sum s is formed from the unlisted classes themselves, with their own maximum: 1 minus
-// the listed ones would lose s where the student is sure of its answer.
+// the listed ones would lose s where the student is sure of its answer.  All sums and the
+// loss are fp32 over a row, fp64 over the rows.
+//
+// Bound by one read of Z and one write of J.  A row stays in registers between its sums and
+// its gradient: in a few lanes of a wave (up to 2,048 classes), in a workgroup (up to 65,536
+// fp32 or 131,072 bf16 classes).  Longer rows, and few rows, are cut into parts and read twice.
 #include <algorithm>
 
 #include "ops.h"
@@ -18,296 +22,699 @@ namespace pgcn {
 
 namespace {
 
-constexpr float kNegInf = -INFINITY;
+constexpr float kLog2e = 1.44269504088896341f;
 
-// ------------------------------------------------------------- log-sums ----
+// e^{(x - m) T'} with scale = T' log2 e; 0 for x = -inf (m finite)
+__device__ __forceinline__ float exp_at(float x, float m, float scale) { return __builtin_amdgcn_exp2f((x - m) * scale); }
+// a maximum to subtract: 0 where there was nothing but -inf
+__device__ __forceinline__ float base_of(float m) { return m == kNegInf ? 0.f : m; }
 
-// sum of e^{(x - m) a} over some x, with m their maximum (s == 0: none but -inf seen)
-struct LogSum {
-  float m, s;
-};
-constexpr LogSum kNothing = {kNegInf, 0.f};
-
-__device__ __forceinline__ float exp_diff(float x, float m, float a) { return x == kNegInf ? 0.f : __expf((x - m) * a); }
-
-// A NaN leaves m and makes s NaN.
-__device__ __forceinline__ void add(LogSum &l, float x, float a) {
-  if (x == kNegInf) return;
-  const float m = fmaxf(l.m, x);
-  l.s = l.s * exp_diff(l.m, m, a) + __expf((x - m) * a);
-  l.m = m;
-}
-
-__device__ __forceinline__ LogSum merge(const LogSum &x, const LogSum &y, float a) {
-  LogSum r;
-  r.m = fmaxf(x.m, y.m);
-  r.s = x.s * exp_diff(x.m, r.m, a) + y.s * exp_diff(y.m, r.m, a);
-  return r;
-}
-
-template <int kLanes>
-__device__ __forceinline__ LogSum lanes_merge(LogSum l, float a) {
-#pragma unroll
-  for (int o = kLanes / 2; o > 0; o >>= 1) {
-    LogSum y;
-    y.m = __shfl_xor(l.m, o, 64);
-    y.s = __shfl_xor(l.s, o, 64);
-    l = merge(l, y, a);
-  }
-  return l;
-}
-
-// Over a workgroup of kThreads: every thread gets the result.  `part` is not reused by the
-// next call without a barrier in between.
-template <int kThreads>
-__device__ __forceinline__ LogSum block_merge(LogSum l, float a, LogSum *part) {
-  l = lanes_merge<64>(l, a);
-  if (kThreads == 64) return l;
-  if (threadIdx.x % 64 == 0) part[threadIdx.x / 64] = l;
-  __syncthreads();
-  LogSum r = part[0];
-#pragma unroll
-  for (int w = 1; w < kThreads / 64; ++w) r = merge(r, part[w], a);
-  return r;
-}
-
-// ------------------------------------------------------------ top logits ---
-
-// Order of (value, lowest class first) as whole numbers; -0 counts as +0.  0: never chosen
-// (-inf and NaN).
-__device__ __forceinline__ uint64_t top_key(float x, int c) {
-  if (!(x > kNegInf)) return 0;
-  const uint32_t b = __float_as_uint(x + 0.f);
-  const uint32_t o = (b & 0x80000000u) ? ~b : b | 0x80000000u;
-  return ((uint64_t)o << 32) | (uint32_t)~c;
-}
-
-__device__ __forceinline__ float key_value(uint64_t k) {
-  const uint32_t o = (uint32_t)(k >> 32);
-  return __uint_as_float((o & 0x80000000u) ? o & 0x7fffffffu : ~o);
-}
-
-__device__ __forceinline__ int key_class(uint64_t k) { return (int)~(uint32_t)k; }
-
-// One workgroup per row; every listed class is found by a pass over the row.
-template <class T>
-__global__ __launch_bounds__(256) void top_rows_kernel(pgcn_top_logits_args a) {
-  __shared__ uint64_t best[4];
-  __shared__ LogSum part[4];
-  const int64_t r = blockIdx.x;
-  const int C = a.classes, lane = threadIdx.x % 64, wave = threadIdx.x / 64;
-  const typename T::type *z = (const typename T::type *)a.Z + r * a.ld;
-  uint64_t last = ~(uint64_t)0;
-  for (int k = 0; k < a.top; ++k) {
-    uint64_t m = 0;
-    for (int c = threadIdx.x; c < C; c += 256) {
-      const uint64_t key = top_key(T::get(z + c), c);
-      if (key < last && key > m) m = key;
-    }
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) {
-      const uint64_t y = __shfl_xor((unsigned long long)m, o, 64);
-      m = y > m ? y : m;
-    }
-    __syncthreads();
-    if (lane == 0) best[wave] = m;
-    __syncthreads();
-    m = best[0];
-    for (int w = 1; w < 4; ++w) m = best[w] > m ? best[w] : m;
-    if (threadIdx.x == 0) {
-      a.top_values[r * a.ld_top + k] = m ? key_value(m) : kNegInf;
-      a.top_ids[r * a.ld_top + k] = m ? key_class(m) : -1;
-    }
-    last = m;
-  }
-  if (!a.tail_lse) return;
-  const float inv_t = 1.0f / a.temperature;
-  LogSum l = kNothing;
-  for (int c = threadIdx.x; c < C; c += 256) {
-    const float x = T::get(z + c);
-    if (top_key(x, c) < last || x != x) add(l, x, inv_t);
-  }
-  l = block_merge<256>(l, inv_t, part);
-  if (threadIdx.x == 0) a.tail_lse[r] = l.m * inv_t + __logf(l.s);
-}
-
-// ---------------------------------------------------------- distillation ---
-
-// What the gradient needs of a row: see the formulas above.  All exponents are taken
+// What the loss and the gradient need of a row: see the formulas above.  Exponents are taken
 // relative to a maximum, in the logits' own units.
 struct RowStats {
-  float m;          // maximum of the student's row
-  float log_all;    // log sum e^{(z - m) / T}
-  float m_rest, inv_rest, rest_gain;  // unlisted: e^{(z - m_rest) / T} inv_rest rest_gain = q (1 - rho / s)
-  float mt, log_t;  // teacher: p_k = e^{(t_k - mt) / T - log_t}
-  float rho, log_rho, log_s;
-  float inv_hard;   // 1 / sum e^{z - m}
-  float log_hard;
-  bool soft;        // the teacher lists something
+  float m, log_all;       // of the student's row: maximum, log sum e^{(z - m) / T}
+  float m_rest, log_s;    // unlisted: maximum, log of their share s
+  float gain;             // unlisted: d KL / d z T = e^{(z - m_rest) / T} gain
+  float mt, log_t;        // teacher: p_k = e^{(t_k - mt) / T - log_t}
+  float rho, log_rho;
+  float inv_hard, log_hard;   // sum e^{z - m}: its reciprocal, its logarithm
+  bool soft;              // the teacher lists something
+  bool some;              // there is an unlisted logit above -inf
 };
 
-__device__ __forceinline__ RowStats row_stats(const LogSum &rest, const LogSum &top, const LogSum &teacher,
-                                              const LogSum &hard, bool has_tail, float tail, float inv_t) {
+__device__ __forceinline__ RowStats row_stats(const LogSum &rest, const LogSum &top, const LogSum &teacher, float hard, float m,
+                                              const float *tail_lse, int64_t r, float inv_t) {
   RowStats st;
   const LogSum all = merge(rest, top, inv_t);
-  st.m = all.m;
+  st.m = m;
   st.log_all = __logf(all.s);
   st.soft = teacher.s != 0.f;                      // NaN counts: it has to show
-  st.mt = teacher.m;
-  st.log_rho = kNegInf;
-  if (has_tail && tail != kNegInf) {
-    const float b = tail - teacher.m * inv_t;      // e^b beside the listed ones' sum
-    const float top_ = fmaxf(b, 0.f);
-    st.log_t = top_ + __logf(teacher.s * __expf(-top_) + __expf(b - top_));
+  st.mt = base_of(teacher.m);
+  const float tail = tail_lse ? tail_lse[r] : kNegInf;
+  if (tail != kNegInf) {
+    const float b = tail - st.mt * inv_t;          // e^b beside the listed ones' sum
+    const float big = fmaxf(b, 0.f);
+    st.log_t = big + __logf(teacher.s * __expf(-big) + __expf(b - big));
     st.log_rho = b - st.log_t;
     st.rho = __expf(st.log_rho);
   } else {
     st.log_t = __logf(teacher.s);
+    st.log_rho = kNegInf;
     st.rho = 0.f * st.log_t;                       // a NaN among the listed values spreads to the row
   }
-  st.m_rest = rest.m;
-  const bool some = rest.s != 0.f;
-  st.log_s = some ? (rest.m - all.m) * inv_t + __logf(rest.s) - st.log_all : kNegInf;
-  st.inv_rest = some ? 1.0f / rest.s : 0.f;
-  st.rest_gain = __expf(st.log_s) - st.rho;        // s - rho
-  st.log_hard = __logf(hard.s);
-  st.inv_hard = 1.0f / hard.s;
+  st.m_rest = base_of(rest.m);
+  st.some = rest.s != 0.f;
+  st.log_s = st.some ? (rest.m - all.m) * inv_t + __logf(rest.s) - st.log_all : kNegInf;
+  st.gain = st.some ? (__expf(st.log_s) - st.rho) / rest.s : 0.f;
+  st.log_hard = __logf(hard);
+  st.inv_hard = 1.0f / hard;
   return st;
 }
 
-__device__ __forceinline__ float kl_term(float p, float log_p, float log_q) { return p > 0.f ? p * (log_p - log_q) : (p == 0.f ? 0.f : p); }
+__device__ __forceinline__ float kl_term(float p, float log_p, float log_q) {
+  return p > 0.f ? p * (log_p - log_q) : (p == 0.f ? 0.f : p);
+}
 
-// One workgroup per row, the row read twice.
-template <class T>
-__global__ __launch_bounds__(256) void distill_rows_kernel(pgcn_distill_args a, float *row_loss) {
-  extern __shared__ uint32_t listed[];             // a bit for every class: listed by the teacher
-  __shared__ LogSum part[4][4];
-  __shared__ int ids[PGCN_MAX_TOP];
-  __shared__ float wave_loss[4];
-  __shared__ int bad;
-  const int64_t r = blockIdx.x;
-  const int C = a.classes, K = a.top, k = threadIdx.x, lane = k % 64, wave = k / 64;
-  const typename T::type *z = (const typename T::type *)a.Z + r * a.ld;
-  typename T::type *j = (typename T::type *)a.J + r * a.ld;
-  const float inv_t = 1.0f / a.temperature;
+// A listed class: its loss term, and its gradient without the one-hot part.
+__device__ __forceinline__ float listed_term(const RowStats &st, float t, float z, float inv_t, float soft, float hard, float soft_scale,
+                                             float &loss) {
+  float g = 0.f;
+  if (st.soft) {
+    const float log_p = (t - st.mt) * inv_t - st.log_t, p = t == kNegInf ? 0.f : __expf(log_p);
+    const float log_q = (z - st.m) * inv_t - st.log_all;
+    loss = soft_scale * kl_term(p, log_p, log_q);
+    g = soft * (__expf(log_q) - p);
+  }
+  if (hard != 0.f) g += hard * (z == kNegInf ? 0.f : __expf(z - st.m)) * st.inv_hard;
+  return g;
+}
 
-  for (int w = k; w < (C + 31) / 32; w += 256) listed[w] = 0;
-  int id = -1;
-  float t = kNegInf, zk = kNegInf;
+// The row's loss beside its listed terms.
+__device__ __forceinline__ float row_loss(const RowStats &st, float listed, float z_label, bool has_label, bool poison, float soft_scale,
+                                          float hard) {
+  float l = listed;
+  if (st.soft) l += soft_scale * kl_term(st.rho, st.log_rho, st.log_s);
+  if (has_label) l += hard * (st.m + st.log_hard - z_label);
+  return poison ? __builtin_nanf("") : l;          // an id or label out of range
+}
+
+// ---- short rows: kLanes lanes of a wave hold a row, kVecs vectors each ---------------------
+//
+// The row's image in LDS serves the listed classes, kSlots to a lane: their logits are read
+// from it, and their gradients written into it for the lane that holds the class.  mark[c] is
+// the lowest slot that lists c (an integer minimum, so its order does not matter).
+
+constexpr int kUnlisted = 0x7fffffff;
+
+template <class T, int kLanes, int kVecs, int kSlots>
+__global__ __launch_bounds__(256) void distill_short_kernel(pgcn_distill_args a, double *part) {
+  constexpr int kWide = kLanes * kVecs * T::E, kRows = 256 / kLanes;
+  __shared__ __align__(16) float image_[kRows * kWide];
+  __shared__ __align__(16) int mark_[kRows * kWide];
+  __shared__ double sums[kRows];
+  const int lane = threadIdx.x % kLanes, slot = threadIdx.x / kLanes, C = a.classes, K = a.top;
+  float *image = image_ + slot * kWide;
+  int *mark = mark_ + slot * kWide;
+  const float inv_t = 1.0f / a.temperature, scale_t = inv_t * kLog2e;
+  const bool same = a.temperature == 1.0f;         // the hard term's exponentials are the soft ones
+  double total = 0.0;
+
+  for (int64_t r = (int64_t)blockIdx.x * kRows + slot; r < a.rows; r += (int64_t)gridDim.x * kRows) {
+    const typename T::type *zr = (const typename T::type *)a.Z + r * a.ld;
+    float x[kVecs][T::E];
+    typename T::raw raw[kVecs];
+#pragma unroll
+    for (int i = 0; i < kVecs; ++i) {
+      const int c0 = (lane + kLanes * i) * T::E;
+      raw[i] = c0 < C ? *reinterpret_cast<const typename T::raw *>(zr + c0) : typename T::raw{};
+    }
+    int id[kSlots];
+    float t[kSlots], zk[kSlots];
+#pragma unroll
+    for (int i = 0; i < kSlots; ++i) {
+      const int k = lane + kLanes * i;
+      id[i] = k < K ? a.top_ids[r * a.ld_top + k] : -1;
+      t[i] = k < K ? a.top_values[r * a.ld_top + k] : kNegInf;
+    }
+    const int y = a.labels ? a.labels[r] : -1;
+    const bool has_y = y >= 0 && y < C;
+    bool bad = y != -1 && !has_y;
+
+    wave_sync();                                   // the row before is done with its image
+#pragma unroll
+    for (int i = 0; i < kVecs; ++i) {
+      const int c0 = (lane + kLanes * i) * T::E;
+      T::unpack(raw[i], x[i]);
+#pragma unroll
+      for (int e = 0; e < T::E; ++e) {
+        if (c0 + e >= C) x[i][e] = kNegInf;
+        image[c0 + e] = x[i][e];
+        mark[c0 + e] = kUnlisted;
+      }
+    }
+    wave_sync();
+#pragma unroll
+    for (int i = 0; i < kSlots; ++i) {
+      if (id[i] >= C) {
+        bad = true;
+        id[i] = -1;
+      }
+      if (id[i] >= 0) atomicMin(&mark[id[i]], lane + kLanes * i);
+    }
+    wave_sync();
+    float mt = kNegInf, m_top = kNegInf, m_rest = kNegInf;
+#pragma unroll
+    for (int i = 0; i < kSlots; ++i) {
+      if (id[i] >= 0 && mark[id[i]] != lane + kLanes * i) id[i] = -1;       // listed before
+      if (id[i] < 0) t[i] = kNegInf;
+      zk[i] = id[i] >= 0 ? image[id[i]] : kNegInf;
+      mt = fmaxf(mt, t[i]);
+      m_top = fmaxf(m_top, zk[i]);
+    }
+    const float z_label = has_y ? image[y] : 0.f;
+    bool free_[kVecs][T::E];
+#pragma unroll
+    for (int i = 0; i < kVecs; ++i)
+#pragma unroll
+      for (int e = 0; e < T::E; ++e) {
+        free_[i][e] = mark[(lane + kLanes * i) * T::E + e] == kUnlisted;
+        m_rest = fmaxf(m_rest, free_[i][e] ? x[i][e] : kNegInf);
+      }
+    mt = lanes_max<kLanes>(mt);
+    m_top = lanes_max<kLanes>(m_top);
+    m_rest = lanes_max<kLanes>(m_rest);
+    const float m = fmaxf(m_top, m_rest), bt = base_of(mt), b_top = base_of(m_top), b_rest = base_of(m_rest), b_all = base_of(m);
+    float st_ = 0.f, s_top = 0.f, s_rest = 0.f, s_hard = 0.f;
+#pragma unroll
+    for (int i = 0; i < kSlots; ++i) {
+      st_ += exp_at(t[i], bt, scale_t);
+      s_top += exp_at(zk[i], b_top, scale_t);
+      if (!same) s_hard += exp_at(zk[i], b_all, kLog2e);
+    }
+    float h[kVecs][T::E];
+#pragma unroll
+    for (int i = 0; i < kVecs; ++i)
+#pragma unroll
+      for (int e = 0; e < T::E; ++e) {
+        const float v = free_[i][e] ? x[i][e] : kNegInf;
+        x[i][e] = exp_at(v, b_rest, scale_t);
+        s_rest += x[i][e];
+        h[i][e] = 0.f;
+        if (!same && a.labels) {
+          h[i][e] = exp_at(v, b_all, kLog2e);
+          s_hard += h[i][e];
+        }
+      }
+    st_ = lanes_sum<kLanes>(st_);
+    s_top = lanes_sum<kLanes>(s_top);
+    s_rest = lanes_sum<kLanes>(s_rest);
+    const LogSum rest = {m_rest, s_rest}, top = {m_top, s_top};
+    s_hard = same ? merge(rest, top, 1.0f).s : lanes_sum<kLanes>(s_hard);
+    const RowStats st = row_stats(rest, top, LogSum{mt, st_}, s_hard, m, a.tail_lse, r, inv_t);
+    const float soft = st.soft ? a.soft_scale * inv_t : 0.f, hard = has_y ? a.hard_scale : 0.f;
+
+    float loss = 0.f;
+#pragma unroll
+    for (int i = 0; i < kSlots; ++i)
+      if (id[i] >= 0) {
+        float l = 0.f;
+        image[id[i]] = listed_term(st, t[i], zk[i], inv_t, soft, hard, a.soft_scale, l);
+        loss += l;
+      }
+    loss = lanes_sum<kLanes>(loss);
+    float any_bad = lanes_max<kLanes>(bad ? 1.f : 0.f);
+    wave_sync();
+    // unlisted: soft e^{(z - m_rest) / T} gain + hard e^{z - m} / sum
+    const float gs = soft != 0.f ? soft * st.gain : 0.f;
+    const float gh = hard != 0.f ? hard * st.inv_hard : 0.f;
+    const float g_one = same && gh != 0.f && st.some ? gs + gh * exp_at(b_rest, b_all, kLog2e) : gs;
+#pragma unroll
+    for (int i = 0; i < kVecs; ++i) {
+      const int c0 = (lane + kLanes * i) * T::E;
+      if (c0 >= C) continue;
+      float g[T::E];
+#pragma unroll
+      for (int e = 0; e < T::E; ++e) {
+        float v = g_one != 0.f ? x[i][e] * g_one : 0.f;
+        if (!same && gh != 0.f) v += h[i][e] * gh;
+        if (!free_[i][e]) v = image[c0 + e];
+        g[e] = c0 + e == y ? v - hard : v;
+      }
+      store_some<T>((typename T::type *)a.J + r * a.ld + c0, g, C - c0);
+    }
+    if (lane == 0) total += (double)row_loss(st, loss, z_label, has_y, any_bad != 0.f, a.soft_scale, hard);
+  }
+  if (lane == 0) sums[slot] = total;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    for (int i = 1; i < kRows; ++i) total += sums[i];
+    if (gridDim.x == 1) *a.loss_out = (float)total;
+    else part[blockIdx.x] = total;
+  }
+}
+
+// ---- long rows: a workgroup holds a row, kVecs vectors to a thread --------------------------
+//
+// The listed classes have a bit each in LDS and are taken out of the threads' vectors (-inf);
+// thread k takes slot k, and writes its class's gradient over the one that the vector left.
+
+template <int kThreads>
+struct ListLds {
+  int ids[PGCN_MAX_TOP];
+  int twice, bad;
+  float m_rest[kThreads / 64], s_rest[kThreads / 64], s_hard[kThreads / 64];
+  float m_top[4], m_t[4], s_top[4], s_t[4], s_hard_top[4], loss[4];
+};
+
+// Slot threadIdx.x of row r: its class (-1: none, or listed before) in `id`.  Sets a bit for
+// every listed class in [first, first + 32 words), seen by all after the call.
+template <int kThreads>
+__device__ __forceinline__ void list_classes(const pgcn_distill_args &a, int64_t r, uint32_t *bits, int first, int words,
+                                             ListLds<kThreads> &l, int &id, float &t) {
+  const int k = threadIdx.x, K = a.top;
+  id = -1;
+  t = kNegInf;
   if (k < K) {
     id = a.top_ids[r * a.ld_top + k];
     t = a.top_values[r * a.ld_top + k];
   }
-  if (k == 0) bad = 0;
-  if (k < PGCN_MAX_TOP) ids[k] = id;
+  for (int w = k; w < words; w += kThreads) bits[w] = 0;
+  if (k == 0) l.twice = l.bad = 0;
   __syncthreads();
-  if (id >= C) {
-    bad = 1;                                       // every writer writes the same value
+  if (id >= a.classes) {
+    l.bad = 1;                                     // every writer writes the same value
     id = -1;
   }
-  for (int i = 0; i < k && i < K; ++i)
-    if (ids[i] == id) id = -1;                     // listed before: the lowest slot counts
+  if (k < PGCN_MAX_TOP) l.ids[k] = id;
+  const int c = id - first;
   if (id >= 0) {
-    atomicOr(&listed[id / 32], 1u << (id % 32));
-    zk = T::get(z + id);
-  } else {
-    t = kNegInf;
+    if (c >= 0 && c < 32 * words) {
+      if ((atomicOr(&bits[c / 32], 1u << (c % 32)) >> (c % 32)) & 1u) l.twice = 1;
+    } else {
+      l.twice = 1;                                 // no bit of its own: compare the ids
+    }
+  }
+  __syncthreads();
+  if (l.twice && id >= 0) {                        // of equal ids the lowest slot counts
+    bool again = false;
+    for (int i = 0; i < k; ++i) again |= l.ids[i] == id;
+    if (again) id = -1;
+  }
+  if (id < 0) t = kNegInf;
+}
+
+// -inf for the elements whose bit is set, and from the n-th on.
+template <class T>
+__device__ __forceinline__ void drop_listed(float (&x)[T::E], uint32_t bits, int n) {
+  if (n < T::E) bits |= ~0u << (n > 0 ? n : 0);
+#pragma unroll
+  for (int e = 0; e < T::E; ++e)
+    if ((bits >> e) & 1u) x[e] = kNegInf;
+}
+
+// The same value, unknown to the compiler: what follows from it is computed anew in each pass over
+// a row, and not kept in registers that the row needs.
+__device__ __forceinline__ int again(int x) {
+  asm volatile("" : "+s"(x));
+  return x;
+}
+
+// Maximum and sums over the workgroup, of the listed classes (the first four waves) and the
+// others: m_rest is the maximum of the thread's own unlisted logits, rest(base, scale) the sum
+// of their e^{(z - base) scale ln 2}, hard(base) of e^{z - base}.
+template <int kThreads, class Rest, class Hard>
+__device__ __forceinline__ RowStats block_stats(const pgcn_distill_args &a, int64_t r, ListLds<kThreads> &l, float t, float zk,
+                                                float m_rest, float inv_t, Rest rest_sum, Hard hard_sum) {
+  constexpr int kWaves = kThreads / 64;
+  const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+  const float scale_t = inv_t * kLog2e;
+  const bool same = a.temperature == 1.0f;
+  m_rest = lanes_max<64>(m_rest);
+  if (lane == 0) l.m_rest[wave] = m_rest;
+  if (wave < 4) {
+    const float m_top = lanes_max<64>(zk), m_t = lanes_max<64>(t);
+    if (lane == 0) {
+      l.m_top[wave] = m_top;
+      l.m_t[wave] = m_t;
+    }
+  }
+  __syncthreads();
+  m_rest = l.m_rest[0];
+#pragma unroll
+  for (int w = 1; w < kWaves; ++w) m_rest = fmaxf(m_rest, l.m_rest[w]);
+  const float m_top = fmaxf(fmaxf(l.m_top[0], l.m_top[1]), fmaxf(l.m_top[2], l.m_top[3]));
+  const float m_t = fmaxf(fmaxf(l.m_t[0], l.m_t[1]), fmaxf(l.m_t[2], l.m_t[3]));
+  const float m = fmaxf(m_rest, m_top), b_rest = base_of(m_rest), b_all = base_of(m);
+  float s_rest = lanes_sum<64>(rest_sum(b_rest, scale_t));
+  float s_hard = a.labels && !same ? lanes_sum<64>(hard_sum(b_all)) : 0.f;
+  if (lane == 0) {
+    l.s_rest[wave] = s_rest;
+    l.s_hard[wave] = s_hard;
+  }
+  if (wave < 4) {
+    const float s_top = lanes_sum<64>(exp_at(zk, base_of(m_top), scale_t)), s_t = lanes_sum<64>(exp_at(t, base_of(m_t), scale_t));
+    const float s_h = lanes_sum<64>(exp_at(zk, b_all, kLog2e));
+    if (lane == 0) {
+      l.s_top[wave] = s_top;
+      l.s_t[wave] = s_t;
+      l.s_hard_top[wave] = s_h;
+    }
+  }
+  __syncthreads();
+  s_rest = l.s_rest[0];
+  s_hard = l.s_hard[0];
+#pragma unroll
+  for (int w = 1; w < kWaves; ++w) {
+    s_rest += l.s_rest[w];
+    s_hard += l.s_hard[w];
+  }
+  const LogSum rest = {m_rest, s_rest}, top = {m_top, (l.s_top[0] + l.s_top[1]) + (l.s_top[2] + l.s_top[3])};
+  const LogSum teacher = {m_t, (l.s_t[0] + l.s_t[1]) + (l.s_t[2] + l.s_t[3])};
+  s_hard += (l.s_hard_top[0] + l.s_hard_top[1]) + (l.s_hard_top[2] + l.s_hard_top[3]);
+  if (same) s_hard = merge(rest, top, 1.0f).s;
+  return row_stats(rest, top, teacher, s_hard, m, a.tail_lse, r, inv_t);
+}
+
+// Keeps the packed vectors, and not what one pass over them computed, in registers for the next.
+template <class Raw, int kVecs>
+__device__ __forceinline__ void keep_packed(Raw (&raw)[kVecs]) {
+#pragma unroll
+  for (int i = 0; i < kVecs; ++i) asm volatile("" : "+v"(raw[i]));
+}
+
+template <class T, int kVecs>
+__device__ __forceinline__ float vectors_sum(typename T::raw (&raw)[kVecs], float base, float scale) {
+  keep_packed(raw);
+  float s[2] = {0.f, 0.f};
+#pragma unroll
+  for (int i = 0; i < kVecs; ++i) {
+    float x[T::E];
+    T::unpack(raw[i], x);
+#pragma unroll
+    for (int e = 0; e < T::E; ++e) s[e % 2] += exp_at(x[e], base, scale);
+    if (kVecs > 4) __builtin_amdgcn_sched_barrier(0);
+  }
+  return s[0] + s[1];
+}
+
+// Gradient of unlisted logits: one factor for each exponential.
+struct RestGrad {
+  float soft, hard, b_rest, b_all, scale_t;
+  bool two;               // the hard term has exponentials of its own
+  __device__ __forceinline__ RestGrad(const pgcn_distill_args &a, const RowStats &st, float soft_, float hard_, float inv_t) {
+    const float gh = hard_ != 0.f ? hard_ * st.inv_hard : 0.f;
+    soft = soft_ != 0.f ? soft_ * st.gain : 0.f;
+    b_rest = st.m_rest;
+    b_all = base_of(st.m);
+    scale_t = inv_t * kLog2e;
+    two = a.temperature != 1.0f && gh != 0.f;
+    hard = two ? gh : 0.f;
+    if (!two && gh != 0.f && st.some) soft += gh * exp_at(b_rest, b_all, kLog2e);
+  }
+  __device__ __forceinline__ float operator()(float x) const {
+    float g = soft != 0.f ? exp_at(x, b_rest, scale_t) * soft : 0.f;
+    if (two) g += exp_at(x, b_all, kLog2e) * hard;
+    return g;
+  }
+};
+
+// The gradient of a thread's vectors (from class `first` on), less `hard` at the label.
+template <class T, int kThreads, int kVecs>
+__device__ __forceinline__ void store_vectors(typename T::raw (&raw)[kVecs], const RestGrad &grad, typename T::type *jr, int first,
+                                              int C, int y, float hard) {
+  keep_packed(raw);
+#pragma unroll
+  for (int i = 0; i < kVecs; ++i) {
+    const int c0 = first + ((int)threadIdx.x + kThreads * i) * T::E;
+    if (c0 < C) {
+      float x[T::E];
+      T::unpack(raw[i], x);
+#pragma unroll
+      for (int e = 0; e < T::E; ++e) x[e] = grad(x[e]) - (y - c0 == e ? hard : 0.f);
+      store_some<T>(jr + c0, x, C - c0);
+    }
+    __builtin_amdgcn_sched_barrier(0);             // one vector at a time: their temporaries do not add up
+  }
+}
+
+template <class T, int kThreads, int kVecs>
+__global__ __launch_bounds__(kThreads, kThreads == 1024 && kVecs <= 8 ? 8 : 0) void distill_long_kernel(pgcn_distill_args a, double *part) {
+  extern __shared__ uint32_t bits[];
+  __shared__ ListLds<kThreads> l;
+  const int64_t r = blockIdx.x;
+  const int C = a.classes, k = threadIdx.x, lane = k % 64, wave = k / 64;
+  const typename T::type *zr = (const typename T::type *)a.Z + r * a.ld;
+  typename T::type *jr = (typename T::type *)a.J + r * a.ld;
+  const float inv_t = 1.0f / a.temperature;
+  typename T::raw raw[kVecs];
+#pragma unroll
+  for (int i = 0; i < kVecs; ++i) {
+    const int c0 = (k + kThreads * i) * T::E;
+    raw[i] = c0 < C ? *reinterpret_cast<const typename T::raw *>(zr + c0) : typename T::raw{};
   }
   const int y = a.labels ? a.labels[r] : -1;
   const bool has_y = y >= 0 && y < C;
-  __syncthreads();
-
-  LogSum rest = kNothing, hard = kNothing, top = kNothing, teacher = kNothing;
-  for (int c = k; c < C; c += 256) {
-    const float x = T::get(z + c);
-    if (!((listed[c / 32] >> (c % 32)) & 1u)) add(rest, x, inv_t);
-    add(hard, x, 1.0f);
-  }
-  add(top, zk, inv_t);
-  add(teacher, t, inv_t);
-  rest = block_merge<256>(rest, inv_t, part[0]);
-  hard = block_merge<256>(hard, 1.0f, part[1]);
-  top = block_merge<256>(top, inv_t, part[2]);
-  teacher = block_merge<256>(teacher, inv_t, part[3]);
-  const RowStats st = row_stats(rest, top, teacher, hard, a.tail_lse != nullptr, a.tail_lse ? a.tail_lse[r] : 0.f, inv_t);
-
-  const float soft = st.soft ? a.soft_scale * inv_t : 0.f, hs = has_y ? a.hard_scale : 0.f;
-  for (int c = k; c < C; c += 256) {
-    if ((listed[c / 32] >> (c % 32)) & 1u) continue;
-    const float x = T::get(z + c);
-    float g = 0.f;
-    if (st.soft) g = soft * exp_diff(x, st.m_rest, inv_t) * st.inv_rest * st.rest_gain;
-    if (has_y) g += hs * (exp_diff(x, st.m, 1.0f) * st.inv_hard - (c == y ? 1.f : 0.f));
-    T::put(j + c, g);
-  }
-  float loss = 0.f;
-  if (id >= 0) {
-    float g = 0.f;
-    if (st.soft) {
-      const float log_p = (t - st.mt) * inv_t - st.log_t, p = t == kNegInf ? 0.f : __expf(log_p);
-      const float log_q = (zk - st.m) * inv_t - st.log_all;
-      loss = a.soft_scale * kl_term(p, log_p, log_q);
-      g = soft * (__expf(log_q) - p);
-    }
-    if (has_y) g += hs * (exp_diff(zk, st.m, 1.0f) * st.inv_hard - (id == y ? 1.f : 0.f));
-    T::put(j + id, g);
-  }
+  int id;
+  float t;
+  list_classes<kThreads>(a, r, bits, 0, (C + 31) / 32, l, id, t);
+  const float zk = id >= 0 ? T::get(zr + id) : kNegInf, z_label = has_y ? T::get(zr + y) : 0.f;
+  float m_rest = kNegInf;
+  const int n = again(C);
 #pragma unroll
-  for (int o = 32; o > 0; o >>= 1) loss += __shfl_xor(loss, o, 64);
-  if (lane == 0) wave_loss[wave] = loss;
-  __syncthreads();
+  for (int i = 0; i < kVecs; ++i) {
+    const int c0 = (k + kThreads * i) * T::E;
+    float x[T::E];
+    T::unpack(raw[i], x);
+    drop_listed<T>(x, (c0 < n ? bits[c0 / 32] : 0u) >> (c0 % 32), n - c0);
+#pragma unroll
+    for (int e = 0; e < T::E; ++e) m_rest = fmaxf(m_rest, x[e]);
+    raw[i] = T::pack(x);                           // exact: values that were read, or -inf
+    __builtin_amdgcn_sched_barrier(0);
+  }
+  auto sum = [&](float base, float scale) { return vectors_sum<T>(raw, base, scale); };
+  const RowStats st = block_stats<kThreads>(a, r, l, t, zk, m_rest, inv_t, sum, [&](float base) { return sum(base, kLog2e); });
+  const float soft = st.soft ? a.soft_scale * inv_t : 0.f, hard = has_y ? a.hard_scale : 0.f;
+  const RestGrad grad(a, st, soft, hard, inv_t);
+  store_vectors<T, kThreads>(raw, grad, jr, 0, again(C), y, hard);
+  float loss = 0.f, g = 0.f;
+  if (id >= 0) g = listed_term(st, t, zk, inv_t, soft, hard, a.soft_scale, loss) - (id == y ? hard : 0.f);
+  if (wave < 4) {
+    loss = lanes_sum<64>(loss);
+    if (lane == 0) l.loss[wave] = loss;
+  }
+  __syncthreads();                                 // the vectors' stores come before the listed ones
+  if (id >= 0) T::put(jr + id, g);
   if (k == 0) {
-    loss = wave_loss[0] + wave_loss[1] + wave_loss[2] + wave_loss[3];
-    if (st.soft) loss += a.soft_scale * kl_term(st.rho, st.log_rho, st.log_s);
-    if (has_y) loss += hs * (st.m + st.log_hard - T::get(z + y));
-    if (bad || (y != -1 && !has_y)) loss = __builtin_nanf("");  // an id out of range poisons the loss
-    row_loss[r] = loss;
+    const float listed = (l.loss[0] + l.loss[1]) + (l.loss[2] + l.loss[3]);
+    part[r] = (double)row_loss(st, listed, z_label, has_y, l.bad || (y != -1 && !has_y), a.soft_scale, hard);
   }
 }
 
-// Sum of the rows' losses in a fixed order, fp64.
-__global__ __launch_bounds__(1024) void distill_sum_kernel(const float *row_loss, int64_t rows, float *out) {
-  __shared__ double part[1024];
-  double s = 0.0;
-  for (int64_t r = threadIdx.x; r < rows; r += 1024) s += (double)row_loss[r];
-  part[threadIdx.x] = s;
+// ---- parts of a row: few rows, and rows too long for a workgroup ----------------------------
+//
+// A first launch leaves every part's maximum and sums, a second one joins a row's parts in each
+// of its workgroups and writes the part's gradient.
+
+constexpr int kPartThreads = 256, kPartVecs = 4;
+
+// The part's own vectors without its listed classes, and slot threadIdx.x of the row.
+template <class T>
+__device__ __forceinline__ float load_part(const pgcn_distill_args &a, int64_t r, int first, uint32_t *bits, ListLds<kPartThreads> &l,
+                                           typename T::raw (&raw)[kPartVecs], int &id, float &t) {
+  constexpr int kRange = kPartThreads * kPartVecs * T::E;
+  const typename T::type *zr = (const typename T::type *)a.Z + r * a.ld;
+#pragma unroll
+  for (int i = 0; i < kPartVecs; ++i) {
+    const int c0 = first + ((int)threadIdx.x + kPartThreads * i) * T::E;
+    raw[i] = c0 < a.classes ? *reinterpret_cast<const typename T::raw *>(zr + c0) : typename T::raw{};
+  }
+  list_classes<kPartThreads>(a, r, bits, first, kRange / 32, l, id, t);
+  float m = kNegInf;
+  const int n = again(a.classes - first);
+#pragma unroll
+  for (int i = 0; i < kPartVecs; ++i) {
+    const int c = ((int)threadIdx.x + kPartThreads * i) * T::E;
+    float x[T::E];
+    T::unpack(raw[i], x);
+    drop_listed<T>(x, bits[c / 32] >> (c % 32), n - c);
+#pragma unroll
+    for (int e = 0; e < T::E; ++e) m = fmaxf(m, x[e]);
+    raw[i] = T::pack(x);
+  }
+  return m;
+}
+
+// sums[row][part] = maximum, sum of e^{(z - m) / T}, sum of e^{z - m}
+template <class T>
+__global__ __launch_bounds__(kPartThreads) void distill_part_sums_kernel(pgcn_distill_args a, int parts, float4 *sums) {
+  constexpr int kRange = kPartThreads * kPartVecs * T::E;
+  __shared__ uint32_t bits[kRange / 32];
+  __shared__ ListLds<kPartThreads> l;
+  const int64_t r = blockIdx.x / parts;
+  const int part = (int)(blockIdx.x - r * parts), lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+  typename T::raw raw[kPartVecs];
+  int id;
+  float t;
+  float m = lanes_max<64>(load_part<T>(a, r, part * kRange, bits, l, raw, id, t));
+  if (lane == 0) l.m_rest[wave] = m;
   __syncthreads();
-  for (int w = 512; w > 0; w >>= 1) {
-    if ((int)threadIdx.x < w) part[threadIdx.x] += part[threadIdx.x + w];
-    __syncthreads();
+  m = fmaxf(fmaxf(l.m_rest[0], l.m_rest[1]), fmaxf(l.m_rest[2], l.m_rest[3]));
+  const bool two = a.labels && a.temperature != 1.0f;
+  const float s = lanes_sum<64>(vectors_sum<T>(raw, base_of(m), kLog2e / a.temperature));
+  const float h = two ? lanes_sum<64>(vectors_sum<T>(raw, base_of(m), kLog2e)) : 0.f;
+  if (lane == 0) {
+    l.s_rest[wave] = s;
+    l.s_hard[wave] = h;
   }
-  if (threadIdx.x == 0) *out = (float)part[0];
+  __syncthreads();
+  if (threadIdx.x == 0)
+    sums[blockIdx.x] = make_float4(m, (l.s_rest[0] + l.s_rest[1]) + (l.s_rest[2] + l.s_rest[3]),
+                                   (l.s_hard[0] + l.s_hard[1]) + (l.s_hard[2] + l.s_hard[3]), 0.f);
 }
 
-}  // namespace
+template <class T>
+__global__ __launch_bounds__(kPartThreads) void distill_part_grad_kernel(pgcn_distill_args a, int parts, const float4 *sums,
+                                                                         double *losses) {
+  constexpr int kRange = kPartThreads * kPartVecs * T::E;
+  __shared__ uint32_t bits[kRange / 32];
+  __shared__ ListLds<kPartThreads> l;
+  const int64_t r = blockIdx.x / parts;
+  const int part = (int)(blockIdx.x - r * parts), first = part * kRange, C = a.classes, k = threadIdx.x, lane = k % 64, wave = k / 64;
+  const typename T::type *zr = (const typename T::type *)a.Z + r * a.ld;
+  typename T::type *jr = (typename T::type *)a.J + r * a.ld;
+  const float inv_t = 1.0f / a.temperature;
+  const float4 p = k < parts ? sums[r * parts + k] : make_float4(kNegInf, 0.f, 0.f, 0.f);       // at most 64 parts
+  const int y = a.labels ? a.labels[r] : -1;
+  const bool has_y = y >= 0 && y < C;
+  typename T::raw raw[kPartVecs];
+  int id;
+  float t;
+  load_part<T>(a, r, first, bits, l, raw, id, t);
+  const float zk = id >= 0 ? T::get(zr + id) : kNegInf, z_label = has_y ? T::get(zr + y) : 0.f;
+  const RowStats st = block_stats<kPartThreads>(a, r, l, t, zk, p.x, inv_t,
+                                                [&](float base, float scale) { return p.y == 0.f ? 0.f : p.y * exp_at(p.x, base, scale); },
+                                                [&](float base) { return p.z == 0.f ? 0.f : p.z * exp_at(p.x, base, kLog2e); });
+  const float soft = st.soft ? a.soft_scale * inv_t : 0.f, hard = has_y ? a.hard_scale : 0.f;
+  const RestGrad grad(a, st, soft, hard, inv_t);
+  store_vectors<T, kPartThreads>(raw, grad, jr, first, again(C), y, hard);
+  float loss = 0.f, g = 0.f;
+  if (id >= 0) g = listed_term(st, t, zk, inv_t, soft, hard, a.soft_scale, loss) - (id == y ? hard : 0.f);
+  loss = lanes_sum<64>(loss);
+  if (lane == 0) l.loss[wave] = loss;
+  __syncthreads();                                 // the vectors' stores come before the listed ones
+  if (id >= first && id < first + kRange) T::put(jr + id, g);
+  if (part == 0 && k == 0) {
+    const float listed = (l.loss[0] + l.loss[1]) + (l.loss[2] + l.loss[3]);
+    losses[r] = (double)row_loss(st, listed, z_label, has_y, l.bad || (y != -1 && !has_y), a.soft_scale, hard);
+  }
+}
 
-size_t top_logits_workspace(int32_t, int64_t, int32_t, int32_t) { return 0; }
+// Sum of the parts in a fixed order.
+__global__ __launch_bounds__(1024) void distill_sum_kernel(const double *part, int64_t n, float *out) {
+  __shared__ double red[16];
+  double s = 0.0;
+#pragma unroll 4
+  for (int64_t i = threadIdx.x; i < n; i += 1024) s += part[i];
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o, 64);
+  if (threadIdx.x % 64 == 0) red[threadIdx.x / 64] = s;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    for (int i = 1; i < 16; ++i) s += red[i];
+    *out = (float)s;
+  }
+}
 
-int launch_top_logits(const pgcn_top_logits_args &a, hipStream_t s) {
-  if (a.rows == 0) return PGCN_OK;
-  TraceScope ts(PGCN_TK_TOP_LOGITS, s);
-  if (a.dtype == PGCN_BF16)
-    hipLaunchKernelGGL(top_rows_kernel<BF16>, dim3((unsigned)a.rows), dim3(256), 0, s, a);
+constexpr int kShortBlocks = 2048;
+
+// Lanes and vectors of a short row: the fewest lanes that hold it in one vector each, up to a wave.
+void short_row(int vecs, int &lanes, int &per) {
+  lanes = 8;
+  while (lanes < 64 && lanes < vecs) lanes *= 2;
+  per = 1;
+  while (lanes * per < vecs) per *= 2;
+}
+
+constexpr int kShortClasses = 2048;
+
+int vector_elems(int32_t dtype) { return dtype == PGCN_BF16 ? BF16::E : F32::E; }
+
+unsigned short_blocks(int64_t rows, int lanes) {
+  const int64_t n = 256 / lanes;
+  return (unsigned)std::min<int64_t>((rows + n - 1) / n, kShortBlocks);
+}
+
+template <class T, int kLanes, int kVecs>
+int short_go(const pgcn_distill_args &a, hipStream_t s) {
+  const unsigned blocks = short_blocks(a.rows, kLanes);
+  double *part = (double *)a.workspace;
+  const int slots = (a.top + kLanes - 1) / kLanes;
+  if (slots == 1)
+    hipLaunchKernelGGL((distill_short_kernel<T, kLanes, kVecs, 1>), dim3(blocks), dim3(256), 0, s, a, part);
+  else if (slots == 2)
+    hipLaunchKernelGGL((distill_short_kernel<T, kLanes, kVecs, 2>), dim3(blocks), dim3(256), 0, s, a, part);
   else
-    hipLaunchKernelGGL(top_rows_kernel<F32>, dim3((unsigned)a.rows), dim3(256), 0, s, a);
+    hipLaunchKernelGGL((distill_short_kernel<T, kLanes, kVecs, 8>), dim3(blocks), dim3(256), 0, s, a, part);
+  PGCN_HIP(hipGetLastError());
+  if (blocks == 1) return PGCN_OK;
+  hipLaunchKernelGGL(distill_sum_kernel, dim3(1), dim3(1024), 0, s, part, (int64_t)blocks, a.loss_out);
   PGCN_HIP(hipGetLastError());
   return PGCN_OK;
 }
 
-size_t distill_workspace(int32_t, int64_t rows, int32_t, int32_t) { return (size_t)rows * sizeof(float); }
+template <class T, int kThreads, int kVecs>
+int long_go(const pgcn_distill_args &a, hipStream_t s) {
+  double *part = (double *)a.workspace;
+  const size_t lds = (size_t)((a.classes + 31) / 32) * 4;
+  hipLaunchKernelGGL((distill_long_kernel<T, kThreads, kVecs>), dim3((unsigned)a.rows), dim3(kThreads), lds, s, a, part);
+  PGCN_HIP(hipGetLastError());
+  hipLaunchKernelGGL(distill_sum_kernel, dim3(1), dim3(1024), 0, s, part, a.rows, a.loss_out);
+  PGCN_HIP(hipGetLastError());
+  return PGCN_OK;
+}
+
+// Parts of a row, 0: whole rows.  A row that no workgroup's registers hold goes in parts, and so do
+// rows too few to fill the chip.
+int row_parts(int32_t dtype, int64_t rows, int32_t classes) {
+  const int64_t range = kPartThreads * kPartVecs * vector_elems(dtype), parts = (classes + range - 1) / range;
+  if (classes <= kShortClasses) return 0;
+  if (classes > 1024 * 16 * vector_elems(dtype) || (rows <= 128 && parts >= 4)) return (int)parts;
+  return 0;
+}
+
+template <class T>
+int parts_go(const pgcn_distill_args &a, int parts, hipStream_t s) {
+  double *losses = (double *)a.workspace;
+  float4 *sums = (float4 *)((char *)a.workspace + align_up((size_t)a.rows * sizeof(double), 16));
+  const dim3 grid((unsigned)(a.rows * parts));
+  hipLaunchKernelGGL(distill_part_sums_kernel<T>, grid, dim3(kPartThreads), 0, s, a, parts, sums);
+  PGCN_HIP(hipGetLastError());
+  hipLaunchKernelGGL(distill_part_grad_kernel<T>, grid, dim3(kPartThreads), 0, s, a, parts, sums, losses);
+  PGCN_HIP(hipGetLastError());
+  hipLaunchKernelGGL(distill_sum_kernel, dim3(1), dim3(1024), 0, s, losses, a.rows, a.loss_out);
+  PGCN_HIP(hipGetLastError());
+  return PGCN_OK;
+}
+
+template <class T>
+int distill_go(const pgcn_distill_args &a, hipStream_t s) {
+  const int vecs = (a.classes + T::E - 1) / T::E;
+  if (a.classes <= kShortClasses) {
+    int lanes, per;
+    short_row(vecs, lanes, per);
+    switch (lanes * 10 + per) {
+      case 81: return short_go<T, 8, 1>(a, s);
+      case 161: return short_go<T, 16, 1>(a, s);
+      case 321: return short_go<T, 32, 1>(a, s);
+      case 641: return short_go<T, 64, 1>(a, s);
+      case 642: return short_go<T, 64, 2>(a, s);
+      case 644: return short_go<T, 64, 4>(a, s);
+      default: return short_go<T, 64, T::E == 4 ? 8 : 4>(a, s);
+    }
+  }
+  const int parts = row_parts(a.dtype, a.rows, a.classes);
+  if (parts) return parts_go<T>(a, parts, s);
+  if (vecs <= 256 * 4) return long_go<T, 256, 4>(a, s);
+  if (vecs <= 256 * 8) return long_go<T, 256, 8>(a, s);
+  if (vecs <= 512 * 8) return long_go<T, 512, 8>(a, s);
+  if (vecs <= 1024 * 8) return long_go<T, 1024, 8>(a, s);
+  return long_go<T, 1024, 16>(a, s);
+}
+
+}  // namespace
+
+size_t distill_workspace(int32_t dtype, int64_t rows, int32_t classes, int32_t) {
+  if (classes > kShortClasses)
+    return align_up((size_t)rows * sizeof(double), 16) + (size_t)rows * row_parts(dtype, rows, classes) * sizeof(float4);
+  int lanes, per;
+  short_row((classes + vector_elems(dtype) - 1) / vector_elems(dtype), lanes, per);
+  return short_blocks(rows, lanes) * sizeof(double);
+}
 
 int launch_distill(const pgcn_distill_args &a, hipStream_t s) {
   TraceScope ts(PGCN_TK_DISTILL, s);
-  float *row_loss = (float *)a.workspace;
-  if (a.rows > 0) {
-    const size_t lds = (size_t)((a.classes + 31) / 32) * 4;
-    if (a.dtype == PGCN_BF16)
-      hipLaunchKernelGGL(distill_rows_kernel<BF16>, dim3((unsigned)a.rows), dim3(256), lds, s, a, row_loss);
-    else
-      hipLaunchKernelGGL(distill_rows_kernel<F32>, dim3((unsigned)a.rows), dim3(256), lds, s, a, row_loss);
-    PGCN_HIP(hipGetLastError());
-  }
-  hipLaunchKernelGGL(distill_sum_kernel, dim3(1), dim3(1024), 0, s, row_loss, a.rows, a.loss_out);
+  if (a.rows > 0) return a.dtype == PGCN_BF16 ? distill_go<BF16>(a, s) : distill_go<F32>(a, s);
+  hipLaunchKernelGGL(distill_sum_kernel, dim3(1), dim3(1024), 0, s, (const double *)nullptr, (int64_t)0, a.loss_out);
   PGCN_HIP(hipGetLastError());
   return PGCN_OK;
 }

@@ -71,6 +71,69 @@ __device__ __forceinline__ void store_some(typename T::type *p, const float (&v)
       if (e < n) T::put(p + e, v[e]);
   }
 }
+
+// ---- log-sums ---------------------------------------------------------------
+
+constexpr float kNegInf = -INFINITY;
+
+// sum of e^{(x - m) a} over some x, with m their maximum (s == 0: none but -inf seen)
+struct LogSum {
+  float m, s;
+};
+constexpr LogSum kNothing = {kNegInf, 0.f};
+
+__device__ __forceinline__ float exp_diff(float x, float m, float a) { return x == kNegInf ? 0.f : __expf((x - m) * a); }
+
+// A NaN leaves m and makes s NaN.
+__device__ __forceinline__ void add(LogSum &l, float x, float a) {
+  if (x == kNegInf) return;
+  const float m = fmaxf(l.m, x);
+  l.s = l.s * exp_diff(l.m, m, a) + __expf((x - m) * a);
+  l.m = m;
+}
+
+__device__ __forceinline__ LogSum merge(const LogSum &x, const LogSum &y, float a) {
+  LogSum r;
+  r.m = fmaxf(x.m, y.m);
+  r.s = x.s * exp_diff(x.m, r.m, a) + y.s * exp_diff(y.m, r.m, a);
+  return r;
+}
+
+// ---- sums and maxima over neighbouring lanes --------------------------------
+//
+// kLanes (a power of two up to 64) lanes each get the result: the first four steps are register
+// moves within rows of 16 lanes (exchange in pairs, in quads, mirrored halves, mirrored row), the
+// rest shuffles.  Every lane adds the same pairs, so all hold the same bits.
+template <int kCtrl>
+__device__ __forceinline__ float lane_move(float v) {
+  return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), kCtrl, 0xf, 0xf, true));
+}
+
+template <int kLanes, class Op>
+__device__ __forceinline__ float lanes_all(float v, Op op) {
+  if (kLanes >= 2) v = op(v, lane_move<0xB1>(v));
+  if (kLanes >= 4) v = op(v, lane_move<0x4E>(v));
+  if (kLanes >= 8) v = op(v, lane_move<0x141>(v));
+  if (kLanes >= 16) v = op(v, lane_move<0x140>(v));
+  if (kLanes >= 32) v = op(v, __shfl_xor(v, 16, 64));
+  if (kLanes >= 64) v = op(v, __shfl_xor(v, 32, 64));
+  return v;
+}
+
+template <int kLanes>
+__device__ __forceinline__ float lanes_max(float v) {
+  return lanes_all<kLanes>(v, [](float a, float b) { return fmaxf(a, b); });
+}
+template <int kLanes>
+__device__ __forceinline__ float lanes_sum(float v) {
+  return lanes_all<kLanes>(v, [](float a, float b) { return a + b; });
+}
+
+// Orders the LDS accesses of a wave's lanes (they are executed in order; this keeps the compiler from moving them).
+__device__ __forceinline__ void wave_sync() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
 #endif
 
 }  // namespace pgcn

@@ -259,7 +259,7 @@ def test_distill_sizes(rows, C, K, dtype):
 
 @pytest.mark.parametrize("rows,C,K", [(40, 41, 8), (12, 300, 60), (3, 5000, 64), (2, 70000, 40)])
 @pytest.mark.parametrize("kind", ["masked", "sure", "far", "all_absent", "repeats", "inf_slots", "offset", "label_in_list", "lowest",
-                                  "covers_all"])
+                                  "covers_all", "far_below", "only_listed"])
 def test_distill_masks_and_lists(rows, C, K, kind):
     rng = np.random.default_rng(C + K)
     z, T = logits(rng, rows, C).astype(np.float32).astype(np.float64), 1.3
@@ -294,6 +294,16 @@ def test_distill_masks_and_lists(rows, C, K, kind):
         z[1, :] = float(np.finfo(np.float32).min)
         y = np.where(y >= C // 2, 0, y)
         i = np.where(i >= C // 2, -1, i)
+    elif kind == "far_below":               # exponentials of the logits themselves all underflow
+        z, v, tail = z - 400.0, v - 400.0, tail - 400.0 / T
+        z[0, :C // 2] -= 300.0
+    elif kind == "only_listed":             # ... and nothing but -inf is left outside the list
+        low = np.full_like(z, NINF)
+        for r in range(rows):
+            on = i[r][i[r] >= 0] if (i[r] >= 0).any() else [0, 1]
+            low[r, on] = z[r, on] - 400.0
+            y[r] = on[0]
+        z, T, tail = low, 1.0, np.full(rows, NINF)
     elif kind == "covers_all" and C <= 300:
         v, i, tail = teacher(rng, z, min(C, 256), T, none=0.2)
     Z = matrix(z, "f32")
