@@ -42,15 +42,15 @@ struct RowStats {
   bool some;              // there is an unlisted logit above -inf
 };
 
-__device__ __forceinline__ RowStats row_stats(const LogSum &rest, const LogSum &top, const LogSum &teacher, float hard, float m,
-                                              const float *tail_lse, int64_t r, float inv_t) {
+// `two`: `hard` is the sum of e^{z - m}; else the temperature is 1 (or no row has a label) and the soft sum is it.
+__device__ __forceinline__ RowStats row_stats(const LogSum &rest, const LogSum &top, const LogSum &teacher, bool two, float hard, float m,
+                                              float tail, float inv_t) {
   RowStats st;
   const LogSum all = merge(rest, top, inv_t);
   st.m = m;
   st.log_all = __logf(all.s);
   st.soft = teacher.s != 0.f;                      // NaN counts: it has to show
   st.mt = base_of(teacher.m);
-  const float tail = tail_lse ? tail_lse[r] : kNegInf;
   if (tail != kNegInf) {
     const float b = tail - st.mt * inv_t;          // e^b beside the listed ones' sum
     const float big = fmaxf(b, 0.f);
@@ -65,9 +65,9 @@ __device__ __forceinline__ RowStats row_stats(const LogSum &rest, const LogSum &
   st.m_rest = base_of(rest.m);
   st.some = rest.s != 0.f;
   st.log_s = st.some ? (rest.m - all.m) * inv_t + __logf(rest.s) - st.log_all : kNegInf;
-  st.gain = st.some ? (__expf(st.log_s) - st.rho) / rest.s : 0.f;
-  st.log_hard = __logf(hard);
-  st.inv_hard = 1.0f / hard;
+  st.gain = st.some ? (__expf(st.log_s) - st.rho) * __builtin_amdgcn_rcpf(rest.s) : 0.f;
+  st.log_hard = two ? __logf(hard) : st.log_all;
+  st.inv_hard = __builtin_amdgcn_rcpf(two ? hard : all.s);
   return st;
 }
 
@@ -100,23 +100,25 @@ __device__ __forceinline__ float row_loss(const RowStats &st, float listed, floa
 
 // ---- short rows: kLanes lanes of a wave hold a row, kVecs vectors each ---------------------
 //
-// The row's image in LDS serves the listed classes, kSlots to a lane: their logits are read
-// from it, and their gradients written into it for the lane that holds the class.  mark[c] is
-// the lowest slot that lists c (an integer minimum, so its order does not matter).
-
-constexpr int kUnlisted = 0x7fffffff;
+// What a row costs besides its elements (reductions, logarithms) is spent by every lane, so few
+// lanes take a row: about 16 elements each, down to 4 lanes.  The row's image in LDS serves the
+// listed classes, kSlots to a lane: their logits are read from it, and their gradients written
+// into it for the lane that holds the class.
 
 template <class T, int kLanes, int kVecs, int kSlots>
 __global__ __launch_bounds__(256) void distill_short_kernel(pgcn_distill_args a, double *part) {
   constexpr int kWide = kLanes * kVecs * T::E, kRows = 256 / kLanes;
-  __shared__ __align__(16) float image_[kRows * kWide];
-  __shared__ __align__(16) int mark_[kRows * kWide];
+  constexpr int kStride = kWide + 4;               // neighbouring rows begin in other banks
+  constexpr int kWords = (kWide + 31) / 32;
+  __shared__ __align__(16) float image_[kRows * kStride];
+  __shared__ uint32_t bits_[kRows * kWords];
   __shared__ double sums[kRows];
   const int lane = threadIdx.x % kLanes, slot = threadIdx.x / kLanes, C = a.classes, K = a.top;
-  float *image = image_ + slot * kWide;
-  int *mark = mark_ + slot * kWide;
+  float *image = image_ + slot * kStride;
+  uint32_t *bits = bits_ + slot * kWords;
   const float inv_t = 1.0f / a.temperature, scale_t = inv_t * kLog2e;
   const bool same = a.temperature == 1.0f;         // the hard term's exponentials are the soft ones
+  const bool two = !same && a.labels;
   double total = 0.0;
 
   for (int64_t r = (int64_t)blockIdx.x * kRows + slot; r < a.rows; r += (int64_t)gridDim.x * kRows) {
@@ -137,10 +139,14 @@ __global__ __launch_bounds__(256) void distill_short_kernel(pgcn_distill_args a,
       t[i] = k < K ? a.top_values[r * a.ld_top + k] : kNegInf;
     }
     const int y = a.labels ? a.labels[r] : -1;
+    const float tail = a.tail_lse ? a.tail_lse[r] : kNegInf;
     const bool has_y = y >= 0 && y < C;
     bool bad = y != -1 && !has_y;
 
     wave_sync();                                   // the row before is done with its image
+#pragma unroll
+    for (int w = 0; w < kWords; w += kLanes)
+      if (w + lane < kWords) bits[w + lane] = 0;
 #pragma unroll
     for (int i = 0; i < kVecs; ++i) {
       const int c0 = (lane + kLanes * i) * T::E;
@@ -149,68 +155,83 @@ __global__ __launch_bounds__(256) void distill_short_kernel(pgcn_distill_args a,
       for (int e = 0; e < T::E; ++e) {
         if (c0 + e >= C) x[i][e] = kNegInf;
         image[c0 + e] = x[i][e];
-        mark[c0 + e] = kUnlisted;
       }
     }
     wave_sync();
+    bool twice = false;
 #pragma unroll
     for (int i = 0; i < kSlots; ++i) {
       if (id[i] >= C) {
         bad = true;
         id[i] = -1;
       }
-      if (id[i] >= 0) atomicMin(&mark[id[i]], lane + kLanes * i);
+      if (id[i] >= 0) twice |= (atomicOr(&bits[id[i] / 32], 1u << (id[i] % 32)) >> (id[i] % 32)) & 1u;
+    }
+    if (__any(twice)) {                            // of equal ids the lowest slot counts
+      int keep[kSlots];
+#pragma unroll
+      for (int i = 0; i < kSlots; ++i) keep[i] = id[i];
+      for (int o = 0; o < kLanes; ++o)
+#pragma unroll
+        for (int j = 0; j < kSlots; ++j) {
+          const int other = __shfl(id[j], o, kLanes);
+#pragma unroll
+          for (int i = 0; i < kSlots; ++i)
+            if (other == id[i] && o + kLanes * j < lane + kLanes * i) keep[i] = -1;
+        }
+#pragma unroll
+      for (int i = 0; i < kSlots; ++i) id[i] = keep[i];
     }
     wave_sync();
     float mt = kNegInf, m_top = kNegInf, m_rest = kNegInf;
 #pragma unroll
     for (int i = 0; i < kSlots; ++i) {
-      if (id[i] >= 0 && mark[id[i]] != lane + kLanes * i) id[i] = -1;       // listed before
       if (id[i] < 0) t[i] = kNegInf;
       zk[i] = id[i] >= 0 ? image[id[i]] : kNegInf;
       mt = fmaxf(mt, t[i]);
       m_top = fmaxf(m_top, zk[i]);
     }
     const float z_label = has_y ? image[y] : 0.f;
-    bool free_[kVecs][T::E];
 #pragma unroll
-    for (int i = 0; i < kVecs; ++i)
+    for (int i = 0; i < kVecs; ++i) {
+      const int c0 = (lane + kLanes * i) * T::E;
+      const uint32_t listed = bits[c0 / 32] >> (c0 % 32);
 #pragma unroll
       for (int e = 0; e < T::E; ++e) {
-        free_[i][e] = mark[(lane + kLanes * i) * T::E + e] == kUnlisted;
-        m_rest = fmaxf(m_rest, free_[i][e] ? x[i][e] : kNegInf);
+        x[i][e] = (listed >> e) & 1u ? kNegInf : x[i][e];
+        m_rest = fmaxf(m_rest, x[i][e]);
       }
+    }
     mt = lanes_max<kLanes>(mt);
     m_top = lanes_max<kLanes>(m_top);
     m_rest = lanes_max<kLanes>(m_rest);
     const float m = fmaxf(m_top, m_rest), bt = base_of(mt), b_top = base_of(m_top), b_rest = base_of(m_rest), b_all = base_of(m);
-    float st_ = 0.f, s_top = 0.f, s_rest = 0.f, s_hard = 0.f;
+    float s_t = 0.f, s_top = 0.f, s_rest = 0.f, s_hard = 0.f;
 #pragma unroll
     for (int i = 0; i < kSlots; ++i) {
-      st_ += exp_at(t[i], bt, scale_t);
+      s_t += exp_at(t[i], bt, scale_t);
       s_top += exp_at(zk[i], b_top, scale_t);
-      if (!same) s_hard += exp_at(zk[i], b_all, kLog2e);
+      if (two) s_hard += exp_at(zk[i], b_all, kLog2e);
     }
-    float h[kVecs][T::E];
+    if (two) {
+#pragma unroll
+      for (int i = 0; i < kVecs; ++i)
+#pragma unroll
+        for (int e = 0; e < T::E; ++e) s_hard += exp_at(x[i][e], b_all, kLog2e);
+    }
 #pragma unroll
     for (int i = 0; i < kVecs; ++i)
 #pragma unroll
       for (int e = 0; e < T::E; ++e) {
-        const float v = free_[i][e] ? x[i][e] : kNegInf;
-        x[i][e] = exp_at(v, b_rest, scale_t);
+        x[i][e] = exp_at(x[i][e], b_rest, scale_t);
         s_rest += x[i][e];
-        h[i][e] = 0.f;
-        if (!same && a.labels) {
-          h[i][e] = exp_at(v, b_all, kLog2e);
-          s_hard += h[i][e];
-        }
       }
-    st_ = lanes_sum<kLanes>(st_);
+    s_t = lanes_sum<kLanes>(s_t);
     s_top = lanes_sum<kLanes>(s_top);
     s_rest = lanes_sum<kLanes>(s_rest);
     const LogSum rest = {m_rest, s_rest}, top = {m_top, s_top};
-    s_hard = same ? merge(rest, top, 1.0f).s : lanes_sum<kLanes>(s_hard);
-    const RowStats st = row_stats(rest, top, LogSum{mt, st_}, s_hard, m, a.tail_lse, r, inv_t);
+    if (two) s_hard = lanes_sum<kLanes>(s_hard);
+    const RowStats st = row_stats(rest, top, LogSum{mt, s_t}, two, s_hard, m, tail, inv_t);
     const float soft = st.soft ? a.soft_scale * inv_t : 0.f, hard = has_y ? a.hard_scale : 0.f;
 
     float loss = 0.f;
@@ -222,23 +243,34 @@ __global__ __launch_bounds__(256) void distill_short_kernel(pgcn_distill_args a,
         loss += l;
       }
     loss = lanes_sum<kLanes>(loss);
-    float any_bad = lanes_max<kLanes>(bad ? 1.f : 0.f);
+    const float any_bad = lanes_max<kLanes>(bad ? 1.f : 0.f);
     wave_sync();
     // unlisted: soft e^{(z - m_rest) / T} gain + hard e^{z - m} / sum
-    const float gs = soft != 0.f ? soft * st.gain : 0.f;
     const float gh = hard != 0.f ? hard * st.inv_hard : 0.f;
-    const float g_one = same && gh != 0.f && st.some ? gs + gh * exp_at(b_rest, b_all, kLog2e) : gs;
+    float gs = soft != 0.f ? soft * st.gain : 0.f;
+    if (same && gh != 0.f && st.some) gs += gh * exp_at(b_rest, b_all, kLog2e);
+    if (has_y && lane == 0) {                      // the label's gradient goes by the image too
+      const uint32_t old = atomicOr(&bits[y / 32], 1u << (y % 32));
+      float g = image[y];
+      if (!((old >> (y % 32)) & 1u)) {
+        g = exp_at(z_label, b_rest, scale_t) * gs;
+        if (two) g += exp_at(z_label, b_all, kLog2e) * gh;
+      }
+      image[y] = g - hard;
+    }
+    wave_sync();
 #pragma unroll
     for (int i = 0; i < kVecs; ++i) {
       const int c0 = (lane + kLanes * i) * T::E;
       if (c0 >= C) continue;
+      const uint32_t given = bits[c0 / 32] >> (c0 % 32);
       float g[T::E];
 #pragma unroll
       for (int e = 0; e < T::E; ++e) {
-        float v = g_one != 0.f ? x[i][e] * g_one : 0.f;
-        if (!same && gh != 0.f) v += h[i][e] * gh;
-        if (!free_[i][e]) v = image[c0 + e];
-        g[e] = c0 + e == y ? v - hard : v;
+        const float im = image[c0 + e];
+        float v = x[i][e] * gs;
+        if (two) v += exp_at(im, b_all, kLog2e) * gh;
+        g[e] = (given >> e) & 1u ? im : v;
       }
       store_some<T>((typename T::type *)a.J + r * a.ld + c0, g, C - c0);
     }
@@ -328,7 +360,7 @@ __device__ __forceinline__ RowStats block_stats(const pgcn_distill_args &a, int6
   constexpr int kWaves = kThreads / 64;
   const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
   const float scale_t = inv_t * kLog2e;
-  const bool same = a.temperature == 1.0f;
+  const bool two = a.labels && a.temperature != 1.0f;      // the hard term has exponentials of its own
   m_rest = lanes_max<64>(m_rest);
   if (lane == 0) l.m_rest[wave] = m_rest;
   if (wave < 4) {
@@ -346,7 +378,7 @@ __device__ __forceinline__ RowStats block_stats(const pgcn_distill_args &a, int6
   const float m_t = fmaxf(fmaxf(l.m_t[0], l.m_t[1]), fmaxf(l.m_t[2], l.m_t[3]));
   const float m = fmaxf(m_rest, m_top), b_rest = base_of(m_rest), b_all = base_of(m);
   float s_rest = lanes_sum<64>(rest_sum(b_rest, scale_t));
-  float s_hard = a.labels && !same ? lanes_sum<64>(hard_sum(b_all)) : 0.f;
+  float s_hard = two ? lanes_sum<64>(hard_sum(b_all)) : 0.f;
   if (lane == 0) {
     l.s_rest[wave] = s_rest;
     l.s_hard[wave] = s_hard;
@@ -371,8 +403,7 @@ __device__ __forceinline__ RowStats block_stats(const pgcn_distill_args &a, int6
   const LogSum rest = {m_rest, s_rest}, top = {m_top, (l.s_top[0] + l.s_top[1]) + (l.s_top[2] + l.s_top[3])};
   const LogSum teacher = {m_t, (l.s_t[0] + l.s_t[1]) + (l.s_t[2] + l.s_t[3])};
   s_hard += (l.s_hard_top[0] + l.s_hard_top[1]) + (l.s_hard_top[2] + l.s_hard_top[3]);
-  if (same) s_hard = merge(rest, top, 1.0f).s;
-  return row_stats(rest, top, teacher, s_hard, m, a.tail_lse, r, inv_t);
+  return row_stats(rest, top, teacher, two, s_hard, m, a.tail_lse ? a.tail_lse[r] : kNegInf, inv_t);
 }
 
 // Keeps the packed vectors, and not what one pass over them computed, in registers for the next.
@@ -438,7 +469,7 @@ __device__ __forceinline__ void store_vectors(typename T::raw (&raw)[kVecs], con
 }
 
 template <class T, int kThreads, int kVecs>
-__global__ __launch_bounds__(kThreads, kThreads == 1024 && kVecs <= 8 ? 8 : 0) void distill_long_kernel(pgcn_distill_args a, double *part) {
+__global__ __launch_bounds__(kThreads, 4) void distill_long_kernel(pgcn_distill_args a, double *part) {
   extern __shared__ uint32_t bits[];
   __shared__ ListLds<kThreads> l;
   const int64_t r = blockIdx.x;
@@ -607,10 +638,10 @@ __global__ __launch_bounds__(1024) void distill_sum_kernel(const double *part, i
 
 constexpr int kShortBlocks = 2048;
 
-// Lanes and vectors of a short row: the fewest lanes that hold it in one vector each, up to a wave.
-void short_row(int vecs, int &lanes, int &per) {
-  lanes = 8;
-  while (lanes < 64 && lanes < vecs) lanes *= 2;
+// Lanes and vectors of a short row: 16 elements to a lane, 4 to 64 lanes, then more elements.
+void short_row(int elems, int vecs, int &lanes, int &per) {
+  lanes = 4;
+  while (lanes < 64 && lanes * 16 < vecs * elems) lanes *= 2;
   per = 1;
   while (lanes * per < vecs) per *= 2;
 }
@@ -629,12 +660,15 @@ int short_go(const pgcn_distill_args &a, hipStream_t s) {
   const unsigned blocks = short_blocks(a.rows, kLanes);
   double *part = (double *)a.workspace;
   const int slots = (a.top + kLanes - 1) / kLanes;
-  if (slots == 1)
+  constexpr int kMost = kLanes * kVecs * T::E / kLanes < PGCN_MAX_TOP / kLanes ? kVecs * T::E : PGCN_MAX_TOP / kLanes;
+  if (slots <= 1)
     hipLaunchKernelGGL((distill_short_kernel<T, kLanes, kVecs, 1>), dim3(blocks), dim3(256), 0, s, a, part);
-  else if (slots == 2)
+  else if (slots <= 2)
     hipLaunchKernelGGL((distill_short_kernel<T, kLanes, kVecs, 2>), dim3(blocks), dim3(256), 0, s, a, part);
+  else if (slots <= 4)
+    hipLaunchKernelGGL((distill_short_kernel<T, kLanes, kVecs, 4>), dim3(blocks), dim3(256), 0, s, a, part);
   else
-    hipLaunchKernelGGL((distill_short_kernel<T, kLanes, kVecs, 8>), dim3(blocks), dim3(256), 0, s, a, part);
+    hipLaunchKernelGGL((distill_short_kernel<T, kLanes, kVecs, kMost>), dim3(blocks), dim3(256), 0, s, a, part);
   PGCN_HIP(hipGetLastError());
   if (blocks == 1) return PGCN_OK;
   hipLaunchKernelGGL(distill_sum_kernel, dim3(1), dim3(1024), 0, s, part, (int64_t)blocks, a.loss_out);
@@ -681,23 +715,25 @@ int distill_go(const pgcn_distill_args &a, hipStream_t s) {
   const int vecs = (a.classes + T::E - 1) / T::E;
   if (a.classes <= kShortClasses) {
     int lanes, per;
-    short_row(vecs, lanes, per);
-    switch (lanes * 10 + per) {
-      case 81: return short_go<T, 8, 1>(a, s);
-      case 161: return short_go<T, 16, 1>(a, s);
-      case 321: return short_go<T, 32, 1>(a, s);
-      case 641: return short_go<T, 64, 1>(a, s);
-      case 642: return short_go<T, 64, 2>(a, s);
-      case 644: return short_go<T, 64, 4>(a, s);
-      default: return short_go<T, 64, T::E == 4 ? 8 : 4>(a, s);
+    short_row(T::E, vecs, lanes, per);
+    constexpr int k16 = 16 / T::E;                 // vectors of 16 elements
+    switch (lanes * 100 + per) {
+      case 401: return short_go<T, 4, 1>(a, s);
+      case 402: return short_go<T, 4, 2>(a, s);
+      case 404: return short_go<T, 4, k16>(a, s);
+      case 800 + k16: return short_go<T, 8, k16>(a, s);
+      case 1600 + k16: return short_go<T, 16, k16>(a, s);
+      case 3200 + k16: return short_go<T, 32, k16>(a, s);
+      case 6400 + k16: return short_go<T, 64, k16>(a, s);
+      default: return short_go<T, 64, 2 * k16>(a, s);
     }
   }
   const int parts = row_parts(a.dtype, a.rows, a.classes);
   if (parts) return parts_go<T>(a, parts, s);
   if (vecs <= 256 * 4) return long_go<T, 256, 4>(a, s);
   if (vecs <= 256 * 8) return long_go<T, 256, 8>(a, s);
-  if (vecs <= 512 * 8) return long_go<T, 512, 8>(a, s);
-  if (vecs <= 1024 * 8) return long_go<T, 1024, 8>(a, s);
+  if (vecs <= 256 * 16) return long_go<T, 256, 16>(a, s);
+  if (vecs <= 512 * 16) return long_go<T, 512, 16>(a, s);
   return long_go<T, 1024, 16>(a, s);
 }
 
@@ -707,7 +743,8 @@ size_t distill_workspace(int32_t dtype, int64_t rows, int32_t classes, int32_t) 
   if (classes > kShortClasses)
     return align_up((size_t)rows * sizeof(double), 16) + (size_t)rows * row_parts(dtype, rows, classes) * sizeof(float4);
   int lanes, per;
-  short_row((classes + vector_elems(dtype) - 1) / vector_elems(dtype), lanes, per);
+  const int e = vector_elems(dtype);
+  short_row(e, (classes + e - 1) / e, lanes, per);
   return short_blocks(rows, lanes) * sizeof(double);
 }
 
