@@ -557,7 +557,7 @@ typedef struct {
   int32_t dtype;               /* pgcn_dtype of Z                                */
   int32_t classes;             /* 1 .. PGCN_MAX_CLASSES                          */
   int32_t top;                 /* 1 .. min(classes, PGCN_MAX_TOP)                */
-  float temperature;           /* > 0, with a finite reciprocal                  */
+  float temperature;           /* 1e-4 .. 1e4                                    */
   int64_t rows;
   int64_t ld;                  /* stride of Z (elements)                         */
   int64_t ld_top;              /* stride of top_values and top_ids, >= top       */
@@ -589,7 +589,8 @@ int pgcn_top_logits(const pgcn_top_logits_args *args, hipStream_t stream);
  *     it is +inf where p > 0 and q = 0.
  *   - An id or label >= classes (a label < -1 too) makes the loss NaN; the id is otherwise
  *     ignored.  A row without any finite logit that has a soft or hard term makes it NaN.
- *   - A NaN among a row's logits or listed values makes the loss and the row's J NaN.
+ *   - A NaN among a row's logits makes the row's J NaN, and the loss if the row has a term; a NaN
+ *     among its listed values makes both NaN.
  * J: [rows, ld], the dtype and stride of Z.  loss_out: one device float, written (not
  * accumulated), reduced in a fixed order.
  */
@@ -597,7 +598,7 @@ typedef struct {
   int32_t dtype;               /* pgcn_dtype of Z and J                          */
   int32_t classes;             /* 1 .. PGCN_MAX_CLASSES                          */
   int32_t top;                 /* 1 .. min(classes, PGCN_MAX_TOP)                */
-  float temperature;           /* > 0, with a finite reciprocal                  */
+  float temperature;           /* 1e-4 .. 1e4                                    */
   int64_t rows;
   int64_t ld;                  /* stride of Z and J (elements)                   */
   int64_t ld_top;              /* stride of top_values and top_ids, >= top       */

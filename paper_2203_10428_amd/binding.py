@@ -348,18 +348,21 @@ def pgcn_refill_async(dst, src, nbytes: int, flags: int = 0, stream=None):
     _check(lib.pgcn_refill_async(_ptr(dst), _ptr(src), nbytes, flags, _stream(stream)), "pgcn_refill_async")
 
 
-def _same_device(*xs):
-    """Tensors of a call without a partition handle have to be on the current device (a pointer given as an
-    int is the caller's word)."""
-    cur = -1
+def _ptrs(*xs):
+    """Pointers of the buffers of a call without a partition handle, whose tensors have to be on the current
+    device (a pointer given as an int is the caller's word)."""
+    cur = None
+    out = []
     for x in xs:
         if isinstance(x, torch.Tensor):
-            if not x.is_cuda:
-                raise ValueError("a tensor of the call is not in device memory")
-            if cur < 0:
-                cur = torch.cuda.current_device()
-            if x.get_device() != cur:
-                raise ValueError("a tensor of the call is on another device than the current one")
+            if cur is None:
+                cur = torch.cuda.current_device() if x.is_cuda else -1
+            if cur < 0 or x.get_device() != cur:
+                raise ValueError("a tensor of the call is not in the current device's memory")
+            out.append(x.data_ptr())
+        else:
+            out.append(_ptr(x))
+    return out
 
 
 def pgcn_top_logits_workspace_size(dtype: int, rows: int, classes: int, top: int) -> int:
@@ -368,9 +371,8 @@ def pgcn_top_logits_workspace_size(dtype: int, rows: int, classes: int, top: int
 
 def pgcn_top_logits(*, dtype, rows, classes, ld, top, ld_top, temperature, Z, top_values, top_ids, tail_lse,
                     workspace=None, workspace_bytes=0, stream=None):
-    _same_device(Z, top_values, top_ids, tail_lse, workspace)
-    a = pgcn_top_logits_args(dtype, classes, top, temperature, rows, ld, ld_top, _ptr(Z), _ptr(top_values),
-                             _ptr(top_ids), _ptr(tail_lse), _ptr(workspace), workspace_bytes)
+    a = pgcn_top_logits_args(dtype, classes, top, temperature, rows, ld, ld_top,
+                             *_ptrs(Z, top_values, top_ids, tail_lse, workspace), workspace_bytes)
     _check(lib.pgcn_top_logits(C.byref(a), _stream(stream)), "pgcn_top_logits")
 
 
@@ -381,10 +383,8 @@ def pgcn_distill_workspace_size(dtype: int, rows: int, classes: int, top: int) -
 def pgcn_distill_loss_fwd_bwd(*, dtype, rows, classes, ld, top, ld_top, temperature, soft_scale, hard_scale, Z,
                               top_values, top_ids, tail_lse, labels, J, loss_out, workspace, workspace_bytes,
                               stream=None):
-    _same_device(Z, top_values, top_ids, tail_lse, labels, J, loss_out, workspace)
-    a = pgcn_distill_args(dtype, classes, top, temperature, rows, ld, ld_top, soft_scale, hard_scale, _ptr(Z),
-                          _ptr(top_values), _ptr(top_ids), _ptr(tail_lse), _ptr(labels), _ptr(J), _ptr(loss_out),
-                          _ptr(workspace), workspace_bytes)
+    a = pgcn_distill_args(dtype, classes, top, temperature, rows, ld, ld_top, soft_scale, hard_scale,
+                          *_ptrs(Z, top_values, top_ids, tail_lse, labels, J, loss_out, workspace), workspace_bytes)
     _check(lib.pgcn_distill_loss_fwd_bwd(C.byref(a), _stream(stream)), "pgcn_distill_loss_fwd_bwd")
 
 
@@ -394,20 +394,17 @@ def pgcn_group_norm_workspace_size(dtype: int, channels: int, groups: int, sampl
 
 def pgcn_group_norm_fwd(*, dtype, act, channels, groups, samples, sample_rows, ld_x, ld_y, eps, X, gamma, beta, Y,
                         mean, rstd, workspace=None, workspace_bytes=0, stream=None):
-    _same_device(X, gamma, beta, Y, mean, rstd, workspace)
-    a = pgcn_group_norm_fwd_args(dtype, act, channels, groups, samples, sample_rows, ld_x, ld_y, eps, _ptr(X),
-                                 _ptr(gamma), _ptr(beta), _ptr(Y), _ptr(mean), _ptr(rstd), _ptr(workspace),
-                                 workspace_bytes)
+    a = pgcn_group_norm_fwd_args(dtype, act, channels, groups, samples, sample_rows, ld_x, ld_y, eps,
+                                 *_ptrs(X, gamma, beta, Y, mean, rstd, workspace), workspace_bytes)
     _check(lib.pgcn_group_norm_fwd(C.byref(a), _stream(stream)), "pgcn_group_norm_fwd")
 
 
 def pgcn_group_norm_bwd(*, dtype, act, channels, groups, samples, sample_rows, ld_x, ld_j_out, ld_j_in, X, J_out,
                         gamma, beta, mean, rstd, J_in, dgamma, dbeta, workspace=None, workspace_bytes=0,
                         stream=None):
-    _same_device(X, J_out, gamma, beta, mean, rstd, J_in, dgamma, dbeta, workspace)
-    a = pgcn_group_norm_bwd_args(dtype, act, channels, groups, samples, sample_rows, ld_x, ld_j_out, ld_j_in, _ptr(X),
-                                 _ptr(J_out), _ptr(gamma), _ptr(beta), _ptr(mean), _ptr(rstd), _ptr(J_in),
-                                 _ptr(dgamma), _ptr(dbeta), _ptr(workspace), workspace_bytes)
+    a = pgcn_group_norm_bwd_args(dtype, act, channels, groups, samples, sample_rows, ld_x, ld_j_out, ld_j_in,
+                                 *_ptrs(X, J_out, gamma, beta, mean, rstd, J_in, dgamma, dbeta, workspace),
+                                 workspace_bytes)
     _check(lib.pgcn_group_norm_bwd(C.byref(a), _stream(stream)), "pgcn_group_norm_bwd")
 
 

@@ -338,10 +338,12 @@ __device__ __forceinline__ void list_classes(const pgcn_distill_args &a, int64_t
 // -inf for the elements whose bit is set, and from the n-th on.
 template <class T>
 __device__ __forceinline__ void drop_listed(float (&x)[T::E], uint32_t bits, int n) {
+  bits &= (1u << T::E) - 1;
   if (n < T::E) bits |= ~0u << (n > 0 ? n : 0);
+  if (bits)                                        // most vectors have none
 #pragma unroll
-  for (int e = 0; e < T::E; ++e)
-    if ((bits >> e) & 1u) x[e] = kNegInf;
+    for (int e = 0; e < T::E; ++e)
+      if ((bits >> e) & 1u) x[e] = kNegInf;
 }
 
 // The same value, unknown to the compiler: what follows from it is computed anew in each pass over
@@ -413,46 +415,68 @@ __device__ __forceinline__ void keep_packed(Raw (&raw)[kVecs]) {
   for (int i = 0; i < kVecs; ++i) asm volatile("" : "+v"(raw[i]));
 }
 
+// e^{(x - m) T'} for many x: one product-sum each, 2^{x scale - shift} fix, where fix takes up what
+// shift = m scale was rounded by.
+struct Exps {
+  float scale, shift, fix;
+  __device__ __forceinline__ Exps(float m, float scale_) {
+    // from 2^64 on (a row of the type's lowest value) neighbours are 2^40 apart: any scale that keeps
+    // the product finite gives the same 1 and 0
+    scale = fabsf(m) < 0x1p64f ? scale_ : 0x1p-30f;
+    shift = m * scale;
+    fix = __builtin_amdgcn_exp2f(-__builtin_fmaf(m, scale, -shift));
+  }
+  __device__ __forceinline__ float raw(float x) const { return __builtin_amdgcn_exp2f(__builtin_fmaf(x, scale, -shift)); }
+};
+
 template <class T, int kVecs>
 __device__ __forceinline__ float vectors_sum(typename T::raw (&raw)[kVecs], float base, float scale) {
   keep_packed(raw);
+  const Exps ex(base, scale);
   float s[2] = {0.f, 0.f};
 #pragma unroll
   for (int i = 0; i < kVecs; ++i) {
     float x[T::E];
     T::unpack(raw[i], x);
 #pragma unroll
-    for (int e = 0; e < T::E; ++e) s[e % 2] += exp_at(x[e], base, scale);
+    for (int e = 0; e < T::E; ++e) s[e % 2] += ex.raw(x[e]);
     if (kVecs > 4) __builtin_amdgcn_sched_barrier(0);
   }
-  return s[0] + s[1];
+  return (s[0] + s[1]) * ex.fix;
 }
 
-// Gradient of unlisted logits: one factor for each exponential.
+// Gradient of unlisted logits: soft e^{(z - m_rest) / T} gain + hard e^{z - m} / sum, a factor for
+// each exponential, a single one where the temperature is 1.
 struct RestGrad {
-  float soft, hard, b_rest, b_all, scale_t;
-  bool two;               // the hard term has exponentials of its own
-  __device__ __forceinline__ RestGrad(const pgcn_distill_args &a, const RowStats &st, float soft_, float hard_, float inv_t) {
+  Exps rest, all;
+  float soft, hard;
+  bool two;
+  __device__ __forceinline__ RestGrad(const pgcn_distill_args &a, const RowStats &st, float soft_, float hard_, float inv_t)
+      : rest(st.m_rest, inv_t * kLog2e), all(base_of(st.m), kLog2e) {
     const float gh = hard_ != 0.f ? hard_ * st.inv_hard : 0.f;
     soft = soft_ != 0.f ? soft_ * st.gain : 0.f;
-    b_rest = st.m_rest;
-    b_all = base_of(st.m);
-    scale_t = inv_t * kLog2e;
     two = a.temperature != 1.0f && gh != 0.f;
-    hard = two ? gh : 0.f;
-    if (!two && gh != 0.f && st.some) soft += gh * exp_at(b_rest, b_all, kLog2e);
+    hard = two ? gh * all.fix : 0.f;
+    if (!two && gh != 0.f && st.some) soft += gh * exp_at(st.m_rest, base_of(st.m), kLog2e);
+    soft *= rest.fix;
   }
-  __device__ __forceinline__ float operator()(float x) const {
-    float g = soft != 0.f ? exp_at(x, b_rest, scale_t) * soft : 0.f;
-    if (two) g += exp_at(x, b_all, kLog2e) * hard;
-    return g;
+  template <int N>
+  __device__ __forceinline__ void operator()(float (&x)[N]) const {
+    if (two) {
+#pragma unroll
+      for (int e = 0; e < N; ++e) x[e] = rest.raw(x[e]) * soft + all.raw(x[e]) * hard;
+    } else {
+#pragma unroll
+      for (int e = 0; e < N; ++e) x[e] = rest.raw(x[e]) * soft;
+    }
   }
+  __device__ __forceinline__ float one(float x) const { return rest.raw(x) * soft + (two ? all.raw(x) * hard : 0.f); }
 };
 
-// The gradient of a thread's vectors (from class `first` on), less `hard` at the label.
+// The gradient of a thread's vectors, from class `first` on.
 template <class T, int kThreads, int kVecs>
 __device__ __forceinline__ void store_vectors(typename T::raw (&raw)[kVecs], const RestGrad &grad, typename T::type *jr, int first,
-                                              int C, int y, float hard) {
+                                              int C) {
   keep_packed(raw);
 #pragma unroll
   for (int i = 0; i < kVecs; ++i) {
@@ -460,12 +484,21 @@ __device__ __forceinline__ void store_vectors(typename T::raw (&raw)[kVecs], con
     if (c0 < C) {
       float x[T::E];
       T::unpack(raw[i], x);
-#pragma unroll
-      for (int e = 0; e < T::E; ++e) x[e] = grad(x[e]) - (y - c0 == e ? hard : 0.f);
+      grad(x);
       store_some<T>(jr + c0, x, C - c0);
     }
     __builtin_amdgcn_sched_barrier(0);             // one vector at a time: their temporaries do not add up
   }
+}
+
+// What the vectors left out, once they are stored: the listed classes of [first, last), and the label
+// if no slot lists it (`bits` begin with class `first`).
+template <class T>
+__device__ __forceinline__ void store_listed(const RestGrad &grad, typename T::type *jr, int id, float g, int y, float z_label,
+                                             float hard, const uint32_t *bits, int first, int last) {
+  if (id >= first && id < last) T::put(jr + id, g);
+  if (threadIdx.x == 0 && hard != 0.f && y >= first && y < last && !((bits[(y - first) / 32] >> ((y - first) % 32)) & 1u))
+    T::put(jr + y, grad.one(z_label) - hard);
 }
 
 template <class T, int kThreads, int kVecs>
@@ -506,7 +539,7 @@ __global__ __launch_bounds__(kThreads, 4) void distill_long_kernel(pgcn_distill_
   const RowStats st = block_stats<kThreads>(a, r, l, t, zk, m_rest, inv_t, sum, [&](float base) { return sum(base, kLog2e); });
   const float soft = st.soft ? a.soft_scale * inv_t : 0.f, hard = has_y ? a.hard_scale : 0.f;
   const RestGrad grad(a, st, soft, hard, inv_t);
-  store_vectors<T, kThreads>(raw, grad, jr, 0, again(C), y, hard);
+  store_vectors<T, kThreads>(raw, grad, jr, 0, again(C));
   float loss = 0.f, g = 0.f;
   if (id >= 0) g = listed_term(st, t, zk, inv_t, soft, hard, a.soft_scale, loss) - (id == y ? hard : 0.f);
   if (wave < 4) {
@@ -514,7 +547,7 @@ __global__ __launch_bounds__(kThreads, 4) void distill_long_kernel(pgcn_distill_
     if (lane == 0) l.loss[wave] = loss;
   }
   __syncthreads();                                 // the vectors' stores come before the listed ones
-  if (id >= 0) T::put(jr + id, g);
+  store_listed<T>(grad, jr, id, g, y, z_label, hard, bits, 0, C);
   if (k == 0) {
     const float listed = (l.loss[0] + l.loss[1]) + (l.loss[2] + l.loss[3]);
     part[r] = (double)row_loss(st, listed, z_label, has_y, l.bad || (y != -1 && !has_y), a.soft_scale, hard);
@@ -562,7 +595,7 @@ __global__ __launch_bounds__(kPartThreads) void distill_part_sums_kernel(pgcn_di
   __shared__ uint32_t bits[kRange / 32];
   __shared__ ListLds<kPartThreads> l;
   const int64_t r = blockIdx.x / parts;
-  const int part = (int)(blockIdx.x - r * parts), lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+  const int part = (int)(blockIdx.x % parts), lane = threadIdx.x % 64, wave = threadIdx.x / 64;
   typename T::raw raw[kPartVecs];
   int id;
   float t;
@@ -590,7 +623,7 @@ __global__ __launch_bounds__(kPartThreads) void distill_part_grad_kernel(pgcn_di
   __shared__ uint32_t bits[kRange / 32];
   __shared__ ListLds<kPartThreads> l;
   const int64_t r = blockIdx.x / parts;
-  const int part = (int)(blockIdx.x - r * parts), first = part * kRange, C = a.classes, k = threadIdx.x, lane = k % 64, wave = k / 64;
+  const int part = (int)(blockIdx.x % parts), first = part * kRange, C = a.classes, k = threadIdx.x, lane = k % 64, wave = k / 64;
   const typename T::type *zr = (const typename T::type *)a.Z + r * a.ld;
   typename T::type *jr = (typename T::type *)a.J + r * a.ld;
   const float inv_t = 1.0f / a.temperature;
@@ -607,13 +640,13 @@ __global__ __launch_bounds__(kPartThreads) void distill_part_grad_kernel(pgcn_di
                                                 [&](float base) { return p.z == 0.f ? 0.f : p.z * exp_at(p.x, base, kLog2e); });
   const float soft = st.soft ? a.soft_scale * inv_t : 0.f, hard = has_y ? a.hard_scale : 0.f;
   const RestGrad grad(a, st, soft, hard, inv_t);
-  store_vectors<T, kPartThreads>(raw, grad, jr, first, again(C), y, hard);
+  store_vectors<T, kPartThreads>(raw, grad, jr, first, again(C));
   float loss = 0.f, g = 0.f;
   if (id >= 0) g = listed_term(st, t, zk, inv_t, soft, hard, a.soft_scale, loss) - (id == y ? hard : 0.f);
   loss = lanes_sum<64>(loss);
   if (lane == 0) l.loss[wave] = loss;
   __syncthreads();                                 // the vectors' stores come before the listed ones
-  if (id >= first && id < first + kRange) T::put(jr + id, g);
+  store_listed<T>(grad, jr, id, g, y, z_label, hard, bits, first, first + kRange);
   if (part == 0 && k == 0) {
     const float listed = (l.loss[0] + l.loss[1]) + (l.loss[2] + l.loss[3]);
     losses[r] = (double)row_loss(st, listed, z_label, has_y, l.bad || (y != -1 && !has_y), a.soft_scale, hard);
@@ -687,12 +720,14 @@ int long_go(const pgcn_distill_args &a, hipStream_t s) {
   return PGCN_OK;
 }
 
+constexpr int kLongVecs = 8192;                    // vectors of the longest row that a workgroup holds
+
 // Parts of a row, 0: whole rows.  A row that no workgroup's registers hold goes in parts, and so do
 // rows too few to fill the chip.
 int row_parts(int32_t dtype, int64_t rows, int32_t classes) {
   const int64_t range = kPartThreads * kPartVecs * vector_elems(dtype), parts = (classes + range - 1) / range;
   if (classes <= kShortClasses) return 0;
-  if (classes > 1024 * 16 * vector_elems(dtype) || (rows <= 128 && parts >= 4)) return (int)parts;
+  if (parts > kLongVecs / (kPartThreads * kPartVecs) || (rows <= 128 && parts >= 4)) return (int)parts;
   return 0;
 }
 
@@ -730,18 +765,27 @@ int distill_go(const pgcn_distill_args &a, hipStream_t s) {
   }
   const int parts = row_parts(a.dtype, a.rows, a.classes);
   if (parts) return parts_go<T>(a, parts, s);
-  if (vecs <= 256 * 4) return long_go<T, 256, 4>(a, s);
-  if (vecs <= 256 * 8) return long_go<T, 256, 8>(a, s);
-  if (vecs <= 256 * 16) return long_go<T, 256, 16>(a, s);
-  if (vecs <= 512 * 16) return long_go<T, 512, 16>(a, s);
-  return long_go<T, 1024, 16>(a, s);
+  if constexpr (T::E == 4) {                       // short rows end at 512 vectors
+    if (vecs <= 1024) return long_go<T, 256, 4>(a, s);
+    if (vecs <= 2048) return long_go<T, 256, 8>(a, s);
+    if (vecs <= 4096) return long_go<T, 256, 16>(a, s);
+    return long_go<T, 512, 16>(a, s);
+  } else {                                         // unpacked bf16 takes more registers: 8 vectors at most
+    if (vecs <= 512) return long_go<T, 256, 2>(a, s);
+    if (vecs <= 1024) return long_go<T, 256, 4>(a, s);
+    if (vecs <= 2048) return long_go<T, 256, 8>(a, s);
+    if (vecs <= 4096) return long_go<T, 512, 8>(a, s);
+    return long_go<T, 1024, 8>(a, s);
+  }
 }
 
 }  // namespace
 
 size_t distill_workspace(int32_t dtype, int64_t rows, int32_t classes, int32_t) {
-  if (classes > kShortClasses)
-    return align_up((size_t)rows * sizeof(double), 16) + (size_t)rows * row_parts(dtype, rows, classes) * sizeof(float4);
+  if (classes > kShortClasses) {
+    const size_t parts = (size_t)row_parts(dtype, rows, classes);
+    return align_up((size_t)rows * sizeof(double), 16) + parts * (size_t)rows * sizeof(float4);
+  }
   int lanes, per;
   const int e = vector_elems(dtype);
   short_row(e, (classes + e - 1) / e, lanes, per);

@@ -70,8 +70,7 @@ int check_top(int32_t dtype, int64_t rows, int32_t classes, int32_t top, int64_t
   PGCN_REQUIRE(top >= 1 && top <= PGCN_MAX_TOP && top <= classes, f + ": top must be in [1, min(classes, PGCN_MAX_TOP)]");
   PGCN_REQUIRE(stride_ok(dtype, ld, classes), f + ": ld must be >= classes and a multiple of 4 (fp32) or 8 (bf16)");
   PGCN_REQUIRE(ld_top >= top && ld_top <= (int64_t(1) << 40), f + ": ld_top must be >= top");
-  PGCN_REQUIRE(temperature > 0.f && std::isfinite(temperature) && std::isfinite(1.0f / temperature),
-               f + ": temperature must be positive and finite, and so its reciprocal");
+  PGCN_REQUIRE(temperature >= 1e-4f && temperature <= 1e4f, f + ": temperature must be in [1e-4, 1e4]");
   return PGCN_OK;
 }
 

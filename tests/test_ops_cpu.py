@@ -30,7 +30,7 @@ BWD = dict(NORM, ld_j_out=32, ld_j_in=32, J_out=at(6), J_in=at(7), dgamma=at(8),
 BAD_TOP = [dict(dtype=2), dict(rows=-1), dict(rows=1 << 31), dict(classes=0), dict(classes=B.PGCN_MAX_CLASSES + 1, ld=1 << 20),
            dict(top=0), dict(top=42), dict(classes=512, ld=512, top=257, ld_top=257), dict(ld=40), dict(ld=42),
            dict(dtype=B.PGCN_BF16, ld=44), dict(ld_top=7), dict(temperature=0.0), dict(temperature=-1.0),
-           dict(temperature=float("nan")), dict(temperature=float("inf")), dict(temperature=1e-45),
+           dict(temperature=float("nan")), dict(temperature=float("inf")), dict(temperature=1e-45), dict(temperature=0.9e-4), dict(temperature=1.1e4),
            dict(Z=None), dict(top_values=None), dict(top_ids=None), dict(Z=at(0) + 4), dict(top_values=at(0)),
            dict(tail_lse=at(1) + 8), dict(workspace=at(4) + 4)]
 BAD_DISTILL = BAD_TOP[:-3] + [dict(J=None), dict(J=at(6) + 8), dict(J=at(0)), dict(J=at(0) + 16), dict(loss_out=None),
@@ -104,7 +104,7 @@ def test_workspace_sizes_of_rejected_arguments_are_zero():
 
 def test_tensors_in_host_memory_are_refused():
     z = torch.zeros(10, 48)
-    with pytest.raises(ValueError, match="device memory"):
+    with pytest.raises(ValueError, match="current device"):
         B.pgcn_top_logits(**{**TOP, "Z": z})
 
 
