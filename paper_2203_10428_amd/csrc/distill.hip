@@ -408,13 +408,6 @@ __device__ __forceinline__ RowStats block_stats(const pgcn_distill_args &a, int6
   return row_stats(rest, top, teacher, two, s_hard, m, a.tail_lse ? a.tail_lse[r] : kNegInf, inv_t);
 }
 
-// Keeps the packed vectors, and not what one pass over them computed, in registers for the next.
-template <class Raw, int kVecs>
-__device__ __forceinline__ void keep_packed(Raw (&raw)[kVecs]) {
-#pragma unroll
-  for (int i = 0; i < kVecs; ++i) asm volatile("" : "+v"(raw[i]));
-}
-
 // e^{(x - m) T'} for many x: one product-sum each, 2^{x scale - shift} fix, where fix takes up what
 // shift = m scale was rounded by.
 struct Exps {

@@ -72,6 +72,13 @@ __device__ __forceinline__ void store_some(typename T::type *p, const float (&v)
   }
 }
 
+// Keeps the packed vectors, and not what one pass over them computed, in registers for the next.
+template <class Raw, int kVecs>
+__device__ __forceinline__ void keep_packed(Raw (&raw)[kVecs]) {
+#pragma unroll
+  for (int i = 0; i < kVecs; ++i) asm volatile("" : "+v"(raw[i]));
+}
+
 // ---- log-sums ---------------------------------------------------------------
 
 constexpr float kNegInf = -INFINITY;
