@@ -551,8 +551,8 @@ enum pgcn_act { PGCN_ACT_NONE = 0, PGCN_ACT_RELU = 1, PGCN_ACT_SILU = 2, PGCN_AC
  *     tail_lse[r] = log sum of e^{Z[r, c] / temperature} over the classes not listed
  * A logit of -inf marks a class that is no answer: it is never listed and adds nothing to
  * the tail.  Where a row has fewer than `top` others, the slots left hold -inf and -1; a
- * tail of nothing is -inf.  A NaN is never listed either; it, or an unlisted +inf, makes the row's
- * tail NaN.
+ * tail of nothing is -inf.  A NaN is never listed either and makes the row's tail NaN; an unlisted
+ * +inf makes it +inf or NaN.
  */
 typedef struct {
   int32_t dtype;               /* pgcn_dtype of Z                                */

@@ -43,6 +43,8 @@ def top_logits(Z: np.ndarray, top: int, temperature: float):
         rest = np.delete(z, chosen) / temperature
         if np.isnan(rest).any():
             tail[r] = np.nan
+        elif len(rest) and rest.max() == np.inf:
+            tail[r] = np.inf
         elif len(rest) and rest.max() > -np.inf:
             tail[r] = rest.max() + np.log(np.exp(rest - rest.max()).sum())
     return values, ids, tail

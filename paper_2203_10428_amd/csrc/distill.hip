@@ -22,10 +22,6 @@ namespace pgcn {
 
 namespace {
 
-constexpr float kLog2e = 1.44269504088896341f;
-
-// e^{(x - m) T'} with scale = T' log2 e; 0 for x = -inf (m finite)
-__device__ __forceinline__ float exp_at(float x, float m, float scale) { return __builtin_amdgcn_exp2f((x - m) * scale); }
 // a maximum to subtract: 0 where there was nothing but -inf
 __device__ __forceinline__ float base_of(float m) { return m == kNegInf ? 0.f : m; }
 
@@ -407,20 +403,6 @@ __device__ __forceinline__ RowStats block_stats(const pgcn_distill_args &a, int6
   s_hard += (l.s_hard_top[0] + l.s_hard_top[1]) + (l.s_hard_top[2] + l.s_hard_top[3]);
   return row_stats(rest, top, teacher, two, s_hard, m, a.tail_lse ? a.tail_lse[r] : kNegInf, inv_t);
 }
-
-// e^{(x - m) T'} for many x: one product-sum each, 2^{x scale - shift} fix, where fix takes up what
-// shift = m scale was rounded by.
-struct Exps {
-  float scale, shift, fix;
-  __device__ __forceinline__ Exps(float m, float scale_) {
-    // from 2^64 on (a row of the type's lowest value) neighbours are 2^40 apart: any scale that keeps
-    // the product finite gives the same 1 and 0
-    scale = fabsf(m) < 0x1p64f ? scale_ : 0x1p-30f;
-    shift = m * scale;
-    fix = __builtin_amdgcn_exp2f(-__builtin_fmaf(m, scale, -shift));
-  }
-  __device__ __forceinline__ float raw(float x) const { return __builtin_amdgcn_exp2f(__builtin_fmaf(x, scale, -shift)); }
-};
 
 template <class T, int kVecs>
 __device__ __forceinline__ float vectors_sum(typename T::raw (&raw)[kVecs], float base, float scale) {

@@ -106,6 +106,25 @@ __device__ __forceinline__ LogSum merge(const LogSum &x, const LogSum &y, float 
   return r;
 }
 
+constexpr float kLog2e = 1.44269504088896341f;
+
+// e^{(x - m) T'} with scale = T' log2 e; 0 for x = -inf (m finite)
+__device__ __forceinline__ float exp_at(float x, float m, float scale) { return __builtin_amdgcn_exp2f((x - m) * scale); }
+
+// e^{(x - m) T'} for many x: one product-sum each, 2^{x scale - shift} fix, where fix takes up what
+// shift = m scale was rounded by.
+struct Exps {
+  float scale, shift, fix;
+  __device__ __forceinline__ Exps(float m, float scale_) {
+    // from 2^64 on (a row of the type's lowest value) neighbours are 2^40 apart: any scale that keeps
+    // the product finite gives the same 1 and 0
+    scale = fabsf(m) < 0x1p64f ? scale_ : 0x1p-30f;
+    shift = m * scale;
+    fix = __builtin_amdgcn_exp2f(-__builtin_fmaf(m, scale, -shift));
+  }
+  __device__ __forceinline__ float raw(float x) const { return __builtin_amdgcn_exp2f(__builtin_fmaf(x, scale, -shift)); }
+};
+
 // ---- sums and maxima over neighbouring lanes --------------------------------
 //
 // kLanes (a power of two up to 64) lanes each get the result: the first four steps are register

@@ -4,9 +4,9 @@
 // one read of Z.  Three kernels:
 //   - many short rows: a thread walks a row and keeps its list in registers (top_lists_kernel);
 //   - longer rows: a wave or a workgroup holds a row in registers.  The list lies above a
-//     threshold that at least `top` elements reach: each wave's r-th largest lane maximum, r =
-//     top / waves, has r elements of that wave at or above it.  What reaches the smallest of
-//     them, little more than `top` elements, goes to LDS, where each is ranked by counting.
+//     threshold that at least `top` elements reach.  Each wave's r-th largest lane maximum, r =
+//     top / waves, is tried, and the largest taken that `top` lane maxima reach.  What reaches it,
+//     little more than `top` elements, goes to LDS, where each is ranked by counting.
 //     Where too many reach it (ties, sorted rows) the threshold is bisected, and among equal
 //     values the class;
 //   - few rows, and rows longer than that: parts of a row first, then the lists of its parts.
@@ -18,10 +18,6 @@
 namespace pgcn {
 
 namespace {
-
-constexpr float kLog2e = 1.44269504088896341f;
-
-__device__ __forceinline__ float exp_at(float x, float m, float scale) { return __builtin_amdgcn_exp2f((x - m) * scale); }
 
 // Order of (value, lowest class first) as whole numbers.
 __device__ __forceinline__ uint32_t order_of(float x) {
@@ -47,31 +43,32 @@ struct TopArgs {
   int tails;
 };
 
-constexpr int kCandidates = 512;
-
-// Elements of a row's registers: f(x, class) for each.
-template <class T, int kThreads, int kVecs, class F>
-__device__ __forceinline__ void each(typename T::raw (&raw)[kVecs], int lane, F f) {
-  keep_packed(raw);
-#pragma unroll
-  for (int i = 0; i < kVecs; ++i) {
+// f(x, class, true) for n elements read again from memory, by a unit's threads in the order of the
+// registers; f(., ., false) past the end, so that all lanes take the same turns.
+template <class T, int kThreads, class F>
+__device__ __forceinline__ void each_in_memory(const typename T::type *z, int n, int lane, F f) {
+#pragma unroll 1
+  for (int c0 = lane * T::E; c0 - lane * T::E < n; c0 += kThreads * T::E) {
+    const typename T::raw raw = c0 < n ? *reinterpret_cast<const typename T::raw *>(z + c0) : typename T::raw{};
     float x[T::E];
-    T::unpack(raw[i], x);
-    const int c0 = (lane + kThreads * i) * T::E;
+    T::unpack(raw, x);
 #pragma unroll
-    for (int e = 0; e < T::E; ++e) f(x[e], c0 + e);
-    __builtin_amdgcn_sched_barrier(0);             // one vector at a time: their temporaries do not add up
+    for (int e = 0; e < T::E; ++e) f(x[e], c0 + e, c0 + e < n);
   }
 }
 
+// Candidates of a wave, and of a unit's waves together.
+constexpr int wave_candidates(int waves) { return waves == 1 ? 128 : waves == 4 ? 192 : 64; }
+
 template <int kThreads>
 struct TopLds {
-  static constexpr int kWaves = kThreads / 64;
-  uint64_t list[kCandidates];
+  static constexpr int kWaves = kThreads / 64, kEach = wave_candidates(kWaves);
+  uint64_t found[kWaves > 1 ? kWaves * kEach : 1];     // by wave
+  uint64_t list[kWaves * kEach];                       // one after another
   float wave_f[2][kWaves];
-  int wave_n[2][kWaves];
-  int count;
-  uint64_t last, next;         // keys of rank top - 1 and top
+  int wave_n[2][kWaves], reach[kWaves][kWaves];
+  int count, ties;
+  uint64_t last;               // key of rank top - 1
 };
 
 template <int kThreads>
@@ -105,30 +102,20 @@ __device__ __forceinline__ float waves_all(float v, TopLds<kThreads> &l, int &tu
   return v;
 }
 
-// The r-th largest of a wave's 64 values (r <= 64).
-__device__ __forceinline__ float nth_of_wave(float v, int r) {
-  const int lane = threadIdx.x % 64;
-  if (r <= 8) {
-    float m = v;
-    for (int i = 0;; ++i) {
-      m = lanes_max<64>(v);
-      if (i == r - 1) return m;
-      const int first = __ffsll((unsigned long long)__ballot(v == m)) - 1;
-      if (lane == first) v = kNegInf;
-    }
+// A value that at least r of a wave's 64 reach and few more: their r-th largest, less at most 2^12
+// units in the last place.  -inf where fewer than r are above that.
+__device__ __forceinline__ float reached_by(float v, int r) {
+  uint32_t lo = order_of(kNegInf), hi = __builtin_amdgcn_readfirstlane(order_of(lanes_max<64>(v))) + 1;
+  for (int i = 0; i < 20 && hi - lo > 1; ++i) {
+    const uint32_t mid = lo + (hi - lo) / 2;
+    if (__popcll(__ballot(v >= value_of(mid))) >= r) lo = mid;
+    else hi = mid;
   }
-  int rank = 0;
-#pragma unroll 8
-  for (int j = 0; j < 64; ++j) {
-    const float o = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v), j));
-    rank += o > v || (o == v && j < lane) ? 1 : 0;
-  }
-  const int at = __ffsll((unsigned long long)__ballot(rank == r - 1)) - 1;
-  return __shfl(v, at, 64);
+  return value_of(lo);
 }
 
 template <class T, int kThreads, int kVecs>
-__global__ __launch_bounds__(kThreads < 256 ? 256 : kThreads) void top_unit_kernel(TopArgs a) {
+__global__ __launch_bounds__(kThreads < 256 ? 256 : kThreads, kVecs <= 2 ? 8 : kVecs == 4 ? 7 : T::E == 4 ? 7 : 5) void top_unit_kernel(TopArgs a) {
   constexpr int kUnits = kThreads < 256 ? 256 / kThreads : 1, kWaves = kThreads / 64;
   __shared__ TopLds<kThreads> lds[kUnits];
   const int lane = threadIdx.x % kThreads, slot = threadIdx.x / kThreads;
@@ -164,22 +151,83 @@ __global__ __launch_bounds__(kThreads < 256 ? 256 : kThreads) void top_unit_kern
 
   int turn = 0;
   const int r = (K + kWaves - 1) / kWaves;
-  float v = r <= 64 ? nth_of_wave(top, r) : kNegInf;
-  v = waves_all<kThreads>(v, l, turn, [](float x, float y) { return fminf(x, y); });
+  float v = reached_by(top, r);                    // r <= 64: see unit_threads
+  if (kWaves > 1) {
+    // every wave's value is a candidate: the largest that K lane maxima of the unit reach (all reach the smallest)
+    if (threadIdx.x % 64 == 0) l.wave_f[0][threadIdx.x / 64] = v;
+    __syncthreads();
+    int reach = 0;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+      const int k = __popcll(__ballot(top >= l.wave_f[0][w]));
+      reach = threadIdx.x % 64 == w ? k : reach;
+    }
+    if (threadIdx.x % 64 < kWaves) l.reach[threadIdx.x / 64][threadIdx.x % 64] = reach;
+    __syncthreads();
+    v = kNegInf;
+    if (threadIdx.x % 64 < kWaves) {
+      int k = 0;
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) k += l.reach[w][threadIdx.x % 64];
+      if (k >= K) v = l.wave_f[0][threadIdx.x % 64];
+    }
+    v = lanes_max<64>(v);
+  }
   v = fmaxf(v, -FLT_MAX);                          // x >= v: every x above -inf
-  auto count = [&](auto in) {
-    int n = 0;
-    each<T, kThreads>(raw, lane, [&](float x, int c) { n += __popcll(__ballot(in(x, c))); });
-    return waves_add<kThreads>(n, l, turn);
-  };
-  int n = count([&](float x, int) { return x >= v; });
-  float tie = v;                                   // in the list: x > tie, or x == tie and its class is at most `upto`
-  int upto = n_all;
-  if (n > kCandidates) {
-    float m = waves_all<kThreads>(lanes_max<64>(top), l, turn, [](float x, float y) { return fmaxf(x, y); });
+  const int most = K + (kWaves > 1 ? 128 : 32);    // candidates to rank
+  constexpr int kEach = TopLds<kThreads>::kEach;
+  const int wave = kWaves > 1 ? threadIdx.x / 64 : 0, wl = threadIdx.x % 64;
+  uint64_t *found = kWaves > 1 ? l.found + wave * kEach : l.list;
+  int mine = 0;                                    // of this wave
+  keep_packed(raw);
+#pragma unroll
+  for (int i = 0; i < kVecs; ++i) {
+    float x[T::E];
+    T::unpack(raw[i], x);
+#pragma unroll
+    for (int e = 0; e < T::E; ++e) {
+      const uint64_t in = __ballot(x[e] >= v);
+      if (in) {
+        const int at = mine + __builtin_amdgcn_mbcnt_hi((uint32_t)(in >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)in, 0));
+        if (x[e] >= v && at < kEach)
+          found[at] = ((uint64_t)order_of(x[e]) << 32) | (uint32_t)~((lane + kThreads * i) * T::E + e);
+        mine += __popcll(in);
+      }
+    }
+    __builtin_amdgcn_sched_barrier(0);             // one vector at a time: their temporaries do not add up
+  }
+  int n = mine, ties = 0;                          // ties: equal to the last listed value, not listed and not in the list
+  bool over = mine > kEach;
+  if (kWaves > 1) {
+    turn ^= 1;
+    if (wl == 0) l.wave_n[turn][wave] = mine;
+    __syncthreads();
+    int before = 0;
+    n = 0;
+    over = false;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+      const int k = l.wave_n[turn][w];
+      before += w < wave ? k : 0;
+      n += k;
+      over |= k > kEach;
+    }
+    if (n <= most && !over)
+      for (int j = wl; j < mine; j += 64) l.list[before + j] = found[j];
+  }
+  if (lane == 0) l.count = l.ties = 0;
+  unit_sync<kThreads>();
+  if (n > most || over) {                          // ties, or a row in some order: bisect, reading the row again
+    auto count = [&](auto in) {
+      int k = 0;
+      each_in_memory<T, kThreads>(z, n_all, lane, [&](float x, int c, bool ok) { k += __popcll(__ballot(ok && in(x, c))); });
+      return waves_add<kThreads>(k, l, turn);
+    };
+    const float m = waves_all<kThreads>(lanes_max<64>(top), l, turn, [](float x, float y) { return fmaxf(x, y); });
     uint32_t lo = order_of(v), hi = order_of(m) + 1;
     int above = 0;                                 // elements from `hi` on
-    while (n > kCandidates && hi - lo > 1) {
+    n = count([&](float x, int) { return x >= v; });
+    while (n > most && hi - lo > 1) {
       const uint32_t mid = lo + (hi - lo) / 2;
       const float y = value_of(mid);
       const int k = count([&](float x, int) { return x >= y; });
@@ -191,8 +239,9 @@ __global__ __launch_bounds__(kThreads < 256 ? 256 : kThreads) void top_unit_kern
         above = k;
       }
     }
-    tie = value_of(lo);
-    if (n > kCandidates) {                         // all of them equal but for `above` < K: the lowest classes
+    const float tie = value_of(lo);
+    int upto = n_all;
+    if (n > most) {                                // all of them equal but for `above` < K: the lowest classes
       int from = -1, to = n_all - 1;
       while (to - from > 1) {
         const int mid = (from + to) / 2;
@@ -200,19 +249,15 @@ __global__ __launch_bounds__(kThreads < 256 ? 256 : kThreads) void top_unit_kern
         else from = mid;
       }
       upto = to;
+      ties = n - K;
       n = K;
     }
+    each_in_memory<T, kThreads>(z, n_all, lane, [&](float x, int c, bool ok) {
+      if (ok && (x > tie || (x == tie && c <= upto)))
+        l.list[atomicAdd(&l.count, 1)] = ((uint64_t)order_of(x) << 32) | (uint32_t)~c;     // any order: what follows goes by rank
+    });
+    unit_sync<kThreads>();
   }
-
-  if (lane == 0) l.count = 0;
-  unit_sync<kThreads>();
-  each<T, kThreads>(raw, lane, [&](float x, int c) {
-    if (x > tie || (x == tie && c <= upto)) {
-      const int at = atomicAdd(&l.count, 1);       // any order: what follows goes by rank
-      l.list[at] = ((uint64_t)order_of(x) << 32) | (uint32_t)~c;
-    }
-  });
-  unit_sync<kThreads>();
   float *values = a.values + unit * a.ld_top;
   int32_t *ids = a.ids + unit * a.ld_top;
   for (int j = lane; j < n; j += kThreads) {
@@ -226,7 +271,6 @@ __global__ __launch_bounds__(kThreads < 256 ? 256 : kThreads) void top_unit_kern
       ids[rank] = a.listed_ids ? a.listed_ids[row * a.ld + c] : first + c;
     }
     if (rank == K - 1) l.last = key;
-    if (rank == K) l.next = key;
   }
   for (int k = (n < K ? n : K) + lane; k < a.fill; k += kThreads) {
     values[k] = kNegInf;
@@ -234,27 +278,51 @@ __global__ __launch_bounds__(kThreads < 256 ? 256 : kThreads) void top_unit_kern
   }
   if (!a.tail && !a.part_tail) return;
 
+  // the others: below the last listed value, and what equals it and is not listed
   unit_sync<kThreads>();
   const float scale = a.inv_t * kLog2e;
   float last = -FLT_MAX;                           // all above -inf are listed
-  int last_c = n_all;
   if (n >= K) {
-    last = value_of((uint32_t)(l.last >> 32));
-    last_c = (int)~(uint32_t)l.last;
+    const uint64_t key = l.last;
+    last = value_of((uint32_t)(key >> 32));
+    for (int j = lane; j < n; j += kThreads)
+      if (l.list[j] < key && (l.list[j] >> 32) == (key >> 32)) atomicAdd(&l.ties, 1);
+    unit_sync<kThreads>();
+    ties += l.ties;
   }
-  auto other = [&](float x, int c) { return !(x > last || (x == last && c <= last_c)); };
-  float m;
-  if (n > K) {
-    m = value_of((uint32_t)(l.next >> 32));
-  } else {
-    m = kNegInf;
-    each<T, kThreads>(raw, lane, [&](float x, int c) { m = fmaxf(m, other(x, c) ? x : kNegInf); });
-    m = waves_all<kThreads>(lanes_max<64>(m), l, turn, [](float x, float y) { return fmaxf(x, y); });
-  }
-  const float base = m == kNegInf ? 0.f : m;
+  float m = last;                                  // no exponent is above 0
   float s = 0.f;
-  each<T, kThreads>(raw, lane, [&](float x, int c) { s += exp_at(other(x, c) ? x : kNegInf, base, scale); });
-  s = waves_all<kThreads>(lanes_sum<64>(s), l, turn, [](float x, float y) { return x + y; });
+  auto rest = [&](float base) {
+    const Exps ex(base, scale);
+    float s0 = 0.f, s1 = 0.f;
+    keep_packed(raw);
+#pragma unroll
+    for (int i = 0; i < kVecs; ++i) {
+      float x[T::E];
+      T::unpack(raw[i], x);
+#pragma unroll
+      for (int e = 0; e < T::E; ++e) (e % 2 ? s1 : s0) += ex.raw(x[e] >= last ? kNegInf : x[e]);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    return waves_all<kThreads>(lanes_sum<64>((s0 + s1) * ex.fix), l, turn, [](float x, float y) { return x + y; });
+  };
+  if (last <= FLT_MAX) s = rest(m) + (float)ties;
+  if (s < 0x1p-80f) {                              // all far below it, or nothing: take their own maximum
+    m = kNegInf;
+#pragma unroll
+    for (int i = 0; i < kVecs; ++i) {
+      float x[T::E];
+      T::unpack(raw[i], x);
+#pragma unroll
+      for (int e = 0; e < T::E; ++e) m = fmaxf(m, x[e] >= last ? kNegInf : x[e]);
+    }
+    m = waves_all<kThreads>(lanes_max<64>(m), l, turn, [](float x, float y) { return fmaxf(x, y); });
+    s = rest(m == kNegInf ? 0.f : m);
+    if (ties && s == s) {                          // an infinity that is not listed
+      m = INFINITY;
+      s = 1.f;
+    }
+  }
   if (threadIdx.x % kThreads >= 64) return;
   if (a.tails) {                                   // what the row's parts left out (at most 64)
     const float2 p = lane < a.tails ? a.listed_tails[row * a.tails + lane] : make_float2(kNegInf, 0.f);
@@ -271,24 +339,17 @@ __global__ __launch_bounds__(kThreads < 256 ? 256 : kThreads) void top_unit_kern
 
 // ---- a thread to a row ----------------------------------------------------------------------
 //
-// An element is one fp64 number: its value, with the class in the lowest of the 29 bits that a
-// float leaves free, so that of equal values the lower class is larger.  The list is kept sorted by
-// one maximum and one minimum a slot; what falls out at its end is no part of it any more and goes
-// into the log-sum.  A wave's rows pass through LDS in tiles of kTile classes.
+// The list is kept sorted: x > v_i for some i on, and v_i becomes the middle one of v_{i-1}, x and
+// v_i, its class the one that goes with it.  Classes come in ascending order, so of equal values the
+// one that is there stays in front.  What falls out at the end is no part of the list any more and
+// goes into the log-sum.  A wave's rows pass through LDS in tiles of kTile classes.
 
 constexpr int kTile = 32;
-constexpr uint32_t kClassMask = PGCN_MAX_CLASSES - 1;
 
-__device__ __forceinline__ double list_key(float x, int c) {
-  if (!(x > kNegInf)) return -__builtin_inf();
-  const double d = x > FLT_MAX ? 0x1p200 : (double)(x + 0.f);         // infinity, in numbers
-  const uint64_t b = __builtin_bit_cast(uint64_t, d);
-  return __builtin_bit_cast(double, b | ((b >> 63) ? (uint32_t)c : kClassMask - (uint32_t)c));
-}
-
-__device__ __forceinline__ int key_class(double k) {
-  const uint64_t b = __builtin_bit_cast(uint64_t, k);
-  return (b >> 63) ? (int)((uint32_t)b & kClassMask) : (int)(kClassMask - ((uint32_t)b & kClassMask));
+// Both are there: a select, and no branch.
+template <class V>
+__device__ __forceinline__ V pick(bool c, V a, V b) {
+  return c ? a : b;
 }
 
 template <class T, int kSlots>
@@ -311,18 +372,21 @@ __global__ __launch_bounds__(256) void top_lists_kernel(pgcn_top_logits_args a) 
                                    : typename T::raw{};
     }
   };
-  double list[kSlots];
+  float v[kSlots];
+  int ids[kSlots];
 #pragma unroll
-  for (int k = 0; k < kSlots; ++k) list[k] = -__builtin_inf();
+  for (int k = 0; k < kSlots; ++k) {
+    v[k] = kNegInf;
+    ids[k] = -1;
+  }
   float m = kNegInf, s = 0.f;
-  bool nan = false;
+  bool nan = false, inf = false;
   auto left_out = [&](float x) {
+    inf |= x > FLT_MAX;                            // an infinity that is not listed
     const float e = __builtin_amdgcn_exp2f(-fabsf(x - m) * scale);
-    nan |= x > FLT_MAX;                            // an infinity that is not listed
-    if (x > kNegInf) {
-      s = x > m ? s * e + 1.0f : s + e;
-      m = fmaxf(m, x);
-    }
+    const float t = pick(x > m, __builtin_fmaf(s, e, 1.0f), s + e);
+    s = pick(x > kNegInf, t, s);
+    m = pick(x > m, x, m);
   };
   load(0);
   for (int c0 = 0; c0 < C; c0 += kTile) {
@@ -332,37 +396,39 @@ __global__ __launch_bounds__(256) void top_lists_kernel(pgcn_top_logits_args a) 
       float x[T::E];
       T::unpack(raw[i], x);
 #pragma unroll
-      for (int e = 0; e < T::E; ++e) tile[(ty + kDown * i) * (kTile + 1) + tx * T::E + e] = x[e];
+      for (int e = 0; e < T::E; ++e)
+        tile[(ty + kDown * i) * (kTile + 1) + tx * T::E + e] = c0 + tx * T::E + e < C ? x[e] : kNegInf;
     }
     wave_sync();
     if (c0 + kTile < C) load(c0 + kTile);
     const int n = C - c0 < kTile ? C - c0 : kTile;
+#pragma unroll 4
     for (int c = 0; c < n; ++c) {
-      const float x = tile[lane * (kTile + 1) + c];
-      nan |= x != x;
-      double k = list_key(x, c0 + c);
+      const float in = tile[lane * (kTile + 1) + c];
+      nan |= in != in;
+      const float x = pick(in == in, in, kNegInf);
+      const float out = pick(x > v[kSlots - 1], v[kSlots - 1], x);
 #pragma unroll
-      for (int i = 0; i < kSlots; ++i) {
-        const double hi = __builtin_fmax(list[i], k);
-        k = __builtin_fmin(list[i], k);
-        list[i] = hi;
+      for (int i = kSlots - 1; i >= 0; --i) {
+        ids[i] = pick(x > v[i], c0 + c, ids[i]);
+        if (i > 0) ids[i] = pick(x > v[i - 1], ids[i - 1], ids[i]);
+        v[i] = i > 0 ? __builtin_amdgcn_fmed3f(v[i - 1], x, v[i]) : pick(x > v[0], x, v[0]);
       }
-      left_out((float)k);
+      left_out(out);
     }
   }
   const int64_t r = row0 + lane;
   if (r >= a.rows) return;
 #pragma unroll
   for (int k = 0; k < kSlots; ++k) {
-    const bool some = list[k] > -__builtin_inf();
     if (k < K) {
-      a.top_values[r * a.ld_top + k] = some ? (float)list[k] : kNegInf;
-      a.top_ids[r * a.ld_top + k] = some ? key_class(list[k]) : -1;
-    } else if (some) {
-      left_out((float)list[k]);
+      a.top_values[r * a.ld_top + k] = v[k];
+      a.top_ids[r * a.ld_top + k] = ids[k];
+    } else {
+      left_out(v[k]);
     }
   }
-  if (a.tail_lse) a.tail_lse[r] = nan ? __builtin_nanf("") : s == 0.f ? kNegInf : m / a.temperature + __logf(s);
+  if (a.tail_lse) a.tail_lse[r] = nan ? __builtin_nanf("") : inf ? INFINITY : s == 0.f ? kNegInf : m / a.temperature + __logf(s);
 }
 
 // ---- launches -------------------------------------------------------------------------------
@@ -396,16 +462,25 @@ int unit_go(const TopArgs &a, hipStream_t s) {
   return PGCN_OK;
 }
 
+// Threads that a list of this length wants: four lane maxima to a slot keep the threshold tight.
+int unit_threads(int top) { return top <= 16 ? 64 : top <= 64 ? 256 : 1024; }
+
 template <class T>
 int units(const TopArgs &a, hipStream_t s) {
-  const int vecs = (std::min(a.range, a.classes) + T::E - 1) / T::E;
-  if (vecs <= 64) return unit_go<T, 64, 1>(a, s);
-  if (vecs <= 128) return unit_go<T, 64, 2>(a, s);
-  if (vecs <= 256) return unit_go<T, 64, 4>(a, s);
-  if (vecs <= 512) return unit_go<T, 64, 8>(a, s);
-  if (vecs <= 1024) return unit_go<T, 256, 4>(a, s);
-  if (vecs <= 2048) return unit_go<T, 256, 8>(a, s);
-  if (vecs <= 4096) return unit_go<T, 512, 8>(a, s);
+  const int vecs = (std::min(a.range, a.classes) + T::E - 1) / T::E, least = unit_threads(a.top);
+  if (least == 64 && !a.listed_ids && vecs <= 256) {
+    if (vecs <= 64) return unit_go<T, 64, 1>(a, s);
+    if (vecs <= 128) return unit_go<T, 64, 2>(a, s);
+    return unit_go<T, 64, 4>(a, s);
+  }
+  if (least <= 256 && vecs <= 2048) {
+    if (vecs <= 256) return unit_go<T, 256, 1>(a, s);
+    if (vecs <= 512) return unit_go<T, 256, 2>(a, s);
+    if (vecs <= 1024) return unit_go<T, 256, 4>(a, s);
+    return unit_go<T, 256, 8>(a, s);
+  }
+  if (vecs <= 1024) return unit_go<T, 1024, 1>(a, s);
+  if (vecs <= 4096) return unit_go<T, 1024, 4>(a, s);
   return unit_go<T, 1024, 8>(a, s);
 }
 

@@ -64,10 +64,13 @@ def check_top(Z, C, K, T, dtype, **kw):
     assert np.array_equal(v.astype(np.float64), rv)
     if t is None:
         return
+    over = rt == np.inf                      # an infinity is not listed: +inf or NaN, as the interface says
+    assert (np.isnan(t[over]) | (t[over] == np.inf)).all()
+    t, rt, z = t[~over], rt[~over], z[~over]
     assert np.array_equal(np.isnan(t), np.isnan(rt)) and np.array_equal(t == NINF, rt == NINF)
     on = np.isfinite(rt)
     zz = np.where(np.isfinite(z), np.abs(z), 0.0).max(axis=1, initial=0.0)
-    assert (np.abs(t - rt)[on] <= log_error(4 * zz / T, rt)[on]).all()
+    assert (np.abs(t[on] - rt[on]) <= log_error(4 * zz[on] / T, rt[on])).all()
 
 
 def logits(rng, rows, C, scale=2.5):
@@ -87,9 +90,9 @@ def test_top_logits_sizes(rows, C, K, dtype):
     check_top(matrix(logits(rng, rows, C), dtype), C, K, 2.0, dtype, ld_top=K + 3)
 
 
-@pytest.mark.parametrize("C,K", [(41, 8), (100, 64), (300, 32), (5000, 64), (40000, 200), (131072, 256)])
-@pytest.mark.parametrize("kind", ["equal", "ties", "rising", "falling", "masked", "one_left", "none_left", "lowest", "inf", "zeros",
-                                  "last_block"])
+@pytest.mark.parametrize("C,K", [(41, 8), (100, 64), (300, 32), (700, 1), (1500, 100), (5000, 64), (40000, 200), (131072, 256)])
+@pytest.mark.parametrize("kind", ["equal", "ties", "rising", "falling", "masked", "one_left", "none_left", "lowest", "inf", "infs", "far_rest",
+                                  "zeros", "last_block"])
 def test_top_logits_orders_and_masks(C, K, kind):
     rng = np.random.default_rng(C)
     z = logits(rng, 3, C)
@@ -114,6 +117,13 @@ def test_top_logits_orders_and_masks(C, K, kind):
         z[0, C // 2] = np.inf
         z[1, 0] = np.nan
         z[2, C - 1] = np.nan
+    elif kind == "infs":                    # more of them than slots, as many, fewer
+        z[0, :K] = np.inf
+        z[1, 1] = z[1, C - 1] = np.inf
+    elif kind == "far_rest":                # what is not listed underflows relative to what is
+        z[:] = -200.0 + 0.01 * z
+        z[0, :K] = 300.0
+        z[1, C - 1] = 300.0
     elif kind == "zeros":
         z[:] = np.where(rng.random(z.shape) < 0.5, 0.0, -0.0)
     else:
