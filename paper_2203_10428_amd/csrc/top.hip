@@ -58,7 +58,7 @@ __device__ __forceinline__ void each_in_memory(const typename T::type *z, int n,
 }
 
 // Candidates of a wave, and of a unit's waves together.
-constexpr int wave_candidates(int waves) { return waves == 1 ? 128 : waves == 4 ? 192 : 64; }
+constexpr int wave_candidates(int waves) { return waves == 1 ? 128 : waves == 4 ? 192 : 96; }
 
 template <int kThreads>
 struct TopLds {
@@ -102,11 +102,12 @@ __device__ __forceinline__ float waves_all(float v, TopLds<kThreads> &l, int &tu
   return v;
 }
 
-// A value that at least r of a wave's 64 reach and few more: their r-th largest, less at most 2^12
-// units in the last place.  -inf where fewer than r are above that.
+// A value that at least r of a wave's 64 reach and few more: their r-th largest, less at most 2^14
+// units in the last place.
 __device__ __forceinline__ float reached_by(float v, int r) {
-  uint32_t lo = order_of(kNegInf), hi = __builtin_amdgcn_readfirstlane(order_of(lanes_max<64>(v))) + 1;
-  for (int i = 0; i < 20 && hi - lo > 1; ++i) {
+  uint32_t lo = __builtin_amdgcn_readfirstlane(order_of(-lanes_max<64>(-v)));
+  uint32_t hi = __builtin_amdgcn_readfirstlane(order_of(lanes_max<64>(v))) + 1;
+  while (hi - lo > 1u << 14) {
     const uint32_t mid = lo + (hi - lo) / 2;
     if (__popcll(__ballot(v >= value_of(mid))) >= r) lo = mid;
     else hi = mid;
@@ -115,7 +116,7 @@ __device__ __forceinline__ float reached_by(float v, int r) {
 }
 
 template <class T, int kThreads, int kVecs>
-__global__ __launch_bounds__(kThreads < 256 ? 256 : kThreads, kVecs <= 2 ? 8 : kVecs == 4 ? 7 : T::E == 4 ? 7 : 5) void top_unit_kernel(TopArgs a) {
+__global__ __launch_bounds__(kThreads < 256 ? 256 : kThreads, kVecs <= 2 ? 8 : kVecs == 16 ? 4 : kVecs == 4 || T::E == 4 ? 7 : 5) void top_unit_kernel(TopArgs a) {
   constexpr int kUnits = kThreads < 256 ? 256 / kThreads : 1, kWaves = kThreads / 64;
   __shared__ TopLds<kThreads> lds[kUnits];
   const int lane = threadIdx.x % kThreads, slot = threadIdx.x / kThreads;
@@ -150,9 +151,12 @@ __global__ __launch_bounds__(kThreads < 256 ? 256 : kThreads, kVecs <= 2 ? 8 : k
   }
 
   int turn = 0;
-  const int r = (K + kWaves - 1) / kWaves;
-  float v = reached_by(top, r);                    // r <= 64: see unit_threads
-  if (kWaves > 1) {
+  const int most = K + (kWaves > 1 ? 128 : 63);    // candidates to rank
+  const int vecs = (n_all + T::E - 1) / T::E, maxima = vecs < kThreads ? vecs : kThreads;
+  const int r = (64 * K + maxima - 1) / maxima;    // the wave's share of K lane maxima
+  float v = kNegInf;                               // a short row is its own list of candidates
+  if (n_all > most && r <= 64) v = reached_by(top, r);
+  if (kWaves > 1 && n_all > most && r <= 64) {
     // every wave's value is a candidate: the largest that K lane maxima of the unit reach (all reach the smallest)
     if (threadIdx.x % 64 == 0) l.wave_f[0][threadIdx.x / 64] = v;
     __syncthreads();
@@ -174,7 +178,6 @@ __global__ __launch_bounds__(kThreads < 256 ? 256 : kThreads, kVecs <= 2 ? 8 : k
     v = lanes_max<64>(v);
   }
   v = fmaxf(v, -FLT_MAX);                          // x >= v: every x above -inf
-  const int most = K + (kWaves > 1 ? 128 : 32);    // candidates to rank
   constexpr int kEach = TopLds<kThreads>::kEach;
   const int wave = kWaves > 1 ? threadIdx.x / 64 : 0, wl = threadIdx.x % 64;
   uint64_t *found = kWaves > 1 ? l.found + wave * kEach : l.list;
@@ -217,10 +220,23 @@ __global__ __launch_bounds__(kThreads < 256 ? 256 : kThreads, kVecs <= 2 ? 8 : k
   }
   if (lane == 0) l.count = l.ties = 0;
   unit_sync<kThreads>();
-  if (n > most || over) {                          // ties, or a row in some order: bisect, reading the row again
+  if (n > most || over) {                          // ties, or a row in some order: bisect
+    auto visit = [&](auto f) {                     // few registers are walked again, many would be held twice
+      if constexpr (kVecs <= 4) {
+#pragma unroll
+        for (int i = 0; i < kVecs; ++i) {
+          float x[T::E];
+          T::unpack(raw[i], x);
+#pragma unroll
+          for (int e = 0; e < T::E; ++e) f(x[e], (lane + kThreads * i) * T::E + e, true);
+        }
+      } else {
+        each_in_memory<T, kThreads>(z, n_all, lane, f);
+      }
+    };
     auto count = [&](auto in) {
       int k = 0;
-      each_in_memory<T, kThreads>(z, n_all, lane, [&](float x, int c, bool ok) { k += __popcll(__ballot(ok && in(x, c))); });
+      visit([&](float x, int c, bool ok) { k += __popcll(__ballot(ok && in(x, c))); });
       return waves_add<kThreads>(k, l, turn);
     };
     const float m = waves_all<kThreads>(lanes_max<64>(top), l, turn, [](float x, float y) { return fmaxf(x, y); });
@@ -252,7 +268,7 @@ __global__ __launch_bounds__(kThreads < 256 ? 256 : kThreads, kVecs <= 2 ? 8 : k
       ties = n - K;
       n = K;
     }
-    each_in_memory<T, kThreads>(z, n_all, lane, [&](float x, int c, bool ok) {
+    visit([&](float x, int c, bool ok) {
       if (ok && (x > tie || (x == tie && c <= upto)))
         l.list[atomicAdd(&l.count, 1)] = ((uint64_t)order_of(x) << 32) | (uint32_t)~c;     // any order: what follows goes by rank
     });
@@ -344,7 +360,7 @@ __global__ __launch_bounds__(kThreads < 256 ? 256 : kThreads, kVecs <= 2 ? 8 : k
 // one that is there stays in front.  What falls out at the end is no part of the list any more and
 // goes into the log-sum.  A wave's rows pass through LDS in tiles of kTile classes.
 
-constexpr int kTile = 32;
+constexpr int kTile = 32, kStep = 4;
 
 // Both are there: a select, and no branch.
 template <class V>
@@ -381,12 +397,18 @@ __global__ __launch_bounds__(256) void top_lists_kernel(pgcn_top_logits_args a) 
   }
   float m = kNegInf, s = 0.f;
   bool nan = false, inf = false;
-  auto left_out = [&](float x) {
-    inf |= x > FLT_MAX;                            // an infinity that is not listed
-    const float e = __builtin_amdgcn_exp2f(-fabsf(x - m) * scale);
-    const float t = pick(x > m, __builtin_fmaf(s, e, 1.0f), s + e);
-    s = pick(x > kNegInf, t, s);
-    m = pick(x > m, x, m);
+  // kStep values that are no part of the list: one rescaling of the sum for all of them
+  auto left_out = [&](const float (&x)[kStep]) {
+    float big = m;
+#pragma unroll
+    for (int i = 0; i < kStep; ++i) big = pick(x[i] > big, x[i], big);
+    inf |= big > FLT_MAX;                          // an infinity that is not listed
+    const float base = pick(big > kNegInf, big, 0.f);
+    float add[kStep];
+#pragma unroll
+    for (int i = 0; i < kStep; ++i) add[i] = exp_at(x[i], base, scale);
+    s = __builtin_fmaf(s, exp_at(m, base, scale), (add[0] + add[1]) + (add[2] + add[3]));
+    m = big;
   };
   load(0);
   for (int c0 = 0; c0 < C; c0 += kTile) {
@@ -402,32 +424,52 @@ __global__ __launch_bounds__(256) void top_lists_kernel(pgcn_top_logits_args a) 
     wave_sync();
     if (c0 + kTile < C) load(c0 + kTile);
     const int n = C - c0 < kTile ? C - c0 : kTile;
-#pragma unroll 4
-    for (int c = 0; c < n; ++c) {
-      const float in = tile[lane * (kTile + 1) + c];
-      nan |= in != in;
-      const float x = pick(in == in, in, kNegInf);
-      const float out = pick(x > v[kSlots - 1], v[kSlots - 1], x);
+    for (int c = 0; c < n; c += kStep) {           // past C the tile holds -inf
+      float x[kStep];
 #pragma unroll
-      for (int i = kSlots - 1; i >= 0; --i) {
-        ids[i] = pick(x > v[i], c0 + c, ids[i]);
-        if (i > 0) ids[i] = pick(x > v[i - 1], ids[i - 1], ids[i]);
-        v[i] = i > 0 ? __builtin_amdgcn_fmed3f(v[i - 1], x, v[i]) : pick(x > v[0], x, v[0]);
+      for (int j = 0; j < kStep; ++j) x[j] = tile[lane * (kTile + 1) + c + j];
+#pragma unroll
+      for (int j = 0; j < kStep; ++j) {
+        nan |= x[j] != x[j];
+        const float y = pick(x[j] == x[j], x[j], kNegInf);
+        x[j] = pick(y > v[kSlots - 1], v[kSlots - 1], y);
+#pragma unroll
+        for (int i = kSlots - 1; i >= 0; --i) {
+          ids[i] = pick(y > v[i], c0 + c + j, ids[i]);
+          if (i > 0) ids[i] = pick(y > v[i - 1], ids[i - 1], ids[i]);
+          v[i] = i > 0 ? __builtin_amdgcn_fmed3f(v[i - 1], y, v[i]) : pick(y > v[0], y, v[0]);
+        }
       }
-      left_out(out);
+      left_out(x);
     }
   }
+#pragma unroll
+  for (int k = 0; k < kSlots; k += kStep) {
+    float x[kStep];
+#pragma unroll
+    for (int j = 0; j < kStep; ++j) x[j] = k + j < K ? kNegInf : v[k + j];
+    if (k + kStep > K) left_out(x);
+  }
+  // the lists by way of the tile, so that neighbouring lanes write neighbouring slots
+  constexpr int kSide = kSlots < kTile ? kSlots : kTile;
+  const int kx = lane % kSide, ky = lane / kSide;
+  auto write = [&](auto *out, auto *slots, auto value) {
+#pragma unroll
+    for (int k0 = 0; k0 < kSlots; k0 += kSide) {
+      wave_sync();
+#pragma unroll
+      for (int k = 0; k < kSide; ++k) slots[lane * (kTile + 1) + k] = value(k0 + k);
+      wave_sync();
+      if (k0 + kx < K)
+#pragma unroll 4
+        for (int i = ky; i < 64; i += 64 / kSide)
+          if (row0 + i < a.rows) out[(row0 + i) * a.ld_top + k0 + kx] = slots[i * (kTile + 1) + kx];
+    }
+  };
+  write(a.top_values, tile, [&](int k) { return v[k]; });
+  write(a.top_ids, (int32_t *)tile, [&](int k) { return ids[k]; });
   const int64_t r = row0 + lane;
   if (r >= a.rows) return;
-#pragma unroll
-  for (int k = 0; k < kSlots; ++k) {
-    if (k < K) {
-      a.top_values[r * a.ld_top + k] = v[k];
-      a.top_ids[r * a.ld_top + k] = ids[k];
-    } else {
-      left_out(v[k]);
-    }
-  }
   if (a.tail_lse) a.tail_lse[r] = nan ? __builtin_nanf("") : inf ? INFINITY : s == 0.f ? kNegInf : m / a.temperature + __logf(s);
 }
 
@@ -435,21 +477,27 @@ __global__ __launch_bounds__(256) void top_lists_kernel(pgcn_top_logits_args a) 
 
 int vector_elems(int32_t dtype) { return dtype == PGCN_BF16 ? BF16::E : F32::E; }
 
-constexpr int kPartThreads = 256, kPartVecs = 4, kLongVecs = 8192;
+constexpr int kPartThreads = 256, kPartVecs = 4;
+// Vectors of the longest row that a workgroup holds.
+int long_vecs(int32_t dtype) { return dtype == PGCN_BF16 ? 4096 : 8192; }
 
 // Parts of a row, 1: the whole of it at once.
 int top_parts(int32_t dtype, int64_t rows, int32_t classes) {
   const int64_t range = (int64_t)kPartThreads * kPartVecs * vector_elems(dtype), parts = (classes + range - 1) / range;
-  return parts > kLongVecs / (kPartThreads * kPartVecs) || (rows <= 128 && parts >= 4) ? (int)parts : 1;
+  return parts > long_vecs(dtype) / (kPartThreads * kPartVecs) || (rows <= 128 && parts >= 4) ? (int)parts : 1;
 }
 
-// Whether a thread takes a row.
+// Whether a thread takes a row: fits to both kernels' times, in us.  A thread's walk is a chain, so few
+// rows cost its length and many rows their instructions; a unit costs about the same for any row
+// that it holds.  Lists and units, us: 1,000 x 41 top 8 9.7, 5; 58,000 x 41 top 8 11.8, 36; 58,000 x
+// 100 top 64 75, 90; 306,000 x 64 top 16 56, 180; 306,000 x 200 top 16 154, 270; 306,000 x 500 top 64
+// 1,181, 627.
 bool lists_taken(int64_t rows, int32_t classes, int32_t top) {
   if (top > 64) return false;
   int slots = 4;
   while (slots < top) slots *= 2;
-  const int64_t walk = (int64_t)classes * (2 * slots + 12);            // instructions of a wave
-  return walk <= 2048 || (rows >= 32768 && walk / 64 <= 500);
+  const double walk = std::max(0.04 + 0.0085 * slots, (double)rows * (0.8 + 0.105 * slots) * 1e-6);
+  return 3.5 + classes * walk < 5.0 + (double)rows * (top <= 16 ? 0.8e-3 : 1.5e-3);
 }
 
 template <class T, int kThreads, int kVecs>
@@ -462,26 +510,24 @@ int unit_go(const TopArgs &a, hipStream_t s) {
   return PGCN_OK;
 }
 
-// Threads that a list of this length wants: four lane maxima to a slot keep the threshold tight.
-int unit_threads(int top) { return top <= 16 ? 64 : top <= 64 ? 256 : 1024; }
-
+// More lane maxima than slots keep the threshold tight; more threads than that are more to bring together.
 template <class T>
 int units(const TopArgs &a, hipStream_t s) {
-  const int vecs = (std::min(a.range, a.classes) + T::E - 1) / T::E, least = unit_threads(a.top);
-  if (least == 64 && !a.listed_ids && vecs <= 256) {
+  const int vecs = (std::min(a.range, a.classes) + T::E - 1) / T::E;
+  if (a.top <= 64 && vecs <= 256 && !a.listed_ids) {
     if (vecs <= 64) return unit_go<T, 64, 1>(a, s);
     if (vecs <= 128) return unit_go<T, 64, 2>(a, s);
     return unit_go<T, 64, 4>(a, s);
   }
-  if (least <= 256 && vecs <= 2048) {
+  if (vecs <= 1024 || (a.top <= 64 && vecs <= 2048)) {
     if (vecs <= 256) return unit_go<T, 256, 1>(a, s);
     if (vecs <= 512) return unit_go<T, 256, 2>(a, s);
     if (vecs <= 1024) return unit_go<T, 256, 4>(a, s);
     return unit_go<T, 256, 8>(a, s);
   }
-  if (vecs <= 1024) return unit_go<T, 1024, 1>(a, s);
-  if (vecs <= 4096) return unit_go<T, 1024, 4>(a, s);
-  return unit_go<T, 1024, 8>(a, s);
+  if (vecs <= 2048) return unit_go<T, 512, 4>(a, s);
+  if (T::E == 8 || vecs <= 4096) return unit_go<T, 512, 8>(a, s);
+  return unit_go<T, 512, T::E == 8 ? 8 : 16>(a, s);
 }
 
 template <class T, int kSlots>
