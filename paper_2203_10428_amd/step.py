@@ -33,6 +33,22 @@ counted by (layer, iteration).  ``optimizer``: Algorithm 1's SGD or Adam.
 ``"agg"`` (P H) W, ``"transform"`` P (H W), ``"auto"`` transform-first where
 the layer narrows (f_out < f_in), which aggregates fewer columns.
 
+``norm_groups`` > 0 puts a group norm with the activation ``act`` after every
+hidden layer, in place of the layer's own ReLU: the layer then returns Z, and
+the next layer's input is act(gamma xhat + beta).  ``norm_over``: "node"
+normalises every node's features by themselves (one group: layer norm),
+"partition" over all of the partition's nodes together.  gamma and beta start
+at 1 and 0 and are trained like the weights.  The sent rows are those of the
+normalised features, packed in a pass of their own.
+
+Distillation: ``top_logits`` lists the largest logits of every node, and
+``set_teacher`` makes the step's loss
+
+    loss_scale * (distill_hard * CE(labels) + distill_soft * T^2 * KL(teacher || student))
+
+with the teacher's lists at temperature T = ``distill_temp``; nodes with label
+-1 have no hard term, and nodes without a list no soft one.
+
 ``cache_layer1`` keeps layer 1's aggregate across iterations (GCN, no
 dropout): its input X never changes, so after the peers' rows have arrived
 once, A_full = P [X_in; X_bd] is fixed, and with feature smoothing the
@@ -77,6 +93,16 @@ class StepOptions:
     order: str = "agg"               # "agg" | "transform" | "auto" (GCN layers)
     norm: str = "mean"               # GCN propagation: "mean" D̃⁻¹Ã or "sym" D̃^{-1/2} Ã D̃^{-1/2}
     cache_layer1: bool = False       # keep layer 1's aggregate across iterations (see the module notes)
+    norm_groups: int = 0             # groups of the group norm after every hidden layer (0: none)
+    norm_over: str = "node"          # "node" | "partition": the rows that are normalised together
+    norm_eps: float = 1e-5
+    act: str = "relu"                # activation after the norm: "none" | "relu" | "silu" | "gelu"
+    distill_temp: float = 1.0        # with set_teacher: temperature and weights of the two terms
+    distill_soft: float = 0.5
+    distill_hard: float = 0.5
+
+
+ACTS = {"none": B.PGCN_ACT_NONE, "relu": B.PGCN_ACT_RELU, "silu": B.PGCN_ACT_SILU, "gelu": B.PGCN_ACT_GELU}
 
 
 def layer_order(order: str, f_in: int, f_out: int) -> int:
@@ -155,6 +181,27 @@ class PartitionTrainer:
             self.A1_ready = self.A1_started = False
             self.A1_used = self.A[1]
         self.H = {l: z(n, wd[l]) for l in range(1, L + 1)}
+        # group norm of the hidden layers: Z the layer's output, H the normalised and activated rows
+        self.norm = opts.norm_groups > 0
+        self.Z, self.J_z, self.gamma, self.beta, self.dgamma, self.dbeta = {}, {}, {}, {}, {}, {}
+        self.mean, self.rstd, self.norm_m, self.norm_v, self.G_peer_norm = {}, {}, {}, {}, {}
+        if self.norm:
+            assert opts.norm_over in ("node", "partition") and opts.act in ACTS, (opts.norm_over, opts.act)
+            assert not opts.relu_last, "a normalised model's last layer returns logits"
+            self.norm_shape = (n, 1) if opts.norm_over == "node" else (1 if n else 0, max(n, 1))
+            one = lambda f, v: torch.full((f,), v, dtype=torch.float32, device=self.dev)
+            for l in range(1, L):
+                f = wd[l]
+                assert f % opts.norm_groups == 0, (l, f, opts.norm_groups)
+                self.Z[l], self.J_z[l] = z(n, f), z(n, f)
+                self.gamma[l], self.beta[l] = one(f, 1.0), one(f, 0.0)
+                self.dgamma[l], self.dbeta[l] = one(f, 0.0), one(f, 0.0)
+                self.mean[l], self.rstd[l] = (torch.zeros(self.norm_shape[0], opts.norm_groups, device=self.dev)
+                                              for _ in range(2))
+                self.norm_m[l], self.norm_v[l] = (one(f, 0.0), one(f, 0.0)), (one(f, 0.0), one(f, 0.0))
+                self.G_peer_norm[l] = (None, None)
+        self.fuse_pack = opts.fuse_pack and not self.norm
+        self.teacher = None
         self.J_top = z(n, wd[L])
         self.J_in = {l: z(n, wd[l - 1]) for l in range(2, L + 1)}
         self.J_bd_out = {l: z(b, wd[l - 1]) for l in range(2, L + 1)}
@@ -186,6 +233,9 @@ class PartitionTrainer:
         self.loss = torch.zeros(1, dtype=torch.float32, device=self.dev)
         ws = max(B.pgcn_layer_workspace_size(self.part, wd[l - 1], wd[l], self.dtype, self.order[l])
                  for l in range(1, L + 1))
+        if self.norm:
+            ws = max([ws] + [B.pgcn_group_norm_workspace_size(B.PGCN_F32, wd[l], opts.norm_groups, *self.norm_shape)
+                             for l in range(1, L)])
         self.ws_bytes = max(ws, 256)
         self.ws = torch.empty(self.ws_bytes, dtype=torch.uint8, device=self.dev)
         self.stream = torch.cuda.Stream(device=self.dev)
@@ -198,7 +248,78 @@ class PartitionTrainer:
 
     # ------------------------------------------------------------------
     def _relu(self, l):
-        return l < self.L or self.opts.relu_last
+        return (l < self.L and not self.norm) or self.opts.relu_last
+
+    def _layer_out(self, l):
+        """Where layer l's product goes: H, or Z where a group norm follows."""
+        return self.Z[l] if l in self.Z else self.H[l]
+
+    def _norm_args(self, l, st):
+        o, f = self.opts, self.widths[l]
+        return dict(dtype=B.PGCN_F32, act=ACTS[o.act], channels=f, groups=o.norm_groups, samples=self.norm_shape[0],
+                    sample_rows=self.norm_shape[1], ld_x=ld_of(f), X=self.Z[l], gamma=self.gamma[l],
+                    beta=self.beta[l], mean=self.mean[l], rstd=self.rstd[l], workspace=self.ws,
+                    workspace_bytes=self.ws_bytes, stream=st)
+
+    def _norm_forward(self, l, st):
+        if l in self.Z:
+            B.pgcn_group_norm_fwd(ld_y=ld_of(self.widths[l]), eps=self.opts.norm_eps, Y=self.H[l],
+                                  **self._norm_args(l, st))
+
+    def _norm_backward(self, l, J_out, st):
+        """The gradient of layer l's product from that of its normalised rows."""
+        if l not in self.Z:
+            return J_out
+        ld = ld_of(self.widths[l])
+        B.pgcn_group_norm_bwd(ld_j_out=ld, ld_j_in=ld, J_out=J_out, J_in=self.J_z[l], dgamma=self.dgamma[l],
+                              dbeta=self.dbeta[l], **self._norm_args(l, st))
+        return self.J_z[l]
+
+    # ------------------------------------------------------------------
+    def top_logits(self, top: int, temperature: float = 1.0):
+        """The `top` largest logits of every node of the last step's output: (values, ids, tail_lse), to be
+        given to a student's set_teacher."""
+        C_ = self.widths[self.L]
+        v = torch.empty((self.n, top), dtype=torch.float32, device=self.dev)
+        i = torch.empty((self.n, top), dtype=torch.int32, device=self.dev)
+        tail = torch.empty(self.n, dtype=torch.float32, device=self.dev)
+        with torch.cuda.device(self.dev):
+            n = B.pgcn_top_logits_workspace_size(B.PGCN_F32, self.n, C_, top)
+            ws = torch.empty(max(n, 16), dtype=torch.uint8, device=self.dev)
+            B.pgcn_top_logits(dtype=B.PGCN_F32, rows=self.n, classes=C_, ld=ld_of(C_), top=top, ld_top=top,
+                              temperature=temperature, Z=self.H[self.L], top_values=v, top_ids=i, tail_lse=tail,
+                              workspace=ws, workspace_bytes=n, stream=torch.cuda.current_stream(self.dev))
+        return v, i, tail
+
+    def set_teacher(self, values, ids, tail_lse=None):
+        """Train against a teacher's lists ([n, top] values and ids, [n] log-sums at distill_temp or None), in
+        the order of this partition's inner nodes; None instead of the values: against the labels alone."""
+        if values is None:
+            self.teacher = None
+            return
+        assert self.loss_kind == B.PGCN_SOFTMAX_CE, "distillation replaces the softmax cross-entropy"
+        assert values.shape == ids.shape and values.shape[0] == self.n, (tuple(values.shape), self.n)
+        self.teacher = (values.to(self.dev, torch.float32).contiguous(), ids.to(self.dev, torch.int32).contiguous(),
+                        None if tail_lse is None else tail_lse.to(self.dev, torch.float32).contiguous())
+        need = B.pgcn_distill_workspace_size(B.PGCN_F32, self.n, self.widths[self.L], values.shape[1])
+        if need > self.ws_bytes:
+            torch.cuda.synchronize(self.dev)        # a step in flight still uses the smaller one
+            self.ws_bytes = need
+            self.ws = torch.empty(need, dtype=torch.uint8, device=self.dev)
+
+    def _loss(self, st):
+        o, C_, n = self.opts, self.widths[self.L], self.n
+        if self.teacher is None:
+            B.pgcn_loss_fwd_bwd(self.loss_kind, self.H[self.L], n, C_, ld_of(C_), self.labels, self.targets,
+                                ld_of(C_), self.loss_scale, self.J_top, self.loss, self.ws, self.ws_bytes, st)
+            return
+        v, i, tail = self.teacher
+        B.pgcn_distill_loss_fwd_bwd(dtype=B.PGCN_F32, rows=n, classes=C_, ld=ld_of(C_), top=v.shape[1],
+                                    ld_top=v.shape[1], temperature=o.distill_temp,
+                                    soft_scale=self.loss_scale * o.distill_soft * o.distill_temp ** 2,
+                                    hard_scale=self.loss_scale * o.distill_hard, Z=self.H[self.L], top_values=v,
+                                    top_ids=i, tail_lse=tail, labels=self.labels, J=self.J_top, loss_out=self.loss,
+                                    workspace=self.ws, workspace_bytes=self.ws_bytes, stream=st)
 
     def _refill(self, dst, src, stream):
         if self.opts.remote == "host":
@@ -223,7 +344,7 @@ class PartitionTrainer:
         send = self._send_out(1)
         if not self.A1_ready:
             if not self.A1_started:        # the running aggregate starts at P [X_in; 0]
-                B.pgcn_layer_fwd(self.part, H_in=self.X, H_bd=None, A=self.A[1], H_out=self.H[1], send_out=send,
+                B.pgcn_layer_fwd(self.part, H_in=self.X, H_bd=None, A=self.A[1], H_out=self._layer_out(1), send_out=send,
                                  **common)
                 self.A1_started = True
                 if H_bd is None:
@@ -236,14 +357,14 @@ class PartitionTrainer:
             A1 = self.A[1]
         else:
             A1 = self.A1_full
-        B.pgcn_layer_fwd(self.part, H_in=None, H_bd=None, A=A1, H_out=self.H[1], a_given=True, send_out=send,
+        B.pgcn_layer_fwd(self.part, H_in=None, H_bd=None, A=A1, H_out=self._layer_out(1), a_given=True, send_out=send,
                          **common)
         self.A1_used = A1
 
     def _send_out(self, l):
         """Send rows of layer l's output (the next layer's input), written by the layer's own output
-        kernel when packs are fused; None for the last layer or without fusion."""
-        return self.send_f[l + 1] if self.opts.fuse_pack and l < self.L else None
+        kernel when packs are fused; None for the last layer, without fusion and where a norm follows."""
+        return self.send_f[l + 1] if self.fuse_pack and l < self.L else None
 
     def _forward_layer(self, l, H_in, H_bd, st):
         """Dropout of the layer input (after the receive), then the GCN or GraphSAGE layer."""
@@ -257,7 +378,7 @@ class PartitionTrainer:
                 self._dropout(self.Xd_bd[l], H_bd, self.b, l, self.n, None, st)
                 X_bd = self.Xd_bd[l]
         common = dict(f_in=f, f_out=wd[l], gemm_dtype=self.dtype, relu=self._relu(l), ld_in=ld_of(f),
-                      ld_out=ld_of(wd[l]), W=self.W[l - 1], A=self.A[l], A_bf16=self.A16[l], H_out=self.H[l],
+                      ld_out=ld_of(wd[l]), W=self.W[l - 1], A=self.A[l], A_bf16=self.A16[l], H_out=self._layer_out(l),
                       workspace=self.ws, workspace_bytes=self.ws_bytes, stream=st)
         send = self._send_out(l)
         if self.sage:
@@ -273,7 +394,7 @@ class PartitionTrainer:
         wd, f = self.widths, self.widths[l - 1]
         A = self.A1_used if (self.cache1 and l == 1) else self.A[l]
         common = dict(f_in=f, f_out=wd[l], gemm_dtype=self.dtype, relu=self._relu(l), ld_in=ld_of(f),
-                      ld_out=ld_of(wd[l]), J_out=J_out, H_out=self.H[l], A=A, A_bf16=self.A16[l],
+                      ld_out=ld_of(wd[l]), J_out=J_out, H_out=self._layer_out(l), A=A, A_bf16=self.A16[l],
                       W=self.W[l - 1], dW=self.dW[l - 1], J_in=self.J_in.get(l), J_bd_out=self.J_bd_out.get(l),
                       workspace=self.ws, workspace_bytes=self.ws_bytes, stream=st)
         if self.sage:
@@ -307,6 +428,7 @@ class PartitionTrainer:
                 # received in iteration 2) and the smoothing acts on the kept aggregate
                 if self.A1_ready:
                     self._forward_layer1_cached(None, st)
+                    self._norm_forward(1, st)
                     continue
                 if mode == "serial":
                     self._refill(self.feat[1][cur], self.remote_f[1], st)
@@ -322,6 +444,7 @@ class PartitionTrainer:
                         self._refill(self.feat[1][nxt], self.remote_f[1], side)
                         self.ev_feat[1].record(side)
                 self._forward_layer1_cached(H_bd, st)
+                self._norm_forward(1, st)
                 continue
             if mode == "serial":
                 self._refill(self.feat[l][cur], self.remote_f[l], st)
@@ -332,7 +455,7 @@ class PartitionTrainer:
                 if o.smooth_f:
                     B.pgcn_smooth_ema(self.ema_f[l], H_bd, b, f, ld_of(f), o.gamma, st)
                     H_bd = self.ema_f[l]
-            if l == 1 or not o.fuse_pack:      # fused: layer l - 1's output kernel wrote these rows
+            if l == 1 or not self.fuse_pack:   # fused: layer l - 1's output kernel wrote these rows
                 B.pgcn_pack_boundary(self.part, B.PGCN_PACK_FEAT, H_in, self.send_f[l], f, ld_of(f), st)
             if mode == "pipe":
                 self.ev_pack[l].record(st)
@@ -340,17 +463,16 @@ class PartitionTrainer:
                 self._refill(self.feat[l][nxt], self.remote_f[l], side)
                 self.ev_feat[l].record(side)
             self._forward_layer(l, H_in, H_bd, st)
+            self._norm_forward(l, st)
 
         # ---- loss -----------------------------------------------------
-        C_ = wd[L]
-        B.pgcn_loss_fwd_bwd(self.loss_kind, self.H[L], n, C_, ld_of(C_), self.labels, self.targets, ld_of(C_),
-                            self.loss_scale, self.J_top, self.loss, self.ws, self.ws_bytes, st)
+        self._loss(st)
 
         # ---- backward -------------------------------------------------
         for l in range(L, 0, -1):
             f = wd[l - 1]
             J_out = self.J_top if l == L else self.J_in[l + 1]
-            self._backward_layer(l, J_out, st)
+            self._backward_layer(l, self._norm_backward(l, J_out, st), st)
             if l == 1:
                 break
             if mode == "serial":
@@ -376,6 +498,14 @@ class PartitionTrainer:
                                    self.W[l].numel(), o.eta, o.beta1, o.beta2, o.eps, t, st)
             else:
                 B.pgcn_sgd_update(self.W[l], self.dW[l], self.G_peer[l], self.W[l].numel(), o.eta, st)
+        for l in self.gamma:
+            for i, (p, g) in enumerate(((self.gamma[l], self.dgamma[l]), (self.beta[l], self.dbeta[l]))):
+                peer = self.G_peer_norm[l][i]
+                if o.optimizer == "adam":
+                    B.pgcn_adam_update(p, g, peer, self.norm_m[l][i], self.norm_v[l][i], p.numel(), o.eta, o.beta1,
+                                       o.beta2, o.eps, t, st)
+                else:
+                    B.pgcn_sgd_update(p, g, peer, p.numel(), o.eta, st)
         if mode == "pipe":
             self.cur = nxt
         caller.wait_stream(st)          # results are ordered before the caller's next work

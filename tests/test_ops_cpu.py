@@ -27,12 +27,14 @@ NORM = dict(dtype=B.PGCN_F32, act=B.PGCN_ACT_SILU, channels=32, groups=4, sample
 FWD = dict(NORM, ld_y=32, eps=1e-5, Y=at(6))
 BWD = dict(NORM, ld_j_out=32, ld_j_in=32, J_out=at(6), J_in=at(7), dgamma=at(8), dbeta=at(9))
 
+LONG = dict(rows=1, classes=100000, ld=100000, top=50, ld_top=50)          # a row that goes in parts
+
 BAD_TOP = [dict(dtype=2), dict(rows=-1), dict(rows=1 << 31), dict(classes=0), dict(classes=B.PGCN_MAX_CLASSES + 1, ld=1 << 20),
            dict(top=0), dict(top=42), dict(classes=512, ld=512, top=257, ld_top=257), dict(ld=40), dict(ld=42),
            dict(dtype=B.PGCN_BF16, ld=44), dict(ld_top=7), dict(temperature=0.0), dict(temperature=-1.0),
            dict(temperature=float("nan")), dict(temperature=float("inf")), dict(temperature=1e-45), dict(temperature=0.9e-4), dict(temperature=1.1e4),
            dict(Z=None), dict(top_values=None), dict(top_ids=None), dict(Z=at(0) + 4), dict(top_values=at(0)),
-           dict(tail_lse=at(1) + 8), dict(workspace=at(4) + 4)]
+           dict(tail_lse=at(1) + 8), dict(LONG, workspace=at(4) + 4)]
 BAD_DISTILL = BAD_TOP[:-3] + [dict(J=None), dict(J=at(6) + 8), dict(J=at(0)), dict(J=at(0) + 16), dict(loss_out=None),
                               dict(loss_out=at(5) + 4), dict(J=at(2)), dict(soft_scale=float("inf")),
                               dict(hard_scale=float("nan")), dict(loss_out=at(6) + 64), dict(workspace=at(4) + 4)]
@@ -50,8 +52,6 @@ def refused(call, args, code=B.PGCN_EINVAL):
 
 @pytest.mark.parametrize("bad", BAD_TOP, ids=str)
 def test_top_logits_refuses(bad):
-    if B.pgcn_top_logits_workspace_size(TOP["dtype"], 10, 41, 8) == 0 and "workspace" in bad:
-        pytest.skip("this size needs no workspace")
     refused(B.pgcn_top_logits, {**TOP, **bad})
 
 
@@ -79,6 +79,10 @@ def test_short_workspaces_are_refused():
     assert need > 0
     for ws in (dict(workspace=None, workspace_bytes=0), dict(workspace_bytes=need - 1)):
         refused(B.pgcn_distill_loss_fwd_bwd, {**DISTILL, **ws}, B.PGCN_EWORKSPACE)
+    need = B.pgcn_top_logits_workspace_size(B.PGCN_F32, 1, 100000, 50)
+    assert need > 0
+    for ws in (dict(workspace=None, workspace_bytes=0), dict(workspace_bytes=need - 1)):
+        refused(B.pgcn_top_logits, {**TOP, **LONG, **ws}, B.PGCN_EWORKSPACE)
     need = B.pgcn_group_norm_workspace_size(B.PGCN_F32, 32, 4, 3, 5)
     assert need > 0
     for call, args in ((B.pgcn_group_norm_fwd, FWD), (B.pgcn_group_norm_bwd, BWD)):
