@@ -607,24 +607,39 @@ __global__ __launch_bounds__(kThreads) void grad_rows_kernel(pgcn_group_norm_bwd
   }
 }
 
-// ------------------------------------------------- one row to a sample ----
+// -------------------------------------------- samples that fit registers ---
 //
-// kLanes threads hold a row, kVecs 16-byte vectors each (vector lane + kLanes i), so that X (and
-// J) cross the memory once and both passes over the row stay in registers.  A workgroup walks
-// rows at a fixed stride: gamma, beta and the backward's channel sums stay in registers too.
+// kLanes threads hold a sample, one row or a few, kVecs 16-byte vectors each (vector lane + kLanes i
+// of all its rows' vectors), so that X (and J) cross the memory once and both passes over the
+// sample stay in registers.  A workgroup walks samples at a fixed stride: gamma, beta and the
+// backward's channel sums stay in registers too.  Bound by memory in fp32 (30,000 x 1,024: forward
+// 4.97, backward 4.6 TB/s, 2,048 channels 4.6 and 4.8), by the activation's exponents and
+// reciprocals in bf16, where a byte carries twice the elements (2.9 and 2.5, 3.9 and 3.2).
 // How a group's sum is formed:
 enum class Sum {
-  ROW,     // one group: all the row's threads
-  LANES,   // groups of 2^k neighbouring vectors: shuffles inside them
-  LDS      // any other: the row's values through LDS, a team of lanes for each group
-};
+  ROW,     // one group: all the sample's threads
+  LANES    // one row, groups of 2^k neighbouring vectors: shuffles inside them
+};           // any other groups: see any_fwd_kernel
 
 struct RowShape {
   int f, groups, cg, vecs;
+  int rows, all;       // rows of a sample, vectors of all of them
   int span;            // LANES: vectors of a group
-  int team;            // LDS: lanes of a team
+  int team;            // any groups: lanes of a team
   uint32_t magic;      // of groups, see group_of
 };
+
+// A thread's vectors: their first channel (from f on: none) and row.
+template <class T, int kLanes, int kVecs>
+__device__ __forceinline__ void place_vectors(const RowShape &sp, int (&c0)[kVecs], int (&row)[kVecs]) {
+#pragma unroll
+  for (int i = 0; i < kVecs; ++i) {
+    const int p = threadIdx.x % kLanes + kLanes * i;
+    row[i] = sp.rows > 1 ? p / sp.vecs : 0;
+    c0[i] = p < sp.all ? (p - row[i] * sp.vecs) * T::E : 1 << 20;
+    if (p >= sp.all) row[i] = 0;
+  }
+}
 
 template <int kLanes>
 __device__ __forceinline__ void row_sync() {
@@ -636,41 +651,10 @@ __device__ __forceinline__ void row_sync() {
   }
 }
 
-// Sums of w over every group, to every element of it: out[i][e], or out[i][0] for the vector.
-// `lds`: the row's own f + groups floats (LDS), or kThreads / 64 floats (ROW over several waves).
-template <class T, int kLanes, int kVecs, Sum kSum, int kOut>
-__device__ __forceinline__ void group_sums(const float (&w)[kVecs][T::E], float (&out)[kVecs][kOut], const RowShape &sp, float *lds) {
-  const int lane = threadIdx.x % kLanes;
-  if (kSum == Sum::LDS) {
-    float *res = lds + (sp.f + 3) / 4 * 4;
-    row_sync<kLanes>();
-#pragma unroll
-    for (int i = 0; i < kVecs; ++i)
-#pragma unroll
-      for (int e = 0; e < T::E; ++e) {
-        const int c = (lane + kLanes * i) * T::E + e;
-        if (c < sp.f) lds[c] = w[i][e];
-      }
-    row_sync<kLanes>();
-    const int t = lane & (sp.team - 1), teams = kLanes / sp.team;
-    for (int g0 = 0; g0 < sp.groups; g0 += teams) {                   // the same rounds for every lane
-      const int g = g0 + lane / sp.team;
-      float s = 0.f;
-      if (g < sp.groups)
-        for (int c = t; c < sp.cg; c += sp.team) s += lds[g * sp.cg + c];
-      for (int o = sp.team / 2; o > 0; o >>= 1) s += __shfl_xor(s, o, 64);
-      if (t == 0 && g < sp.groups) res[g] = s;
-    }
-    row_sync<kLanes>();
-#pragma unroll
-    for (int i = 0; i < kVecs; ++i)
-#pragma unroll
-      for (int e = 0; e < kOut; ++e) {
-        const int c = (lane + kLanes * i) * T::E + e;
-        out[i][e] = res[group_of(sp.magic, c < sp.f ? c : 0)];
-      }
-    return;
-  }
+// Sums of w (0 past the channels) over every vector's group.  `lds`: kThreads / 64 floats (ROW over
+// several waves).
+template <class T, int kLanes, int kVecs, Sum kSum>
+__device__ __forceinline__ void group_sums(const float (&w)[kVecs][T::E], float (&out)[kVecs], const RowShape &sp, float *lds) {
   float s[kVecs];
 #pragma unroll
   for (int i = 0; i < kVecs; ++i) {
@@ -692,86 +676,131 @@ __device__ __forceinline__ void group_sums(const float (&w)[kVecs][T::E], float 
       r = (lds[0] + lds[1]) + (lds[2] + lds[3]);
     }
 #pragma unroll
-    for (int i = 0; i < kVecs; ++i) out[i][0] = r;
+    for (int i = 0; i < kVecs; ++i) out[i] = r;
   } else {
     for (int o = 1; o < sp.span; o <<= 1)
 #pragma unroll
       for (int i = 0; i < kVecs; ++i) s[i] += __shfl_xor(s[i], o, 64);
 #pragma unroll
-    for (int i = 0; i < kVecs; ++i) out[i][0] = s[i];
+    for (int i = 0; i < kVecs; ++i) out[i] = s[i];
   }
 }
 
+template <class T>
+__device__ __forceinline__ void load_vec_params(const float *p, float other, int f, int c, float (&out)[T::E]) {
+#pragma unroll
+  for (int e = 0; e < T::E; ++e) out[e] = p && c + e < f ? p[c + e] : other;
+}
 template <class T, int kVecs>
-__device__ __forceinline__ void load_params(const float *p, float other, int f, int v0, int step, float (&out)[kVecs][T::E]) {
+__device__ __forceinline__ void load_params(const float *p, float other, int f, const int (&c0)[kVecs], float (&out)[kVecs][T::E]) {
 #pragma unroll
-  for (int i = 0; i < kVecs; ++i)
-#pragma unroll
-    for (int e = 0; e < T::E; ++e) {
-      const int c = (v0 + step * i) * T::E + e;
-      out[i][e] = p && c < f ? p[c] : other;
-    }
+  for (int i = 0; i < kVecs; ++i) load_vec_params<T>(p, other, f, c0[i], out[i]);
 }
 
+// The sample whose first row is row0.
 template <class T, int kVecs>
-__device__ __forceinline__ void load_row(const void *base, int64_t off, int vecs, int v0, int step, float (&x)[kVecs][T::E]) {
-  const typename T::type *p = (const typename T::type *)base + off;
+__device__ __forceinline__ void load_rows(const void *base, int64_t row0, int64_t ld, int f, const int (&c0)[kVecs], const int (&row)[kVecs],
+                                          float (&x)[kVecs][T::E]) {
 #pragma unroll
   for (int i = 0; i < kVecs; ++i) {
     typename T::raw r = {};
-    if (v0 + step * i < vecs) r = *reinterpret_cast<const typename T::raw *>(p + (v0 + step * i) * T::E);
+    if (c0[i] < f) r = *reinterpret_cast<const typename T::raw *>((const typename T::type *)base + (row0 + row[i]) * ld + c0[i]);
     T::unpack(r, x[i]);
   }
 }
 
 template <class T, int kLanes, int kVecs, Sum kSum>
-__global__ __launch_bounds__(kThreads) void rows_fwd_kernel(pgcn_group_norm_fwd_args a, RowShape sp, int lds_row) {
-  extern __shared__ float lds_all[];
-  constexpr int kOut = kSum == Sum::LDS ? T::E : 1;
-  const int lane = threadIdx.x % kLanes, slot = threadIdx.x / kLanes;
-  float *lds = lds_all + slot * lds_row;
+__global__ __launch_bounds__(kThreads) void rows_fwd_kernel(pgcn_group_norm_fwd_args a, RowShape sp) {
+  __shared__ float lds[kThreads / 64];
+  const int slot = threadIdx.x / kLanes;
+  int c0[kVecs], row[kVecs];
+  place_vectors<T, kLanes>(sp, c0, row);
   float ga[kVecs][T::E], be[kVecs][T::E];
-  load_params<T>(a.gamma, 1.f, sp.f, lane, kLanes, ga);
-  load_params<T>(a.beta, 0.f, sp.f, lane, kLanes, be);
-  const float inv_n = 1.0f / (float)sp.cg;
+  load_params<T>(a.gamma, 1.f, sp.f, c0, ga);
+  load_params<T>(a.beta, 0.f, sp.f, c0, be);
+  const float inv_n = 1.0f / ((float)sp.cg * (float)sp.rows);
   for (int64_t r = (int64_t)blockIdx.x * (kThreads / kLanes) + slot; r < a.samples; r += (int64_t)gridDim.x * (kThreads / kLanes)) {
-    float x[kVecs][T::E], w[kVecs][T::E], mu[kVecs][kOut], rs[kVecs][kOut];
-    load_row<T>(a.X, r * a.ld_x, sp.vecs, lane, kLanes, x);
+    float x[kVecs][T::E], w[kVecs][T::E], mu[kVecs], rs[kVecs];
+    load_rows<T>(a.X, r * sp.rows, a.ld_x, sp.f, c0, row, x);
 #pragma unroll
     for (int i = 0; i < kVecs; ++i)
 #pragma unroll
-      for (int e = 0; e < T::E; ++e) w[i][e] = x[i][e] = (lane + kLanes * i) * T::E + e < sp.f ? x[i][e] : 0.f;
+      for (int e = 0; e < T::E; ++e) w[i][e] = x[i][e] = c0[i] + e < sp.f ? x[i][e] : 0.f;
     group_sums<T, kLanes, kVecs, kSum>(w, mu, sp, lds);
 #pragma unroll
     for (int i = 0; i < kVecs; ++i) {
-#pragma unroll
-      for (int e = 0; e < kOut; ++e) mu[i][e] *= inv_n;
+      mu[i] *= inv_n;
 #pragma unroll
       for (int e = 0; e < T::E; ++e) {
-        const float d = x[i][e] - mu[i][e % kOut];
-        w[i][e] = (lane + kLanes * i) * T::E + e < sp.f ? d * d : 0.f;
+        const float d = x[i][e] - mu[i];
+        w[i][e] = c0[i] + e < sp.f ? d * d : 0.f;
       }
     }
     group_sums<T, kLanes, kVecs, kSum>(w, rs, sp, lds);
 #pragma unroll
     for (int i = 0; i < kVecs; ++i) {
-      const int c0 = (lane + kLanes * i) * T::E;
-#pragma unroll
-      for (int e = 0; e < kOut; ++e) rs[i][e] = 1.0f / sqrtf(rs[i][e] * inv_n + a.eps);
-      if (c0 < sp.f) {
-        // the thread with a group's first channel writes its statistics
-#pragma unroll
-        for (int e = 0; e < kOut; ++e) {
-          const int c = c0 + e, g = group_of(sp.magic, c);
-          if (c < sp.f && g * sp.cg == c) {
-            if (a.mean) a.mean[r * sp.groups + g] = mu[i][e];
-            if (a.rstd) a.rstd[r * sp.groups + g] = rs[i][e];
-          }
+      rs[i] = 1.0f / sqrtf(rs[i] * inv_n + a.eps);
+      if (c0[i] < sp.f) {
+        const int g = group_of(sp.magic, c0[i]);
+        if (g * sp.cg == c0[i] && row[i] == 0) {   // the thread with a group's first element writes its statistics
+          if (a.mean) a.mean[r * sp.groups + g] = mu[i];
+          if (a.rstd) a.rstd[r * sp.groups + g] = rs[i];
         }
 #pragma unroll
-        for (int e = 0; e < T::E; ++e) x[i][e] = affine(normed(x[i][e], mu[i][e % kOut], rs[i][e % kOut]), ga[i][e], be[i][e]);
+        for (int e = 0; e < T::E; ++e) x[i][e] = affine(normed(x[i][e], mu[i], rs[i]), ga[i][e], be[i][e]);
         activate(x[i], a.act);
-        store_some<T>((typename T::type *)a.Y + r * a.ld_y + c0, x[i], sp.f - c0);
+        store_some<T>((typename T::type *)a.Y + (r * sp.rows + row[i]) * a.ld_y + c0[i], x[i], sp.f - c0[i]);
+      }
+    }
+  }
+}
+
+// A workgroup's channel sums: its slots' and the sample's rows' joined in a fixed order, p[2][channels].
+template <class T, int kLanes, int kVecs>
+__device__ __forceinline__ void write_channel_sums(const RowShape &sp, const int (&c0)[kVecs], const float (&s1)[kVecs][T::E],
+                                                   const float (&s2)[kVecs][T::E], float *p, float *lds_all) {
+  const int lane = threadIdx.x % kLanes, slot = threadIdx.x / kLanes;
+#pragma unroll
+  for (int half = 0; half < 2; ++half) {
+    if (sp.rows == 1) {
+#pragma unroll
+      for (int i = 0; i < kVecs; ++i) {
+        float v[T::E];
+#pragma unroll
+        for (int e = 0; e < T::E; ++e) v[e] = half ? s2[i][e] : s1[i][e];
+        constexpr int kSlots = kThreads / kLanes;
+        if (kSlots > 1) {
+          __syncthreads();
+#pragma unroll
+          for (int e = 0; e < T::E; ++e) lds_all[e * kThreads + threadIdx.x] = v[e];
+          __syncthreads();
+          if (slot == 0) {
+#pragma unroll 1
+            for (int k = 1; k < kSlots; ++k)
+#pragma unroll
+              for (int e = 0; e < T::E; ++e) v[e] += lds_all[e * kThreads + k * kLanes + lane];
+          }
+        }
+        if (slot == 0)
+#pragma unroll
+          for (int e = 0; e < T::E; ++e)
+            if (c0[i] + e < sp.f) p[half * sp.f + c0[i] + e] = v[e];
+      }
+    } else {
+      // the sums of every slot's vectors side by side, then a thread for every channel
+      __syncthreads();
+      float *at = lds_all + slot * sp.all * T::E;
+#pragma unroll
+      for (int i = 0; i < kVecs; ++i)
+        if (c0[i] < sp.f)
+#pragma unroll
+          for (int e = 0; e < T::E; ++e) at[(lane + kLanes * i) * T::E + e] = half ? s2[i][e] : s1[i][e];
+      __syncthreads();
+      const int wide = sp.vecs * T::E, n = kThreads / kLanes * sp.rows;
+      for (int c = threadIdx.x; c < sp.f; c += kThreads) {
+        float v = 0.f;
+        for (int k = 0; k < n; ++k) v += lds_all[k * wide + c];
+        p[half * sp.f + c] = v;
       }
     }
   }
@@ -779,38 +808,41 @@ __global__ __launch_bounds__(kThreads) void rows_fwd_kernel(pgcn_group_norm_fwd_
 
 // The backward of those rows; a workgroup's channel sums go to part[workgroup][2][channels].
 template <class T, int kLanes, int kVecs, Sum kSum>
-__global__ __launch_bounds__(kThreads) void rows_bwd_kernel(pgcn_group_norm_bwd_args a, RowShape sp, int lds_row, float *part) {
+__global__ __launch_bounds__(kThreads, kVecs * T::E <= 4 ? 4 : kVecs <= 4 ? 2 : 1) void rows_bwd_kernel(pgcn_group_norm_bwd_args a, RowShape sp, float *part) {
   extern __shared__ float lds_all[];
-  constexpr int kOut = kSum == Sum::LDS ? T::E : 1;
-  const int lane = threadIdx.x % kLanes, slot = threadIdx.x / kLanes;
-  float *lds = lds_all + slot * lds_row;
+  const int slot = threadIdx.x / kLanes;
+  int c0[kVecs], row[kVecs];
+  place_vectors<T, kLanes>(sp, c0, row);
   float ga[kVecs][T::E], be[kVecs][T::E], s1[kVecs][T::E] = {}, s2[kVecs][T::E] = {};
-  load_params<T>(a.gamma, 1.f, sp.f, lane, kLanes, ga);
-  load_params<T>(a.beta, 0.f, sp.f, lane, kLanes, be);
-  const float inv_n = 1.0f / (float)sp.cg;
+  constexpr bool kReread = kVecs * T::E > 16;         // gamma and beta out of L1 for every sample
+  if (!kReread) {
+    load_params<T>(a.gamma, 1.f, sp.f, c0, ga);
+    load_params<T>(a.beta, 0.f, sp.f, c0, be);
+  }
+  const float inv_n = 1.0f / ((float)sp.cg * (float)sp.rows);
   for (int64_t r = (int64_t)blockIdx.x * (kThreads / kLanes) + slot; r < a.samples; r += (int64_t)gridDim.x * (kThreads / kLanes)) {
-    float x[kVecs][T::E], j[kVecs][T::E], w[kVecs][T::E], c1[kVecs][kOut], c2[kVecs][kOut], rs[kVecs][kOut];
-    load_row<T>(a.X, r * a.ld_x, sp.vecs, lane, kLanes, x);
-    load_row<T>(a.J_out, r * a.ld_j_out, sp.vecs, lane, kLanes, j);
+    float x[kVecs][T::E], j[kVecs][T::E], w[kVecs][T::E], c1[kVecs], c2[kVecs], rs[kVecs];
+    load_rows<T>(a.X, r * sp.rows, a.ld_x, sp.f, c0, row, x);
+    load_rows<T>(a.J_out, r * sp.rows, a.ld_j_out, sp.f, c0, row, j);
 #pragma unroll
     for (int i = 0; i < kVecs; ++i) {
-      const int c0 = (lane + kLanes * i) * T::E;
-      float mu[kOut], u[T::E];
-#pragma unroll
-      for (int e = 0; e < kOut; ++e) {
-        const int64_t g = r * sp.groups + group_of(sp.magic, c0 + e < sp.f ? c0 + e : 0);
-        mu[e] = a.mean[g];
-        rs[i][e] = a.rstd[g];
+      if (kReread) {
+        load_vec_params<T>(a.gamma, 1.f, sp.f, c0[i], ga[i]);
+        load_vec_params<T>(a.beta, 0.f, sp.f, c0[i], be[i]);
       }
+      const int64_t g = r * sp.groups + group_of(sp.magic, c0[i] < sp.f ? c0[i] : 0);
+      const float mu = a.mean[g];
+      float u[T::E];
+      rs[i] = a.rstd[g];
 #pragma unroll
       for (int e = 0; e < T::E; ++e) {
-        x[i][e] = normed(x[i][e], mu[e % kOut], rs[i][e % kOut]);
+        x[i][e] = normed(x[i][e], mu, rs[i]);
         u[e] = affine(x[i][e], ga[i][e], be[i][e]);
       }
       times_slope(j[i], u, a.act);
 #pragma unroll
       for (int e = 0; e < T::E; ++e) {
-        const bool in = c0 + e < sp.f;
+        const bool in = c0[i] + e < sp.f;
         x[i][e] = in ? x[i][e] : 0.f;
         j[i][e] = in ? j[i][e] : 0.f;
         s1[i][e] += j[i][e];
@@ -820,46 +852,234 @@ __global__ __launch_bounds__(kThreads) void rows_bwd_kernel(pgcn_group_norm_bwd_
       }
     }
     if (!a.J_in) continue;
-    group_sums<T, kLanes, kVecs, kSum>(j, c1, sp, lds);
-    group_sums<T, kLanes, kVecs, kSum>(w, c2, sp, lds);
+    group_sums<T, kLanes, kVecs, kSum>(j, c1, sp, lds_all);
+    group_sums<T, kLanes, kVecs, kSum>(w, c2, sp, lds_all);
 #pragma unroll
     for (int i = 0; i < kVecs; ++i) {
-      const int c0 = (lane + kLanes * i) * T::E;
 #pragma unroll
       for (int e = 0; e < T::E; ++e)
-        x[i][e] = rs[i][e % kOut] * (j[i][e] - c1[i][e % kOut] * inv_n - x[i][e] * (c2[i][e % kOut] * inv_n));
-      if (c0 < sp.f) store_some<T>((typename T::type *)a.J_in + r * a.ld_j_in + c0, x[i], sp.f - c0);
+        x[i][e] = rs[i] * (j[i][e] - c1[i] * inv_n - x[i][e] * (c2[i] * inv_n));
+      if (c0[i] < sp.f)
+        store_some<T>((typename T::type *)a.J_in + (r * sp.rows + row[i]) * a.ld_j_in + c0[i], x[i], sp.f - c0[i]);
+    }
+  }
+  if (part) write_channel_sums<T, kLanes>(sp, c0, s1, s2, part + (int64_t)blockIdx.x * 2 * sp.f, lds_all);
+}
+
+// ---- the same for any groups --------------------------------------------------------------
+//
+// The sample's values go through LDS, where a team of lanes takes each group; what is needed after
+// the sums is read from there again and not held in registers.  gamma and beta lie in LDS too.
+// Bound by LDS instructions: an element is written once and read once (forward: twice) as a single
+// float, gamma, beta and the group's values come from LDS again.  30,000 x 1,000 fp32 in 8 groups:
+// forward 103 us (2.4 TB/s), backward 115 (3.1); 1,024 channels in 32 groups by shuffles 52 and 80.
+
+// Calls f(offset into the image) for the part of group g that lane t of its team takes.
+template <class F>
+__device__ __forceinline__ void group_walk(const RowShape &sp, int wide, int g, int t, F f) {
+  const int n = sp.rows * sp.cg;
+  if (sp.rows == 1) {
+#pragma unroll 4
+    for (int c = t; c < n; c += sp.team) f(g * sp.cg + c);
+  } else {
+#pragma unroll 4
+    for (int k = t; k < n; k += sp.team) {
+      const int r = group_of(sp.magic, k);
+      f(r * wide + g * sp.cg + k - r * sp.cg);
+    }
+  }
+}
+
+__device__ __forceinline__ float team_sum(float s, int team) {
+  for (int o = team / 2; o > 0; o >>= 1) s += __shfl_xor(s, o, 64);
+  return s;
+}
+
+// gamma and beta to LDS: [2][wide].
+__device__ __forceinline__ void stage_params(const float *gamma, const float *beta, int f, int wide, float *to) {
+  for (int c = threadIdx.x; c < wide; c += kThreads) {
+    to[c] = gamma && c < f ? gamma[c] : 1.f;
+    to[wide + c] = beta && c < f ? beta[c] : 0.f;
+  }
+  __syncthreads();
+}
+
+template <class T>
+__device__ __forceinline__ void from_lds(const float *p, float (&v)[T::E]) {
+#pragma unroll
+  for (int e = 0; e < T::E; e += 4) {
+    const op_f32x4 q = *reinterpret_cast<const op_f32x4 *>(p + e);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) v[e + k] = q[k];
+  }
+}
+template <class T>
+__device__ __forceinline__ void to_lds(float *p, const float (&v)[T::E]) {
+#pragma unroll
+  for (int e = 0; e < T::E; e += 4) *reinterpret_cast<op_f32x4 *>(p + e) = op_f32x4{v[e], v[e + 1], v[e + 2], v[e + 3]};
+}
+// Two values of its group for each element of the vector from channel c on, from a[groups] and b[groups].
+template <class T>
+__device__ __forceinline__ void of_groups(const RowShape &sp, int c, const float *a, const float *b, float (&x)[T::E], float (&y)[T::E]) {
+  if (sp.cg % T::E == 0) {
+    const int g = group_of(sp.magic, c);
+#pragma unroll
+    for (int e = 0; e < T::E; ++e) {
+      x[e] = a[g];
+      y[e] = b[g];
+    }
+  } else {
+#pragma unroll
+    for (int e = 0; e < T::E; ++e) {
+      const int g = group_of(sp.magic, c + e < sp.f ? c + e : sp.f - 1);
+      x[e] = a[g];
+      y[e] = b[g];
+    }
+  }
+}
+
+// Floats of LDS: the workgroup's gamma and beta, and for each of its samples `images` images and
+// 2 images values for every group.
+inline int64_t any_lds(const RowShape &sp, int e, int slots, int images) {
+  return 2 * (int64_t)sp.vecs * e + slots * images * ((int64_t)sp.all * e + (2 * sp.groups + 3) / 4 * 4);
+}
+
+template <class T, int kLanes, int kVecs>
+__global__ __launch_bounds__(kThreads, kVecs * T::E <= 16 ? 4 : 2) void any_fwd_kernel(pgcn_group_norm_fwd_args a, RowShape sp) {
+  extern __shared__ __align__(16) float lds_any[];
+  const int lane = threadIdx.x % kLanes, slot = threadIdx.x / kLanes, wide = sp.vecs * T::E;
+  const float *params = lds_any;
+  float *image = lds_any + 2 * wide + slot * (sp.all * T::E + (2 * sp.groups + 3) / 4 * 4), *mu = image + sp.all * T::E, *rs = mu + sp.groups;
+  int c0[kVecs], row[kVecs];
+  place_vectors<T, kLanes>(sp, c0, row);
+  stage_params(a.gamma, a.beta, sp.f, wide, lds_any);
+  const float inv_n = 1.0f / ((float)sp.cg * (float)sp.rows);
+  const int t = lane & (sp.team - 1), teams = kLanes / sp.team;
+  for (int64_t r = (int64_t)blockIdx.x * (kThreads / kLanes) + slot; r < a.samples; r += (int64_t)gridDim.x * (kThreads / kLanes)) {
+    float x[kVecs][T::E];
+    load_rows<T>(a.X, r * sp.rows, a.ld_x, sp.f, c0, row, x);
+    row_sync<kLanes>();                            // the sample before is done with the image
+#pragma unroll
+    for (int i = 0; i < kVecs; ++i)
+      if (c0[i] < sp.f) to_lds<T>(image + (lane + kLanes * i) * T::E, x[i]);
+    row_sync<kLanes>();
+    for (int g0 = 0; g0 < sp.groups; g0 += teams) {                   // the same rounds for every lane
+      const int g = g0 + lane / sp.team;
+      const bool in = g < sp.groups;
+      float s = 0.f, q = 0.f;
+      if (in) group_walk(sp, wide, g, t, [&](int at) { s += image[at]; });
+      const float m = team_sum(s, sp.team) * inv_n;
+      if (in)
+        group_walk(sp, wide, g, t, [&](int at) {
+          const float d = image[at] - m;
+          q += d * d;
+        });
+      q = 1.0f / sqrtf(team_sum(q, sp.team) * inv_n + a.eps);
+      if (in && t == 0) {
+        mu[g] = m;
+        rs[g] = q;
+        if (a.mean) a.mean[r * sp.groups + g] = m;
+        if (a.rstd) a.rstd[r * sp.groups + g] = q;
+      }
+    }
+    row_sync<kLanes>();
+#pragma unroll
+    for (int i = 0; i < kVecs; ++i) {
+      if (c0[i] >= sp.f) continue;
+      float gm[T::E], gr[T::E], ga[T::E], be[T::E];
+      of_groups<T>(sp, c0[i], mu, rs, gm, gr);
+      from_lds<T>(params + c0[i], ga);
+      from_lds<T>(params + wide + c0[i], be);
+#pragma unroll
+      for (int e = 0; e < T::E; ++e) x[i][e] = affine(normed(x[i][e], gm[e], gr[e]), ga[e], be[e]);
+      activate(x[i], a.act);
+      store_some<T>((typename T::type *)a.Y + (r * sp.rows + row[i]) * a.ld_y + c0[i], x[i], sp.f - c0[i]);
+    }
+  }
+}
+
+template <class T, int kLanes, int kVecs>
+__global__ __launch_bounds__(kThreads, kVecs * T::E <= 4 ? 4 : kVecs * T::E <= 8 ? 3 : kVecs * T::E <= 16 ? 2 : 1) void any_bwd_kernel(pgcn_group_norm_bwd_args a, RowShape sp, float *part) {
+  extern __shared__ __align__(16) float lds_any[];
+  const int lane = threadIdx.x % kLanes, slot = threadIdx.x / kLanes, wide = sp.vecs * T::E;
+  const float *params = lds_any;
+  // images of gamma du and xhat; mean and 1 / deviation, then the two sums, for every group
+  float *image = lds_any + 2 * wide + slot * 2 * (sp.all * T::E + (2 * sp.groups + 3) / 4 * 4), *xhat = image + sp.all * T::E;
+  float *mu = xhat + sp.all * T::E, *rs = mu + sp.groups, *c1 = rs + sp.groups, *c2 = c1 + sp.groups;
+  int c0[kVecs], row[kVecs];
+  place_vectors<T, kLanes>(sp, c0, row);
+  stage_params(a.gamma, a.beta, sp.f, wide, lds_any);
+  float s1[kVecs][T::E] = {}, s2[kVecs][T::E] = {};
+  const float inv_n = 1.0f / ((float)sp.cg * (float)sp.rows);
+  const int t = lane & (sp.team - 1), teams = kLanes / sp.team;
+  for (int64_t r = (int64_t)blockIdx.x * (kThreads / kLanes) + slot; r < a.samples; r += (int64_t)gridDim.x * (kThreads / kLanes)) {
+    float x[kVecs][T::E], j[kVecs][T::E];
+    load_rows<T>(a.X, r * sp.rows, a.ld_x, sp.f, c0, row, x);
+    load_rows<T>(a.J_out, r * sp.rows, a.ld_j_out, sp.f, c0, row, j);
+    row_sync<kLanes>();                            // the sample before is done with its values
+    for (int g = lane; g < sp.groups; g += kLanes) {
+      mu[g] = a.mean[r * sp.groups + g];
+      rs[g] = a.rstd[r * sp.groups + g];
+    }
+    row_sync<kLanes>();
+#pragma unroll
+    for (int i = 0; i < kVecs; ++i) {
+      if (c0[i] >= sp.f) continue;
+      float gm[T::E], gr[T::E], ga[T::E], be[T::E], u[T::E];
+      of_groups<T>(sp, c0[i], mu, rs, gm, gr);
+      from_lds<T>(params + c0[i], ga);
+      from_lds<T>(params + wide + c0[i], be);
+#pragma unroll
+      for (int e = 0; e < T::E; ++e) {
+        x[i][e] = normed(x[i][e], gm[e], gr[e]);
+        u[e] = affine(x[i][e], ga[e], be[e]);
+      }
+      times_slope(j[i], u, a.act);
+#pragma unroll
+      for (int e = 0; e < T::E; ++e) {
+        if (c0[i] + e >= sp.f) j[i][e] = x[i][e] = 0.f;
+        s1[i][e] += j[i][e];
+        s2[i][e] += j[i][e] * x[i][e];
+        j[i][e] *= ga[e];
+      }
+      to_lds<T>(image + (lane + kLanes * i) * T::E, j[i]);
+      to_lds<T>(xhat + (lane + kLanes * i) * T::E, x[i]);
+    }
+    if (!a.J_in) continue;
+    row_sync<kLanes>();
+    for (int g0 = 0; g0 < sp.groups; g0 += teams) {
+      const int g = g0 + lane / sp.team;
+      float s = 0.f, q = 0.f;
+      if (g < sp.groups)
+        group_walk(sp, wide, g, t, [&](int at) {
+          const float v = image[at];
+          s += v;
+          q += v * xhat[at];
+        });
+      s = team_sum(s, sp.team) * inv_n;
+      q = team_sum(q, sp.team) * inv_n;
+      if (g < sp.groups && t == 0) {
+        c1[g] = s;
+        c2[g] = q;
+      }
+    }
+    row_sync<kLanes>();
+#pragma unroll
+    for (int i = 0; i < kVecs; ++i) {
+      if (c0[i] >= sp.f) continue;
+      float g1[T::E], g2[T::E], gm[T::E], gr[T::E], xv[T::E], jv[T::E];
+      of_groups<T>(sp, c0[i], c1, c2, g1, g2);
+      of_groups<T>(sp, c0[i], mu, rs, gm, gr);
+      from_lds<T>(image + (lane + kLanes * i) * T::E, jv);
+      from_lds<T>(xhat + (lane + kLanes * i) * T::E, xv);
+#pragma unroll
+      for (int e = 0; e < T::E; ++e) xv[e] = gr[e] * (jv[e] - g1[e] - xv[e] * g2[e]);
+      store_some<T>((typename T::type *)a.J_in + (r * sp.rows + row[i]) * a.ld_j_in + c0[i], xv, sp.f - c0[i]);
     }
   }
   if (!part) return;
-  // join the workgroup's row slots (fixed order), each half of the sums in turn
-  constexpr int kSlots = kThreads / kLanes;
-  float *p = part + (int64_t)blockIdx.x * 2 * sp.f;
-#pragma unroll
-  for (int half = 0; half < 2; ++half) {
-#pragma unroll
-    for (int i = 0; i < kVecs; ++i) {
-      float v[T::E];
-#pragma unroll
-      for (int e = 0; e < T::E; ++e) v[e] = half ? s2[i][e] : s1[i][e];
-      if (kSlots > 1) {
-        __syncthreads();
-#pragma unroll
-        for (int e = 0; e < T::E; ++e) lds_all[e * kThreads + threadIdx.x] = v[e];
-        __syncthreads();
-        if (slot == 0) {
-#pragma unroll
-          for (int e = 0; e < T::E; ++e)
-            for (int k = 1; k < kSlots; ++k) v[e] += lds_all[e * kThreads + k * kLanes + lane];
-        }
-      }
-      const int c0 = (lane + kLanes * i) * T::E;
-      if (slot == 0)
-#pragma unroll
-        for (int e = 0; e < T::E; ++e)
-          if (c0 + e < sp.f) p[half * sp.f + c0 + e] = v[e];
-    }
-  }
+  __syncthreads();
+  write_channel_sums<T, kLanes>(sp, c0, s1, s2, part + (int64_t)blockIdx.x * 2 * sp.f, lds_any);
 }
 
 // part[n][2][channels] summed over n.
@@ -874,26 +1094,52 @@ int launch_param_grads(const float *part, int64_t n, int channels, float *dgamma
 
 bool is_pow2(int x) { return (x & (x - 1)) == 0; }
 
-RowShape row_shape(int32_t dtype, int32_t f, int32_t groups, int lanes) {
+constexpr int kRowElems = 32 * kThreads;          // of the largest sample that fits: 8 fp32 or 4 bf16 vectors to a thread
+
+RowShape row_shape(int32_t dtype, int32_t f, int32_t groups, int64_t sample_rows) {
   const int e = dtype == PGCN_BF16 ? BF16::E : F32::E;
   RowShape sp;
   sp.f = f;
   sp.groups = groups;
   sp.cg = f / groups;
   sp.vecs = (f + e - 1) / e;
-  sp.span = sp.cg % e == 0 ? sp.cg / e : 0;
-  sp.team = 1;
-  while (sp.team < 64 && 2 * sp.team * groups <= lanes) sp.team *= 2;
+  sp.rows = (int)sample_rows;
+  sp.all = sp.vecs * sp.rows;
+  sp.span = sp.rows == 1 && sp.cg % e == 0 ? sp.cg / e : 0;
   sp.magic = group_magic(sp.cg);
+  sp.team = 1;
   return sp;
 }
 
-// Threads and vectors a row: the fewest lanes that hold it in one vector each, a wave up to 4,
-// then a workgroup.
-void row_threads(int vecs, int &lanes, int &per) {
-  lanes = vecs <= 16 ? 16 : vecs <= 32 ? 32 : vecs <= 256 ? 64 : kThreads;
+// Whether lanes shuffle a group's sum, or all add up one.
+bool plain_groups(const RowShape &sp, int lanes) {
+  return sp.groups == 1 || (sp.span > 0 && is_pow2(sp.span) && sp.span <= std::min(lanes, 64));
+}
+
+constexpr int kMaxLds = 150 << 10;      // of a compute unit's 160 KB
+
+// Threads and vectors of a sample: the fewest lanes that hold it in one vector each, a wave up to
+// two, then a workgroup up to kRowElems.  us of 30,000 rows, a wave of four vectors and a workgroup
+// of one: forward / backward of 1,024 fp32 channels 53 / 91 and 50 / 80, of 2,048 bf16 ones
+// 94 / 271 and 65 / 111.  A wave of two and a workgroup of one half idle: 100,000 x 300 fp32 in four
+// groups 108 / 191 and 249 / 258.
+// false: the sample goes in chunks.  us here and in chunks, forward / backward: 100,000 x 4 x 64 in
+// 8 groups 80 / 95 and 564 / 1,364; 5,000 x 32 x 100 in 5 groups 39 / 91 and 55 / 129.  Groups of
+// several rows pay for LDS by the element and fp32 chunks win from 4,096 elements on: 5,000 x
+// 64 x 96 fp32 87 / 207 and 79 / 161, but bf16 68 / 158 and 91 / 203.
+bool row_threads(int32_t dtype, int32_t f, int32_t groups, int64_t sample_rows, int images, RowShape &sp, int &lanes, int &per, bool &plain) {
+  const int e = dtype == PGCN_BF16 ? BF16::E : F32::E;
+  if (sample_rows > kRowElems || (f + e - 1) / e * e * sample_rows > kRowElems) return false;
+  sp = row_shape(dtype, f, groups, sample_rows);
+  const int vecs = sp.all;
+  lanes = vecs <= 4 ? 4 : vecs <= 8 ? 8 : vecs <= 16 ? 16 : vecs <= 32 ? 32 : vecs <= 128 ? 64 : kThreads;
+  plain = plain_groups(sp, lanes);
+  if (!plain) lanes = std::max(lanes, 8);
   per = 1;
   while (lanes * per < vecs) per *= 2;
+  while (sp.team < 64 && 2 * sp.team * sp.groups <= lanes) sp.team *= 2;
+  if (plain) return true;
+  return (sample_rows == 1 || per <= 4) && 4 * any_lds(sp, e, kThreads / lanes, images) <= kMaxLds;
 }
 
 constexpr int kRowBlocksFwd = 2048, kRowBlocksBwd = 1024;
@@ -903,63 +1149,79 @@ unsigned row_blocks(int64_t rows, int lanes, int most) {
   return (unsigned)std::min<int64_t>(b, most);
 }
 
+// LDS bytes of a backward: the sums' join, and what the kernel itself takes.
+template <class T>
+size_t join_lds(const RowShape &sp, int lanes) {
+  return 4 * (size_t)(sp.rows > 1 ? kThreads / lanes * sp.all * T::E : kThreads * T::E);
+}
+
 template <class T, int kLanes, int kVecs, Sum kSum>
-int rows_fwd_go(const pgcn_group_norm_fwd_args &a, const RowShape &sp, hipStream_t s) {
-  const int row = kSum == Sum::LDS ? (sp.f + 3) / 4 * 4 + (sp.groups + 3) / 4 * 4 : 4;
-  hipLaunchKernelGGL((rows_fwd_kernel<T, kLanes, kVecs, kSum>), dim3(row_blocks(a.samples, kLanes, kRowBlocksFwd)), dim3(kThreads),
-                     (size_t)(kThreads / kLanes) * row * 4, s, a, sp, row);
+int rows_go(const pgcn_group_norm_fwd_args &a, const RowShape &sp, hipStream_t s) {
+  hipLaunchKernelGGL((rows_fwd_kernel<T, kLanes, kVecs, kSum>), dim3(row_blocks(a.samples, kLanes, kRowBlocksFwd)), dim3(kThreads), 0, s, a,
+                     sp);
   PGCN_HIP(hipGetLastError());
   return PGCN_OK;
 }
 
 template <class T, int kLanes, int kVecs, Sum kSum>
-int rows_bwd_go(const pgcn_group_norm_bwd_args &a, const RowShape &sp, hipStream_t s) {
-  const int row = kSum == Sum::LDS ? (sp.f + 3) / 4 * 4 + (sp.groups + 3) / 4 * 4 : 4;
+int rows_go(const pgcn_group_norm_bwd_args &a, const RowShape &sp, hipStream_t s) {
   const unsigned blocks = row_blocks(a.samples, kLanes, kRowBlocksBwd);
   float *part = a.dgamma || a.dbeta ? (float *)a.workspace : nullptr;
   if (!part && !a.J_in) return PGCN_OK;
-  const size_t lds = std::max((size_t)(kThreads / kLanes) * row, (size_t)(kThreads * T::E)) * 4;
-  hipLaunchKernelGGL((rows_bwd_kernel<T, kLanes, kVecs, kSum>), dim3(blocks), dim3(kThreads), lds, s, a, sp, row, part);
+  hipLaunchKernelGGL((rows_bwd_kernel<T, kLanes, kVecs, kSum>), dim3(blocks), dim3(kThreads), join_lds<T>(sp, kLanes), s, a, sp, part);
   PGCN_HIP(hipGetLastError());
   return part ? launch_param_grads(part, blocks, a.channels, a.dgamma, a.dbeta, s) : PGCN_OK;
 }
 
-#define PGCN_ROW_SHAPES(go, T, a, s)                                                                              \
-  int lanes, per;                                                                                                 \
-  row_threads((a.channels + T::E - 1) / T::E, lanes, per);                                                        \
-  const RowShape sp = row_shape(a.dtype, a.channels, a.groups, lanes);                                            \
-  const int how = sp.groups == 1 ? 0 : sp.span > 0 && is_pow2(sp.span) && sp.span <= lanes && lanes <= 64 ? 1 : 2; \
-  switch (lanes * 100 + per * 10 + how) {                                                                         \
-    case 1610: return go<T, 16, 1, Sum::ROW>(a, sp, s);                                                           \
-    case 1611: return go<T, 16, 1, Sum::LANES>(a, sp, s);                                                         \
-    case 1612: return go<T, 16, 1, Sum::LDS>(a, sp, s);                                                           \
-    case 3210: return go<T, 32, 1, Sum::ROW>(a, sp, s);                                                           \
-    case 3211: return go<T, 32, 1, Sum::LANES>(a, sp, s);                                                         \
-    case 3212: return go<T, 32, 1, Sum::LDS>(a, sp, s);                                                           \
-    case 6410: return go<T, 64, 1, Sum::ROW>(a, sp, s);                                                           \
-    case 6411: return go<T, 64, 1, Sum::LANES>(a, sp, s);                                                         \
-    case 6412: return go<T, 64, 1, Sum::LDS>(a, sp, s);                                                           \
-    case 6420: return go<T, 64, 2, Sum::ROW>(a, sp, s);                                                           \
-    case 6421: return go<T, 64, 2, Sum::LANES>(a, sp, s);                                                         \
-    case 6422: return go<T, 64, 2, Sum::LDS>(a, sp, s);                                                           \
-    case 6440: return go<T, 64, 4, Sum::ROW>(a, sp, s);                                                           \
-    case 6441: return go<T, 64, 4, Sum::LANES>(a, sp, s);                                                         \
-    case 6442: return go<T, 64, 4, Sum::LDS>(a, sp, s);                                                           \
-    case 25620: return go<T, 256, 2, Sum::ROW>(a, sp, s);                                                         \
-    case 25622: return go<T, 256, 2, Sum::LDS>(a, sp, s);                                                         \
-    case 25640: return go<T, 256, 4, Sum::ROW>(a, sp, s);                                                         \
-    case 25642: return go<T, 256, 4, Sum::LDS>(a, sp, s);                                                         \
-    case 25680: return go<T, 256, 8, Sum::ROW>(a, sp, s);                                                         \
-    default: return go<T, 256, 8, Sum::LDS>(a, sp, s);                                                            \
-  }
-
-template <class T>
-int rows_fwd(const pgcn_group_norm_fwd_args &a, hipStream_t s) {
-  PGCN_ROW_SHAPES(rows_fwd_go, T, a, s)
+template <class T, int kLanes, int kVecs>
+int any_go(const pgcn_group_norm_fwd_args &a, const RowShape &sp, hipStream_t s) {
+  hipLaunchKernelGGL((any_fwd_kernel<T, kLanes, kVecs>), dim3(row_blocks(a.samples, kLanes, kRowBlocksFwd)), dim3(kThreads),
+                     4 * (size_t)any_lds(sp, T::E, kThreads / kLanes, 1), s, a, sp);
+  PGCN_HIP(hipGetLastError());
+  return PGCN_OK;
 }
-template <class T>
-int rows_bwd(const pgcn_group_norm_bwd_args &a, hipStream_t s) {
-  PGCN_ROW_SHAPES(rows_bwd_go, T, a, s)
+
+template <class T, int kLanes, int kVecs>
+int any_go(const pgcn_group_norm_bwd_args &a, const RowShape &sp, hipStream_t s) {
+  const unsigned blocks = row_blocks(a.samples, kLanes, kRowBlocksBwd);
+  float *part = a.dgamma || a.dbeta ? (float *)a.workspace : nullptr;
+  if (!part && !a.J_in) return PGCN_OK;
+  const size_t lds = std::max(4 * (size_t)any_lds(sp, T::E, kThreads / kLanes, 2), join_lds<T>(sp, kLanes));
+  hipLaunchKernelGGL((any_bwd_kernel<T, kLanes, kVecs>), dim3(blocks), dim3(kThreads), lds, s, a, sp, part);
+  PGCN_HIP(hipGetLastError());
+  return part ? launch_param_grads(part, blocks, a.channels, a.dgamma, a.dbeta, s) : PGCN_OK;
+}
+
+// The kernel of a sample's shape; `args` forward or backward.
+template <class T, class Args>
+int rows_of(const Args &a, const RowShape &sp, int lanes, int per, bool plain, hipStream_t s) {
+  constexpr int kMost = T::E == 4 ? 8 : 4;
+  if (!plain) {
+    switch (lanes * 10 + per) {
+      case 81: return any_go<T, 8, 1>(a, sp, s);
+      case 161: return any_go<T, 16, 1>(a, sp, s);
+      case 321: return any_go<T, 32, 1>(a, sp, s);
+      case 641: return any_go<T, 64, 1>(a, sp, s);
+      case 642: return any_go<T, 64, 2>(a, sp, s);
+      case 2561: return any_go<T, 256, 1>(a, sp, s);
+      case 2562: return any_go<T, 256, 2>(a, sp, s);
+      case 2564: return any_go<T, 256, 4>(a, sp, s);
+      default: return any_go<T, 256, kMost>(a, sp, s);
+    }
+  }
+  const bool one = sp.groups == 1;
+  switch (lanes * 10 + per) {
+    case 41: return one ? rows_go<T, 4, 1, Sum::ROW>(a, sp, s) : rows_go<T, 4, 1, Sum::LANES>(a, sp, s);
+    case 81: return one ? rows_go<T, 8, 1, Sum::ROW>(a, sp, s) : rows_go<T, 8, 1, Sum::LANES>(a, sp, s);
+    case 161: return one ? rows_go<T, 16, 1, Sum::ROW>(a, sp, s) : rows_go<T, 16, 1, Sum::LANES>(a, sp, s);
+    case 321: return one ? rows_go<T, 32, 1, Sum::ROW>(a, sp, s) : rows_go<T, 32, 1, Sum::LANES>(a, sp, s);
+    case 641: return one ? rows_go<T, 64, 1, Sum::ROW>(a, sp, s) : rows_go<T, 64, 1, Sum::LANES>(a, sp, s);
+    case 642: return one ? rows_go<T, 64, 2, Sum::ROW>(a, sp, s) : rows_go<T, 64, 2, Sum::LANES>(a, sp, s);
+    case 2561: return one ? rows_go<T, 256, 1, Sum::ROW>(a, sp, s) : rows_go<T, 256, 1, Sum::LANES>(a, sp, s);
+    case 2562: return one ? rows_go<T, 256, 2, Sum::ROW>(a, sp, s) : rows_go<T, 256, 2, Sum::LANES>(a, sp, s);
+    case 2564: return one ? rows_go<T, 256, 4, Sum::ROW>(a, sp, s) : rows_go<T, 256, 4, Sum::LANES>(a, sp, s);
+    default: return one ? rows_go<T, 256, kMost, Sum::ROW>(a, sp, s) : rows_go<T, 256, kMost, Sum::LANES>(a, sp, s);
+  }
 }
 
 // ---- launches: samples of many rows ----------------------------------------
@@ -1008,12 +1270,11 @@ int chunks_bwd(const pgcn_group_norm_bwd_args &a, hipStream_t s) {
 
 size_t group_norm_workspace(int32_t dtype, int32_t channels, int32_t groups, int64_t samples, int64_t sample_rows) {
   if (samples == 0) return 0;
-  if (sample_rows == 1) {
-    int lanes, per;
-    const int e = dtype == PGCN_BF16 ? BF16::E : F32::E;
-    row_threads((channels + e - 1) / e, lanes, per);
+  RowShape sp;
+  int lanes, per;
+  bool plain;
+  if (row_threads(dtype, channels, groups, sample_rows, 2, sp, lanes, per, plain))
     return 8 * (size_t)channels * row_blocks(samples, lanes, kRowBlocksBwd);
-  }
   const Cut cut = cut_rows(dtype, channels, groups, samples, sample_rows);
   return group_part_bytes(cut, groups, samples) + 8 * (size_t)channels * (size_t)chunk_sum_blocks(cut, samples);
 }
@@ -1021,13 +1282,21 @@ size_t group_norm_workspace(int32_t dtype, int32_t channels, int32_t groups, int
 int launch_group_norm_fwd(const pgcn_group_norm_fwd_args &a, hipStream_t s) {
   if (a.samples == 0) return PGCN_OK;
   TraceScope ts(PGCN_TK_GROUP_NORM, s);
-  if (a.sample_rows == 1) return a.dtype == PGCN_BF16 ? rows_fwd<BF16>(a, s) : rows_fwd<F32>(a, s);
+  RowShape sp;
+  int lanes, per;
+  bool plain;
+  if (row_threads(a.dtype, a.channels, a.groups, a.sample_rows, 1, sp, lanes, per, plain))
+    return a.dtype == PGCN_BF16 ? rows_of<BF16>(a, sp, lanes, per, plain, s) : rows_of<F32>(a, sp, lanes, per, plain, s);
   return a.dtype == PGCN_BF16 ? chunks_fwd<BF16>(a, s) : chunks_fwd<F32>(a, s);
 }
 
 int launch_group_norm_bwd(const pgcn_group_norm_bwd_args &a, hipStream_t s) {
   TraceScope ts(PGCN_TK_GROUP_NORM_BWD, s);
-  if (a.sample_rows == 1 && a.samples > 0) return a.dtype == PGCN_BF16 ? rows_bwd<BF16>(a, s) : rows_bwd<F32>(a, s);
+  RowShape sp;
+  int lanes, per;
+  bool plain;
+  if (a.samples > 0 && row_threads(a.dtype, a.channels, a.groups, a.sample_rows, 2, sp, lanes, per, plain))
+    return a.dtype == PGCN_BF16 ? rows_of<BF16>(a, sp, lanes, per, plain, s) : rows_of<F32>(a, sp, lanes, per, plain, s);
   return a.dtype == PGCN_BF16 ? chunks_bwd<BF16>(a, s) : chunks_bwd<F32>(a, s);
 }
 

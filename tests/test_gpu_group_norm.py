@@ -157,7 +157,10 @@ SHAPES = [(1, 1, 1, 1), (1, 1, 32, 4), (37, 1, 8, 2), (1000, 1, 256, 1), (513, 1
           (50, 1, 300, 4), (9, 1, 300, 100), (21, 1, 512, 512), (5, 1, 2048, 1), (7, 1, 2052, 3), (3, 1, 8192, 32), (2, 1, 8191, 1),
           (2, 7, 16, 4), (3, 64, 320, 32), (5, 33, 60, 5), (1, 5000, 256, 8), (2, 1025, 7, 1), (40, 3, 130, 13), (1, 3001, 1, 1),
           (4, 256, 1000, 8), (600, 2, 24, 3), (2, 500, 2100, 7), (1, 40, 8192, 2), (17, 100, 4, 2), (2, 9, 8192, 8192),
-          (1500, 5, 16, 2), (1, 3000, 257, 257), (1, 2000, 24, 3)]
+          (1500, 5, 16, 2), (700, 2, 4, 4), (90, 3, 1, 1), (33, 128, 64, 4), (20, 32, 256, 1), (7, 30, 260, 4), (9, 8, 1000, 8),
+          (3, 2, 4096, 64), (3, 8192, 1, 1), (2, 2049, 4, 2), (5, 129, 64, 4), (2500, 1, 16, 16), (1300, 1, 12, 3), (37, 1, 4100, 4), (1, 3000, 257, 257), (1, 2000, 24, 3),
+          (3, 1, 8000, 5), (3, 1, 8192, 8192), (300, 1, 300, 4), (5, 1, 1200, 2), (5, 1, 2048, 4), (9, 1, 1024, 4), (3, 1, 6000, 1), (2, 1, 5000, 50),
+          (70, 2, 100, 25), (3, 1, 4096, 4096), (3, 4, 2000, 8)]
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
