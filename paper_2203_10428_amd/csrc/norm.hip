@@ -998,8 +998,12 @@ __global__ __launch_bounds__(kThreads, kVecs * T::E <= 16 ? 4 : 2) void any_fwd_
   }
 }
 
+// Four waves to a SIMD are worth the four registers spilt outside the loop (128 of 136), us at three
+// and at four: 100,000 x 300 in 4 groups fp32 189 and 135, bf16 157 and 123; 10,000 x 2 x 1,024 in
+// 8 groups 98 and 69, 82 and 61.
 template <class T, int kLanes, int kVecs>
-__global__ __launch_bounds__(kThreads, kVecs * T::E <= 4 ? 4 : kVecs * T::E <= 8 ? 3 : kVecs * T::E <= 16 ? 2 : 1) void any_bwd_kernel(pgcn_group_norm_bwd_args a, RowShape sp, float *part) {
+__global__ __launch_bounds__(kThreads, kVecs * T::E <= 8 ? 4 : kVecs * T::E <= 16 ? 2 : 1) void any_bwd_kernel(
+    pgcn_group_norm_bwd_args a, RowShape sp, float *part) {
   extern __shared__ __align__(16) float lds_any[];
   const int lane = threadIdx.x % kLanes, slot = threadIdx.x / kLanes, wide = sp.vecs * T::E;
   const float *params = lds_any;
@@ -1122,7 +1126,7 @@ constexpr int kMaxLds = 150 << 10;      // of a compute unit's 160 KB
 // two, then a workgroup up to kRowElems.  us of 30,000 rows, a wave of four vectors and a workgroup
 // of one: forward / backward of 1,024 fp32 channels 53 / 91 and 50 / 80, of 2,048 bf16 ones
 // 94 / 271 and 65 / 111.  A wave of two and a workgroup of one half idle: 100,000 x 300 fp32 in four
-// groups 108 / 191 and 249 / 258.
+// groups 108 / 135 and 249 / 258.
 // false: the sample goes in chunks.  us here and in chunks, forward / backward: 100,000 x 4 x 64 in
 // 8 groups 80 / 95 and 564 / 1,364; 5,000 x 32 x 100 in 5 groups 39 / 91 and 55 / 129.  Groups of
 // several rows pay for LDS by the element and fp32 chunks win from 4,096 elements on: 5,000 x
