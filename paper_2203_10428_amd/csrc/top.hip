@@ -10,6 +10,10 @@
 //     Where too many reach it (ties, sorted rows) the threshold is bisected, and among equal
 //     values the class;
 //   - few rows, and rows longer than that: parts of a row first, then the lists of its parts.
+// The log-sum is one more pass over the registers, with no test for what is listed: an exponential's
+// clamp makes 1 of each listed one, and their number is taken off the sum.
+// The instructions for an element (unpack, maximum, compare, product-sum, exponential, sum) bound bf16:
+// 2,048 x 65,536 top 64 fp32 151 us, 3.6 TB/s, bf16 126 us, 2.1 TB/s.
 #include <algorithm>
 #include <cfloat>
 
@@ -116,7 +120,7 @@ __device__ __forceinline__ float reached_by(float v, int r) {
 }
 
 template <class T, int kThreads, int kVecs>
-__global__ __launch_bounds__(kThreads < 256 ? 256 : kThreads, kVecs <= 2 ? 8 : kVecs == 16 ? 4 : kVecs == 4 || T::E == 4 ? 7 : 5) void top_unit_kernel(TopArgs a) {
+__global__ __launch_bounds__(kThreads < 256 ? 256 : kThreads, kVecs <= 2 ? 8 : kVecs == 4 || T::E == 4 ? 7 : 5) void top_unit_kernel(TopArgs a) {
   constexpr int kUnits = kThreads < 256 ? 256 / kThreads : 1, kWaves = kThreads / 64;
   __shared__ TopLds<kThreads> lds[kUnits];
   const int lane = threadIdx.x % kThreads, slot = threadIdx.x / kThreads;
@@ -133,7 +137,7 @@ __global__ __launch_bounds__(kThreads < 256 ? 256 : kThreads, kVecs <= 2 ? 8 : k
     const int c0 = (lane + kThreads * i) * T::E;
     raw[i] = c0 < n_all ? *reinterpret_cast<const typename T::raw *>(z + c0) : typename T::raw{};
   }
-  float top = kNegInf;                             // a NaN is no maximum
+  float top = kNegInf;
 #pragma unroll
   for (int i = 0; i < kVecs; ++i) {
     const int c0 = (lane + kThreads * i) * T::E;
@@ -146,8 +150,19 @@ __global__ __launch_bounds__(kThreads < 256 ? 256 : kThreads, kVecs <= 2 ? 8 : k
       raw[i] = T::pack(x);
     }
 #pragma unroll
-    for (int e = 0; e < T::E; ++e) top = fmaxf(top, x[e]);
+    for (int e = 0; e < T::E; ++e) top = __builtin_elementwise_maximum(top, x[e]);      // a NaN passes on
     __builtin_amdgcn_sched_barrier(0);
+  }
+  const bool nan = top != top;
+  if (__ballot(nan)) {                             // and is no maximum
+    top = kNegInf;
+#pragma unroll
+    for (int i = 0; i < kVecs; ++i) {
+      float x[T::E];
+      T::unpack(raw[i], x);
+#pragma unroll
+      for (int e = 0; e < T::E; ++e) top = fmaxf(top, x[e]);
+    }
   }
 
   int turn = 0;
@@ -297,19 +312,13 @@ __global__ __launch_bounds__(kThreads < 256 ? 256 : kThreads, kVecs <= 2 ? 8 : k
   // the others: below the last listed value, and what equals it and is not listed
   unit_sync<kThreads>();
   const float scale = a.inv_t * kLog2e;
-  float last = -FLT_MAX;                           // all above -inf are listed
-  if (n >= K) {
-    const uint64_t key = l.last;
-    last = value_of((uint32_t)(key >> 32));
-    for (int j = lane; j < n; j += kThreads)
-      if (l.list[j] < key && (l.list[j] >> 32) == (key >> 32)) atomicAdd(&l.ties, 1);
-    unit_sync<kThreads>();
-    ties += l.ties;
-  }
-  float m = last;                                  // no exponent is above 0
+  const float last = n >= K ? value_of((uint32_t)(l.last >> 32)) : -FLT_MAX;       // all above -inf are listed
+  float m = last;                                  // no exponent of the others is above 0
   float s = 0.f;
-  auto rest = [&](float base) {
-    const Exps ex(base, scale);
+  if (last <= FLT_MAX && n_all > 2 * K) {
+    // all of them, each at most 1: the listed ones count for 1, which the sum holds exactly.  Where
+    // they are not most of it, taking them off again loses no more than a bit.
+    const Exps ex(m, scale);
     float s0 = 0.f, s1 = 0.f;
     keep_packed(raw);
 #pragma unroll
@@ -317,13 +326,22 @@ __global__ __launch_bounds__(kThreads < 256 ? 256 : kThreads, kVecs <= 2 ? 8 : k
       float x[T::E];
       T::unpack(raw[i], x);
 #pragma unroll
-      for (int e = 0; e < T::E; ++e) (e % 2 ? s1 : s0) += ex.raw(x[e] >= last ? kNegInf : x[e]);
+      for (int e = 0; e < T::E; ++e) (e % 2 ? s1 : s0) += __builtin_amdgcn_fmed3f(ex.raw(x[e]), 0.f, 1.f);
       __builtin_amdgcn_sched_barrier(0);
     }
-    return waves_all<kThreads>(lanes_sum<64>((s0 + s1) * ex.fix), l, turn, [](float x, float y) { return x + y; });
-  };
-  if (last <= FLT_MAX) s = rest(m) + (float)ties;
-  if (s < 0x1p-80f) {                              // all far below it, or nothing: take their own maximum
+    if (nan) s0 = __builtin_nanf("");
+    s = waves_all<kThreads>(lanes_sum<64>(s0 + s1), l, turn, [](float x, float y) { return x + y; });
+    const float listed = (float)(n < K ? n : K);
+    s = s - listed < listed ? 0.f : (s - listed) * ex.fix;
+  }
+  if (s == 0.f) {                                  // the others alone, from their own maximum
+    if (n >= K) {                                  // those equal to the last listed one
+      const uint64_t key = l.last;
+      for (int j = lane; j < n; j += kThreads)
+        if (l.list[j] < key && (l.list[j] >> 32) == (key >> 32)) atomicAdd(&l.ties, 1);
+      unit_sync<kThreads>();
+      ties += l.ties;
+    }
     m = kNegInf;
 #pragma unroll
     for (int i = 0; i < kVecs; ++i) {
@@ -332,11 +350,20 @@ __global__ __launch_bounds__(kThreads < 256 ? 256 : kThreads, kVecs <= 2 ? 8 : k
 #pragma unroll
       for (int e = 0; e < T::E; ++e) m = fmaxf(m, x[e] >= last ? kNegInf : x[e]);
     }
-    m = waves_all<kThreads>(lanes_max<64>(m), l, turn, [](float x, float y) { return fmaxf(x, y); });
-    s = rest(m == kNegInf ? 0.f : m);
-    if (ties && s == s) {                          // an infinity that is not listed
-      m = INFINITY;
-      s = 1.f;
+    m = waves_all<kThreads>(lanes_max<64>(ties ? last : m), l, turn, [](float x, float y) { return fmaxf(x, y); });
+    const Exps ex(fabsf(m) <= FLT_MAX ? m : 0.f, scale);
+    float s0 = 0.f;
+#pragma unroll
+    for (int i = 0; i < kVecs; ++i) {
+      float x[T::E];
+      T::unpack(raw[i], x);
+#pragma unroll
+      for (int e = 0; e < T::E; ++e) s0 += ex.raw(x[e] >= last ? kNegInf : x[e]);
+    }
+    s = waves_all<kThreads>(lanes_sum<64>(s0 * ex.fix), l, turn, [](float x, float y) { return x + y; });
+    if (s == s) {
+      if (m == INFINITY) s = 1.f;                  // an infinity that is not listed
+      else s += (float)ties;
     }
   }
   if (threadIdx.x % kThreads >= 64) return;
@@ -477,14 +504,20 @@ __global__ __launch_bounds__(256) void top_lists_kernel(pgcn_top_logits_args a) 
 
 int vector_elems(int32_t dtype) { return dtype == PGCN_BF16 ? BF16::E : F32::E; }
 
-constexpr int kPartThreads = 256, kPartVecs = 4;
-// Vectors of the longest row that a workgroup holds.
-int long_vecs(int32_t dtype) { return dtype == PGCN_BF16 ? 4096 : 8192; }
+// Vectors of the longest row that a workgroup holds: the register file's limit in bf16; 4,096 x 32,768
+// fp32 top 8 whole 148 us, in parts 129, top 64 both 162.
+constexpr int kLongVecs = 4096;
+constexpr int kFewRows = 128;
+
+// Elements of a part of a row: short ones fill the chip when rows are few, long ones share the cost
+// of a part's threshold.  1,024 and 2,048 vectors, us of 2,048 x 65,536: fp32 top 8 157 and 126,
+// top 64 206 and 151, top 256 562 and 420; bf16 top 64 131 and 126, top 256 365 and 278.
+int part_range(int32_t dtype, int64_t rows) { return (rows <= kFewRows ? 1024 : 2048) * vector_elems(dtype); }
 
 // Parts of a row, 1: the whole of it at once.
 int top_parts(int32_t dtype, int64_t rows, int32_t classes) {
-  const int64_t range = (int64_t)kPartThreads * kPartVecs * vector_elems(dtype), parts = (classes + range - 1) / range;
-  return parts > long_vecs(dtype) / (kPartThreads * kPartVecs) || (rows <= 128 && parts >= 4) ? (int)parts : 1;
+  const int range = part_range(dtype, rows), parts = (classes + range - 1) / range;
+  return classes > kLongVecs * vector_elems(dtype) || (rows <= kFewRows && parts >= 4) ? parts : 1;
 }
 
 // Whether a thread takes a row: fits to both kernels' times, in us.  A thread's walk is a chain, so few
@@ -526,8 +559,7 @@ int units(const TopArgs &a, hipStream_t s) {
     return unit_go<T, 256, 8>(a, s);
   }
   if (vecs <= 2048) return unit_go<T, 512, 4>(a, s);
-  if (T::E == 8 || vecs <= 4096) return unit_go<T, 512, 8>(a, s);
-  return unit_go<T, 512, T::E == 8 ? 8 : 16>(a, s);
+  return unit_go<T, 512, 8>(a, s);
 }
 
 template <class T, int kSlots>
@@ -565,7 +597,7 @@ int top_go(const pgcn_top_logits_args &a, hipStream_t s) {
   t.ld = a.ld;
   t.classes = a.classes;
   t.top = t.fill = a.top;
-  t.range = parts > 1 ? kPartThreads * kPartVecs * T::E : a.classes;
+  t.range = parts > 1 ? part_range(a.dtype, a.rows) : a.classes;
   t.parts = parts;
   t.inv_t = 1.0f / a.temperature;
   t.values = a.top_values;
