@@ -688,8 +688,19 @@ template <class T, int kThreads, int kVecs>
 int long_go(const pgcn_distill_args &a, hipStream_t s) {
   double *part = (double *)a.workspace;
   const size_t lds = (size_t)((a.classes + 31) / 32) * 4;
-  hipLaunchKernelGGL((distill_long_kernel<T, kThreads, kVecs>), dim3((unsigned)a.rows), dim3(kThreads), lds, s, a, part);
-  PGCN_HIP(hipGetLastError());
+  const int64_t most = kMaxLaunch / kThreads;
+  for (int64_t row0 = 0; row0 < a.rows; row0 += most) {
+    pgcn_distill_args b = a;
+    b.rows = std::min(most, a.rows - row0);
+    b.Z = (const typename T::type *)a.Z + row0 * a.ld;
+    b.J = (typename T::type *)a.J + row0 * a.ld;
+    b.top_values += row0 * a.ld_top;
+    b.top_ids += row0 * a.ld_top;
+    if (b.tail_lse) b.tail_lse += row0;
+    if (b.labels) b.labels += row0;
+    hipLaunchKernelGGL((distill_long_kernel<T, kThreads, kVecs>), dim3((unsigned)b.rows), dim3(kThreads), lds, s, b, part + row0);
+    PGCN_HIP(hipGetLastError());
+  }
   hipLaunchKernelGGL(distill_sum_kernel, dim3(1), dim3(1024), 0, s, part, a.rows, a.loss_out);
   PGCN_HIP(hipGetLastError());
   return PGCN_OK;

@@ -6,6 +6,9 @@
 
 namespace pgcn {
 
+// Threads of one launch: grids are counted in 32 bits of threads.
+constexpr int64_t kMaxLaunch = int64_t(1) << 31;
+
 // ---- kernel launchers (arguments already checked by the entry points) ------
 int launch_top_logits(const pgcn_top_logits_args &a, hipStream_t s);
 size_t top_logits_workspace(int32_t dtype, int64_t rows, int32_t classes, int32_t top);

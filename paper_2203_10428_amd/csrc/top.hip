@@ -534,12 +534,23 @@ bool lists_taken(int64_t rows, int32_t classes, int32_t top) {
 }
 
 template <class T, int kThreads, int kVecs>
-int unit_go(const TopArgs &a, hipStream_t s) {
-  constexpr int kUnits = kThreads < 256 ? 256 / kThreads : 1;
-  const int64_t units = a.rows * a.parts;
-  hipLaunchKernelGGL((top_unit_kernel<T, kThreads, kVecs>), dim3((unsigned)((units + kUnits - 1) / kUnits)),
-                     dim3(kThreads < 256 ? 256 : kThreads), 0, s, a);
-  PGCN_HIP(hipGetLastError());
+int unit_go(const TopArgs &all, hipStream_t s) {
+  constexpr int kUnits = kThreads < 256 ? 256 / kThreads : 1, kBlock = kThreads < 256 ? 256 : kThreads;
+  const int64_t most = kMaxLaunch / kBlock * kUnits / all.parts;
+  for (int64_t row0 = 0; row0 < all.rows; row0 += most) {
+    TopArgs a = all;
+    a.rows = std::min(most, all.rows - row0);
+    a.Z = (const typename T::type *)all.Z + row0 * all.ld;
+    a.values += row0 * all.parts * all.ld_top;
+    a.ids += row0 * all.parts * all.ld_top;
+    if (a.tail) a.tail += row0;
+    if (a.part_tail) a.part_tail += row0 * all.parts;
+    if (a.listed_ids) a.listed_ids += row0 * all.ld;
+    if (a.listed_tails) a.listed_tails += row0 * all.tails;
+    const int64_t units = a.rows * a.parts;
+    hipLaunchKernelGGL((top_unit_kernel<T, kThreads, kVecs>), dim3((unsigned)((units + kUnits - 1) / kUnits)), dim3(kBlock), 0, s, a);
+    PGCN_HIP(hipGetLastError());
+  }
   return PGCN_OK;
 }
 

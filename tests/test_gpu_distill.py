@@ -146,6 +146,28 @@ def test_top_logits_many_short_rows():
             assert (t == NINF).all()
 
 
+def test_top_logits_of_more_rows_than_a_launch_holds():
+    """2^31 threads are 2^23 rows of 256: rows on both sides of that, and the last one."""
+    rows, C, K = 2 ** 23 + 3, 72, 66
+    rng = np.random.default_rng(7)
+    at = torch.tensor([0, 2 ** 23 - 1, 2 ** 23, rows - 1], device="cuda")
+    Z = torch.zeros((rows, C), dtype=torch.bfloat16, device="cuda")
+    Z[at] = torch.from_numpy(logits(rng, 4, C)).to("cuda").to(torch.bfloat16)
+    v = torch.empty((rows, K), device="cuda")
+    i = torch.empty((rows, K), dtype=torch.int32, device="cuda")
+    t = torch.empty(rows, device="cuda")
+    B.pgcn_top_logits(dtype=B.PGCN_BF16, rows=rows, classes=C, ld=C, top=K, ld_top=K, temperature=1.0, Z=Z, top_values=v, top_ids=i,
+                      tail_lse=t, workspace=None, workspace_bytes=0)
+    rv, ri, rt = ops.top_logits(Z[at].float().cpu().numpy().astype(np.float64), K, 1.0)
+    assert np.array_equal(i[at].cpu().numpy(), ri) and np.array_equal(v[at].cpu().numpy().astype(np.float64), rv)
+    assert (np.abs(t[at].cpu().numpy() - rt) <= log_error(4 * 10.0, rt)).all()
+    # all others are rows of zeros: the first K classes, the rest's logarithm
+    rest = torch.ones(rows, dtype=torch.bool, device="cuda")
+    rest[at] = False
+    assert bool(((i == torch.arange(K, dtype=torch.int32, device="cuda")).all(1) & (v == 0).all(1))[rest].all())
+    assert float((t[rest] - float(np.log(C - K))).abs().max()) <= log_error(0.0, np.log(C - K))
+
+
 def test_top_logits_without_a_tail():
     rng = np.random.default_rng(6)
     for rows, C, K in ((50, 41, 8), (3, 9000, 30), (1, 100003, 50)):
@@ -430,6 +452,43 @@ def test_distill_is_reproducible_on_any_stream_and_in_a_graph(rows, C, K):
         same()
         run(torch.cuda.current_stream())
         same()
+
+
+def test_distill_of_more_rows_than_a_launch_holds():
+    """2^31 threads are 2^23 rows of 256."""
+    rows, C, K = 2 ** 23 + 3, 2056, 2
+    if torch.cuda.mem_get_info()[0] < 90 << 30:
+        pytest.skip("needs 70 GiB of device memory")
+    rng = np.random.default_rng(8)
+    at = torch.tensor([0, 2 ** 23 - 1, 2 ** 23, rows - 1], device="cuda")
+    Z = torch.zeros((rows, C), dtype=torch.bfloat16, device="cuda")
+    Z[at] = torch.from_numpy(logits(rng, 4, C)).to("cuda").to(torch.bfloat16)
+    v = torch.zeros((rows, K), device="cuda")
+    i = torch.tensor([[3, 700]], dtype=torch.int32, device="cuda").repeat(rows, 1)
+    i[at] = torch.tensor([[5, 2055], [1, 9], [2000, 4], [0, 77]], dtype=torch.int32, device="cuda")
+    t = torch.full((rows,), float(np.log(C - K)), device="cuda")
+    y = torch.full((rows,), 11, dtype=torch.int32, device="cuda")
+    J = torch.full((rows, C), 3.0, dtype=torch.bfloat16, device="cuda")
+    loss = torch.empty(1, device="cuda")
+    n = B.pgcn_distill_workspace_size(B.PGCN_BF16, rows, C, K)
+    ws = torch.empty(n, dtype=torch.uint8, device="cuda")
+    B.pgcn_distill_loss_fwd_bwd(dtype=B.PGCN_BF16, rows=rows, classes=C, ld=C, top=K, ld_top=K, temperature=1.0, soft_scale=1.0,
+                                hard_scale=0.5, Z=Z, J=J, top_values=v, top_ids=i, tail_lse=t, labels=y, loss_out=loss, workspace=ws,
+                                workspace_bytes=n)
+    z = Z[at].float().cpu().numpy().astype(np.float64)
+    rl, rj = 0.0, np.zeros((4, C))
+    for k in range(4):
+        f, rj[k] = ops.distill_row(z[k], np.zeros(K), i[at[k]].cpu().numpy(), float(t[0]), 11, 1.0, 1.0, 0.5)
+        rl += f
+    got = J[at].float().cpu().numpy()
+    assert (np.abs(got - rj) <= np.abs(rj) * 2.0 ** -8 + log_error(40.0, 10.0) + 2.0 ** -126).all()
+    # every other row: teacher and student agree, the hard term is log C
+    want = (rows - 4) * 0.5 * np.log(C) + rl
+    assert abs(float(loss) - want) <= want * (U + log_error(0.0, np.log(C)) / (0.25 * np.log(C)))
+    q = 0.5 / C
+    rest = torch.ones(rows, dtype=torch.bool, device="cuda")
+    rest[at] = False
+    assert float((J[:, 12].float()[rest] - q).abs().max()) <= q * 2.0 ** -7
 
 
 def test_two_calls_at_once():
