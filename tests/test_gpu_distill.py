@@ -146,6 +146,21 @@ def test_top_logits_many_short_rows():
             assert (t == NINF).all()
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("C,K", [(16385, 64), (33000, 1), (40001, 256), (50000, 17)])
+def test_top_logits_of_many_long_rows(C, K, dtype):
+    rng = np.random.default_rng(C + K)
+    z = logits(rng, 131, C)
+    z[0, C - 1] = np.nan
+    z[1, 8] = z[1, C - 2] = np.inf
+    z[2] = 0.5                                # ties over the parts
+    z[3, 100:] = NINF
+    z[4] = -300.0 + 0.01 * z[4]               # the rest far below the list
+    z[4, :K] = 300.0
+    z[5, rng.random(C) < 0.999] = NINF
+    check_top(matrix(z, dtype), C, K, 0.9, dtype)
+
+
 def test_top_logits_of_more_rows_than_a_launch_holds():
     """2^31 threads are 2^23 rows of 256: rows on both sides of that, and the last one."""
     rows, C, K = 2 ** 23 + 3, 72, 66
