@@ -13,7 +13,7 @@
 // The log-sum is one more pass over the registers, with no test for what is listed: an exponential's
 // clamp makes 1 of each listed one, and their number is taken off the sum.
 // The instructions for an element (unpack, maximum, compare, product-sum, exponential, sum) bound bf16:
-// 2,048 x 65,536 top 64 fp32 151 us, 3.6 TB/s, bf16 126 us, 2.1 TB/s.
+// 2,048 x 65,536 top 64 fp32 151 us, 3.6 TB/s, bf16 109 us, 2.5 TB/s; top 8 126 and 83 us.
 #include <algorithm>
 #include <cfloat>
 
@@ -119,8 +119,11 @@ __device__ __forceinline__ float reached_by(float v, int r) {
   return value_of(lo);
 }
 
+// Waves to a SIMD: as many as spill (next to) nothing.  8 vectors of bf16 at five waves, 15 registers
+// spilt, and at four: 2,048 x 65,536 top 8 111 and 83 us, 4,096 x 32,768 122 and 90.
 template <class T, int kThreads, int kVecs>
-__global__ __launch_bounds__(kThreads < 256 ? 256 : kThreads, kVecs <= 2 ? 8 : kVecs == 4 || T::E == 4 ? 7 : 5) void top_unit_kernel(TopArgs a) {
+__global__ __launch_bounds__(kThreads < 256 ? 256 : kThreads, kVecs <= 2 ? 8 : T::E == 4 ? 7 : kVecs == 4 ? 6 : 4) void top_unit_kernel(
+    TopArgs a) {
   constexpr int kUnits = kThreads < 256 ? 256 / kThreads : 1, kWaves = kThreads / 64;
   __shared__ TopLds<kThreads> lds[kUnits];
   const int lane = threadIdx.x % kThreads, slot = threadIdx.x / kThreads;
@@ -511,7 +514,7 @@ constexpr int kFewRows = 128;
 
 // Elements of a part of a row: short ones fill the chip when rows are few, long ones share the cost
 // of a part's threshold.  1,024 and 2,048 vectors, us of 2,048 x 65,536: fp32 top 8 157 and 126,
-// top 64 206 and 151, top 256 562 and 420; bf16 top 64 131 and 126, top 256 365 and 278.
+// top 64 206 and 151, top 256 562 and 420; bf16 top 64 131 and 109, top 256 365 and 269.
 int part_range(int32_t dtype, int64_t rows) { return (rows <= kFewRows ? 1024 : 2048) * vector_elems(dtype); }
 
 // Parts of a row, 1: the whole of it at once.
