@@ -9,7 +9,7 @@
 //     little more than `top` elements, goes to LDS, where each is ranked by counting.
 //     Where too many reach it (ties, sorted rows) the threshold is bisected, and among equal
 //     values the class;
-//   - few rows, and rows longer than that: parts of a row first, then the lists of its parts.
+//   - rows longer than that: parts of a row first, then the lists of its parts.
 // The log-sum is one more pass over the registers, with no test for what is listed: an exponential's
 // clamp makes 1 of each listed one, and their number is taken off the sum.
 // The instructions for an element (unpack, maximum, compare, product-sum, exponential, sum) bound bf16:
@@ -508,19 +508,19 @@ __global__ __launch_bounds__(256) void top_lists_kernel(pgcn_top_logits_args a) 
 int vector_elems(int32_t dtype) { return dtype == PGCN_BF16 ? BF16::E : F32::E; }
 
 // Vectors of the longest row that a workgroup holds: the register file's limit in bf16; 4,096 x 32,768
-// fp32 top 8 whole 148 us, in parts 129, top 64 both 162.
+// fp32 top 8 whole 148 us, in parts 129, top 64 both 162.  Few rows are not cut for the sake of more
+// workgroups: the second launch costs more, 1 x 16,000 fp32 top 50 7.9 us whole, 7.5 + 9.9 in parts,
+// 8 x 32,000 bf16 top 8 9.1 and 7.0 + 5.0.
 constexpr int kLongVecs = 4096;
-constexpr int kFewRows = 128;
-
-// Elements of a part of a row: short ones fill the chip when rows are few, long ones share the cost
-// of a part's threshold.  1,024 and 2,048 vectors, us of 2,048 x 65,536: fp32 top 8 157 and 126,
-// top 64 206 and 151, top 256 562 and 420; bf16 top 64 131 and 109, top 256 365 and 269.
-int part_range(int32_t dtype, int64_t rows) { return (rows <= kFewRows ? 1024 : 2048) * vector_elems(dtype); }
+// Vectors of a part of a row: long ones share the cost of a part's threshold.  1,024 and 2,048, us of
+// 2,048 x 65,536: fp32 top 8 157 and 126, top 64 206 and 151, top 256 562 and 420; bf16 top 64 131 and
+// 109, top 256 365 and 269; 1 x 100,003 fp32 top 50 both 17, 128 x 100,003 bf16 top 64 31 and 28.
+constexpr int kPartVecs = 2048;
 
 // Parts of a row, 1: the whole of it at once.
-int top_parts(int32_t dtype, int64_t rows, int32_t classes) {
-  const int range = part_range(dtype, rows), parts = (classes + range - 1) / range;
-  return classes > kLongVecs * vector_elems(dtype) || (rows <= kFewRows && parts >= 4) ? parts : 1;
+int top_parts(int32_t dtype, int32_t classes) {
+  const int e = vector_elems(dtype), range = kPartVecs * e;
+  return classes > kLongVecs * e ? (classes + range - 1) / range : 1;
 }
 
 // Whether a thread takes a row: fits to both kernels' times, in us.  A thread's walk is a chain, so few
@@ -604,14 +604,14 @@ int top_go(const pgcn_top_logits_args &a, hipStream_t s) {
     if (a.top <= 32) return lists_go<T, 32>(a, s);
     return lists_go<T, 64>(a, s);
   }
-  const int parts = top_parts(a.dtype, a.rows, a.classes);
+  const int parts = top_parts(a.dtype, a.classes);
   TopArgs t{};
   t.Z = a.Z;
   t.rows = a.rows;
   t.ld = a.ld;
   t.classes = a.classes;
   t.top = t.fill = a.top;
-  t.range = parts > 1 ? part_range(a.dtype, a.rows) : a.classes;
+  t.range = parts > 1 ? kPartVecs * T::E : a.classes;
   t.parts = parts;
   t.inv_t = 1.0f / a.temperature;
   t.values = a.top_values;
@@ -651,7 +651,7 @@ int top_go(const pgcn_top_logits_args &a, hipStream_t s) {
 
 size_t top_logits_workspace(int32_t dtype, int64_t rows, int32_t classes, int32_t top) {
   if (lists_taken(rows, classes, top)) return 0;
-  const int parts = top_parts(dtype, rows, classes);
+  const int parts = top_parts(dtype, classes);
   return parts > 1 ? part_lists(rows, parts, (top + 3) / 4 * 4).bytes : 0;
 }
 
