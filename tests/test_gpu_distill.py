@@ -90,7 +90,7 @@ def test_top_logits_sizes(rows, C, K, dtype):
     check_top(matrix(logits(rng, rows, C), dtype), C, K, 2.0, dtype, ld_top=K + 3)
 
 
-@pytest.mark.parametrize("C,K", [(41, 8), (100, 64), (300, 32), (700, 1), (1500, 100), (5000, 64), (40000, 200), (131072, 256)])
+@pytest.mark.parametrize("C,K", [(41, 8), (100, 64), (300, 32), (700, 1), (1500, 100), (5000, 64), (40000, 200), (131072, 256), (390, 71), (1000, 128)])
 @pytest.mark.parametrize("kind", ["equal", "ties", "rising", "falling", "masked", "one_left", "none_left", "lowest", "inf", "infs", "far_rest",
                                   "zeros", "last_block"])
 def test_top_logits_orders_and_masks(C, K, kind):
