@@ -16,6 +16,7 @@
 // 2,048 x 65,536 top 64 fp32 151 us, 3.6 TB/s, bf16 109 us, 2.5 TB/s; top 8 126 and 83 us.
 #include <algorithm>
 #include <cfloat>
+#include <type_traits>
 
 #include "ops.h"
 
@@ -294,18 +295,34 @@ __global__ __launch_bounds__(kThreads < 256 ? 256 : kThreads, kVecs <= 2 ? 8 : T
   }
   float *values = a.values + unit * a.ld_top;
   int32_t *ids = a.ids + unit * a.ld_top;
-  for (int j = lane; j < n; j += kThreads) {
-    const uint64_t key = l.list[j];
-    int rank = 0;
+  // A thread's keys together against each key of the list (at most 191 of a wave, 384 of a workgroup), us one
+  // after another and together: 127,010 x 116 top 75 fp32 219 and 171, 20,000 x 250 top 128 81 and 57.
+  auto ranked = [&](auto keys_) {
+    constexpr int kKeys = decltype(keys_)::value;
+    uint64_t key[kKeys];
+    int rank[kKeys] = {};
+#pragma unroll
+    for (int q = 0; q < kKeys; ++q) key[q] = lane + q * kThreads < n ? l.list[lane + q * kThreads] : 0;
 #pragma unroll 4
-    for (int i = 0; i < n; ++i) rank += l.list[i] > key ? 1 : 0;
-    if (rank < K) {
-      const int c = (int)~(uint32_t)key;
-      values[rank] = value_of((uint32_t)(key >> 32));
-      ids[rank] = a.listed_ids ? a.listed_ids[row * a.ld + c] : first + c;
+    for (int i = 0; i < n; ++i) {
+      const uint64_t other = l.list[i];
+#pragma unroll
+      for (int q = 0; q < kKeys; ++q) rank[q] += other > key[q] ? 1 : 0;
     }
-    if (rank == K - 1) l.last = key;
-  }
+#pragma unroll
+    for (int q = 0; q < kKeys; ++q) {
+      if (lane + q * kThreads >= n) continue;
+      if (rank[q] < K) {
+        const int c = (int)~(uint32_t)key[q];
+        values[rank[q]] = value_of((uint32_t)(key[q] >> 32));
+        ids[rank[q]] = a.listed_ids ? a.listed_ids[row * a.ld + c] : first + c;
+      }
+      if (rank[q] == K - 1) l.last = key[q];
+    }
+  };
+  if (n <= kThreads) ranked(std::integral_constant<int, 1>{});
+  else if (n <= 2 * kThreads) ranked(std::integral_constant<int, 2>{});
+  else if constexpr (kThreads == 64) ranked(std::integral_constant<int, 3>{});
   for (int k = (n < K ? n : K) + lane; k < a.fill; k += kThreads) {
     values[k] = kNegInf;
     ids[k] = -1;
@@ -561,7 +578,7 @@ int unit_go(const TopArgs &all, hipStream_t s) {
 
 // More lane maxima than slots keep the threshold tight; more threads than that are more to bring together.
 // A workgroup and a wave to a row of up to 256 vectors, us of 20,000 rows, fp32 and bf16: 500 classes
-// top 65 91 and 53, 145 and 53; 1,000 top 100 106 and 86, 130 and 79; 250 top 128 140 and 81, 153 and 84.
+// top 65 99 and 47, 150 and 47; 1,000 top 100 114 and 74, 135 and 69; 250 top 128 141 and 57, 152 and 61.
 template <class T>
 int units(const TopArgs &a, hipStream_t s) {
   const int vecs = (std::min(a.range, a.classes) + T::E - 1) / T::E;
