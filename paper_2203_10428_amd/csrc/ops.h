@@ -115,13 +115,15 @@ constexpr float kLog2e = 1.44269504088896341f;
 __device__ __forceinline__ float exp_at(float x, float m, float scale) { return __builtin_amdgcn_exp2f((x - m) * scale); }
 
 // e^{(x - m) T'} for many x: one product-sum each, 2^{x scale - shift} fix, where fix takes up what
-// shift = m scale was rounded by.
+// shift = m scale was rounded by: at most 32 below 2^30, so that 2^{m scale - shift}, fix and sums of
+// 2^18 such terms are in range.  From 2^30 on (a finite mask value or a far offset at a low temperature)
+// a neighbour of m is 2^6 exponents away or more, and any scale that leaves it there gives the same 1
+// and 0: the power of two that brings m to [2^30, 2^31), with which m scale is not rounded at all.
 struct Exps {
   float scale, shift, fix;
   __device__ __forceinline__ Exps(float m, float scale_) {
-    // from 2^64 on (a row of the type's lowest value) neighbours are 2^40 apart: any scale that keeps
-    // the product finite gives the same 1 and 0
-    scale = fabsf(m) < 0x1p64f ? scale_ : 0x1p-30f;
+    const uint32_t exponent = (__float_as_uint(m) >> 23) & 0xff;
+    scale = fabsf(m * scale_) < 0x1p30f ? scale_ : __uint_as_float((2 * 127 + 30 - exponent) << 23);
     shift = m * scale;
     fix = __builtin_amdgcn_exp2f(-__builtin_fmaf(m, scale, -shift));
   }
