@@ -59,6 +59,7 @@ outputs across iterations, so it is a variant, not the measured step.
 """
 from __future__ import annotations
 
+import math
 from dataclasses import dataclass
 
 import numpy as np
@@ -298,7 +299,15 @@ class PartitionTrainer:
             self.teacher = None
             return
         assert self.loss_kind == B.PGCN_SOFTMAX_CE, "distillation replaces the softmax cross-entropy"
-        assert values.shape == ids.shape and values.shape[0] == self.n, (tuple(values.shape), self.n)
+        # the kernel sees pointers: what does not fit is refused here, before a step has begun
+        most = min(self.widths[self.L], B.PGCN_MAX_TOP)
+        if values.dim() != 2 or values.shape != ids.shape or values.shape[0] != self.n or not 1 <= values.shape[1] <= most:
+            raise ValueError(f"values and ids must be [{self.n}, 1 .. {most}], not {tuple(values.shape)}, {tuple(ids.shape)}")
+        if tail_lse is not None and tail_lse.numel() != self.n:
+            raise ValueError(f"tail_lse must have {self.n} elements, not {tuple(tail_lse.shape)}")
+        o = self.opts
+        if not (1e-4 <= o.distill_temp <= 1e4 and math.isfinite(o.distill_soft) and math.isfinite(o.distill_hard)):
+            raise ValueError("distill_temp must be in [1e-4, 1e4], distill_soft and distill_hard finite")
         self.teacher = (values.to(self.dev, torch.float32).contiguous(), ids.to(self.dev, torch.int32).contiguous(),
                         None if tail_lse is None else tail_lse.to(self.dev, torch.float32).contiguous())
         need = B.pgcn_distill_workspace_size(B.PGCN_F32, self.n, self.widths[self.L], values.shape[1])
