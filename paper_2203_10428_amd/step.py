@@ -41,7 +41,7 @@ normalises every node's features by themselves (one group: layer norm),
 at 1 and 0 and are trained like the weights.  The sent rows are those of the
 normalised features, packed in a pass of their own.
 
-Distillation: ``top_logits`` lists the largest logits of every node, and
+Distillation: ``top_logits`` lists the largest logits of every node in the last step, and
 ``set_teacher`` makes the step's loss
 
     loss_scale * (distill_hard * CE(labels) + distill_soft * T^2 * KL(teacher || student))
@@ -278,18 +278,22 @@ class PartitionTrainer:
 
     # ------------------------------------------------------------------
     def top_logits(self, top: int, temperature: float = 1.0):
-        """The `top` largest logits of every node of the last step's output: (values, ids, tail_lse), to be
-        given to a student's set_teacher."""
+        """The `top` largest logits of every node: (values, ids, tail_lse), to be given to a student's set_teacher.
+        The logits are those of the last step's forward: of the weights before its update, and with its dropout.
+        Ordered like a step: after what the trainer and the caller's stream have in flight, before either's next work."""
         C_ = self.widths[self.L]
         v = torch.empty((self.n, top), dtype=torch.float32, device=self.dev)
         i = torch.empty((self.n, top), dtype=torch.int32, device=self.dev)
         tail = torch.empty(self.n, dtype=torch.float32, device=self.dev)
+        st, caller = self.stream, torch.cuda.current_stream(self.dev)
         with torch.cuda.device(self.dev):
             n = B.pgcn_top_logits_workspace_size(B.PGCN_F32, self.n, C_, top)
             ws = torch.empty(max(n, 16), dtype=torch.uint8, device=self.dev)
+            st.wait_stream(caller)          # the buffers' memory is free to be written
             B.pgcn_top_logits(dtype=B.PGCN_F32, rows=self.n, classes=C_, ld=ld_of(C_), top=top, ld_top=top,
                               temperature=temperature, Z=self.H[self.L], top_values=v, top_ids=i, tail_lse=tail,
-                              workspace=ws, workspace_bytes=n, stream=torch.cuda.current_stream(self.dev))
+                              workspace=ws, workspace_bytes=n, stream=st)
+            caller.wait_stream(st)
         return v, i, tail
 
     def set_teacher(self, values, ids, tail_lse=None):
