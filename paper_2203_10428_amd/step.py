@@ -319,6 +319,12 @@ class PartitionTrainer:
             torch.cuda.synchronize(self.dev)        # a step in flight still uses the smaller one
             self.ws_bytes = need
             self.ws = torch.empty(need, dtype=torch.uint8, device=self.dev)
+        # a step may be called on another stream than the one that writes the lists, and may still read them
+        # when another teacher takes their place
+        self.stream.wait_stream(torch.cuda.current_stream(self.dev))
+        for x in self.teacher:
+            if x is not None:
+                x.record_stream(self.stream)
 
     def _loss(self, st):
         o, C_, n = self.opts, self.widths[self.L], self.n
