@@ -90,7 +90,7 @@ __device__ __forceinline__ float row_loss(const RowStats &st, float listed, floa
                                           float hard) {
   float l = listed;
   if (st.soft) l += soft_scale * kl_term(st.rho, st.log_rho, st.log_s);
-  if (has_label) l += hard * (st.m + st.log_hard - z_label);
+  if (has_label) l += hard * ((st.m - z_label) + st.log_hard);     // m + log would round the logarithm to m's digits
   return poison ? __builtin_nanf("") : l;          // an id or label out of range
 }
 
