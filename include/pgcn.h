@@ -588,6 +588,7 @@ int pgcn_top_logits(const pgcn_top_logits_args *args, hipStream_t stream);
  *   - labels NULL, or a label -1: no hard term (a node without a label).
  *   - p log(p / q) is 0 where p is 0, also where q is 0 (a logit of -inf masks its class);
  *     it is +inf where p > 0 and q = 0.
+ *   - A scale of 0 takes its term out, whatever it would have been.
  *   - An id or label >= classes (a label < -1 too) makes the loss NaN; the id is otherwise
  *     ignored.  A row without any finite logit that has a soft or hard term makes it NaN.
  *   - A NaN among a row's logits makes the row's J NaN, and the loss if the row has a term; a NaN

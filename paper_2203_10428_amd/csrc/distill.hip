@@ -34,18 +34,18 @@ struct RowStats {
   float mt, log_t;        // teacher: p_k = e^{(t_k - mt) / T - log_t}
   float rho, log_rho;
   float inv_hard, log_hard;   // sum e^{z - m}: its reciprocal, its logarithm
-  bool soft;              // the teacher lists something
+  bool soft;              // the teacher lists something, and its term counts
   bool some;              // there is an unlisted logit above -inf
 };
 
 // `two`: `hard` is the sum of e^{z - m}; else the temperature is 1 (or no row has a label) and the soft sum is it.
 __device__ __forceinline__ RowStats row_stats(const LogSum &rest, const LogSum &top, const LogSum &teacher, bool two, float hard, float m,
-                                              float tail, float inv_t) {
+                                              float tail, float inv_t, float soft_scale) {
   RowStats st;
   const LogSum all = merge(rest, top, inv_t);
   st.m = m;
   st.log_all = __logf(all.s);
-  st.soft = teacher.s != 0.f;                      // NaN counts: it has to show
+  st.soft = teacher.s != 0.f && soft_scale != 0.f; // NaN counts: it has to show
   st.mt = base_of(teacher.m);
   if (tail != kNegInf) {
     const float b = tail - st.mt * inv_t;          // e^b beside the listed ones' sum
@@ -90,7 +90,7 @@ __device__ __forceinline__ float row_loss(const RowStats &st, float listed, floa
                                           float hard) {
   float l = listed;
   if (st.soft) l += soft_scale * kl_term(st.rho, st.log_rho, st.log_s);
-  if (has_label) l += hard * ((st.m - z_label) + st.log_hard);     // m + log would round the logarithm to m's digits
+  if (has_label && hard != 0.f) l += hard * ((st.m - z_label) + st.log_hard);     // m + log would round the logarithm to m's digits
   return poison ? __builtin_nanf("") : l;          // an id or label out of range
 }
 
@@ -230,7 +230,7 @@ __global__ __launch_bounds__(256) void distill_short_kernel(pgcn_distill_args a,
     s_rest = lanes_sum<kLanes>(s_rest);
     const LogSum rest = {m_rest, s_rest}, top = {m_top, s_top};
     if (two) s_hard = lanes_sum<kLanes>(s_hard);
-    const RowStats st = row_stats(rest, top, LogSum{mt, s_t}, two, s_hard, m, tail, inv_t);
+    const RowStats st = row_stats(rest, top, LogSum{mt, s_t}, two, s_hard, m, tail, inv_t, a.soft_scale);
     const float soft = st.soft ? a.soft_scale * inv_t : 0.f, hard = has_y ? a.hard_scale : 0.f;
 
     float loss = 0.f;
@@ -406,7 +406,7 @@ __device__ __forceinline__ RowStats block_stats(const pgcn_distill_args &a, int6
   const LogSum rest = {m_rest, s_rest}, top = {m_top, (l.s_top[0] + l.s_top[1]) + (l.s_top[2] + l.s_top[3])};
   const LogSum teacher = {m_t, (l.s_t[0] + l.s_t[1]) + (l.s_t[2] + l.s_t[3])};
   s_hard += (l.s_hard_top[0] + l.s_hard_top[1]) + (l.s_hard_top[2] + l.s_hard_top[3]);
-  return row_stats(rest, top, teacher, two, s_hard, m, a.tail_lse ? a.tail_lse[r] : kNegInf, inv_t);
+  return row_stats(rest, top, teacher, two, s_hard, m, a.tail_lse ? a.tail_lse[r] : kNegInf, inv_t, a.soft_scale);
 }
 
 template <class T, int kVecs>
