@@ -23,23 +23,54 @@ constexpr int kThreads = 256;
 
 __device__ __forceinline__ float sigmoid(float u) { return __builtin_amdgcn_rcpf(1.0f + __expf(-u)); }
 
-// The normal distribution's Phi(u) and e^{-u^2 / 2}.  On the side where nothing cancels, Phi(-|u|) e^{u^2 / 2}
-// falls smoothly: t times a polynomial of degree 7 in t = 1 / (1 + 0.3 |u|), the minimax fit on [0, 14] (below
-// that e^{-u^2 / 2} is 0), within 1.5e-7 of itself.  That is exact enough for a result of 8 bits.  In fp32 t's
-// rounding shows near 0, where Phi - 1/2 is u times a polynomial in u^2, fitted for |u| <= 1.25 within 5e-11.
-// rms error of u Phi against 64 bits on [-3, -2], [-2, -1], [-1, 0], [0, 1]: 5e-9, 2e-8, 8e-9, 1.6e-8;
-// of u (1 + erf) / 2 in fp32 2.2e-8, 1.6e-8, 8e-9, 1.7e-8.
-template <class T>
+// GELU, u Phi(u), and its slope Phi(u) + u phi(u), by minimax fits.  With a = |u|, v = u^2 and t = 1 / (1 + k a), the tail
+// Phi(-a) is e^{-v / 2} times a smooth function of t (fitted up to a = 14, from where e^{-v / 2} is 0), which keeps the
+// digits of its far end.  An 8-bit result needs no more, one form for both directions, within 1.5e-7 of the tail.
+// In fp32 t's rounding shows near 0, so for a <= 1.25 Phi - 1/2 is u times a polynomial in v (2e-9), and beyond
+// it u Phi = max(u, 0) - a Phi(-a), with a Phi(-a) e^{v / 2} fitted as a whole (2e-7 of itself), and the slope likewise.
+// rms error against 64 bits on [-3, -2], [-2, -1.25], [-1.25, -0.6], [0, 1.25]: u Phi 5e-9, 1.6e-8, 1.2e-8, 1.7e-8, the slope
+// 7e-9, 1.6e-8, 2.5e-8, 3.2e-8; plain fp32 forms with erf 2.2e-8, 1.7e-8, 1.2e-8, 2.3e-8 and 1e-8, 1.4e-8, 1.5e-8, 3.4e-8.
+constexpr float kNear2 = 1.25f * 1.25f, kPhi0 = 0.39894228040143268f;
+
+__device__ __forceinline__ float inv_1p(float k, float a) { return __builtin_amdgcn_rcpf(__builtin_fmaf(k, a, 1.0f)); }
+__device__ __forceinline__ float exp_half(float v) { return __builtin_amdgcn_exp2f(v * (-0.5f * kLog2e)); }
+
 __device__ __forceinline__ float normal_cdf(float u, float &e) {
-  const float v = u * u, t = __builtin_amdgcn_rcpf(__builtin_fmaf(0.3f, fabsf(u), 1.0f));
-  e = __builtin_amdgcn_exp2f(v * (-0.5f * kLog2e));
+  const float t = inv_1p(0.3f, fabsf(u));
+  e = exp_half(u * u);
   const float tail = e * t * (0.119629301f + t * (0.120753959f + t * (0.0999134928f + t * (0.128561616f + t * (-0.0536836162f +
                      t * (0.206353471f + t * (-0.157203063f + t * 0.0356747694f)))))));
-  const float far = u < 0.f ? tail : 1.0f - tail;
-  if (T::E == BF16::E) return far;
-  const float near = 0.5f + u * (0.398942292f + v * (-0.0664903671f + v * (0.00997345522f + v * (-0.00118701311f +
-                     v * (0.000114930343f + v * (-9.00678242e-06f + v * 4.65978673e-07f))))));
-  return v < 1.25f * 1.25f ? near : far;
+  return u < 0.f ? tail : 1.0f - tail;
+}
+
+template <class T>
+__device__ __forceinline__ float gelu(float u) {
+  if (T::E == BF16::E) {
+    float e;
+    return u * normal_cdf(u, e);
+  }
+  const float v = u * u, t = inv_1p(0.6f, fabsf(u));
+  const float far = fmaxf(u, 0.f) - exp_half(v) * (0.398910642f + t * (0.00111445237f + t * (-0.159502506f + t * (-0.168464243f +
+                    t * (-0.775735795f + t * (1.18716598f + t * -0.494058937f))))));
+  const float near = 0.5f * u + v * (0.398942262f + v * (-0.0664899871f + v * (0.00997150317f + v * (-0.00118271261f +
+                     v * (0.000110329238f + v * -6.64525169e-06f)))));
+  return v < kNear2 ? near : far;
+}
+
+template <class T>
+__device__ __forceinline__ float gelu_slope(float u) {
+  if (T::E == BF16::E) {
+    float e;
+    const float c = normal_cdf(u, e);
+    return c + u * e * kPhi0;
+  }
+  const float a = fabsf(u), v = u * u, t = inv_1p(0.3f, a);
+  const float h = exp_half(v) * (t * (0.119705357f + t * (0.119321547f + t * (0.111028418f + t * (0.0824648142f +
+                  t * (0.0568446219f + t * (0.052795399f + t * -0.0424533971f)))))) - kPhi0 * a);       // Phi(-a) - a phi(a)
+  const float far = u < 0.f ? h : 1.0f - h;
+  const float near = 0.5f + u * (0.797884524f + v * (-0.265961289f + v * (0.0598397814f + v * (-0.00949377846f +
+                     v * (0.00114656577f + v * (-0.000106548643f + v * 6.19606453e-06f))))));
+  return v < kNear2 ? near : far;
 }
 
 // y = act(u), the choice once for a whole array
@@ -54,10 +85,7 @@ __device__ __forceinline__ void activate(float (&u)[T::E], int act) {
     for (int i = 0; i < N; ++i) u[i] *= sigmoid(u[i]);
   } else if (act == PGCN_ACT_GELU) {
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-      float e;
-      u[i] *= normal_cdf<T>(u[i], e);
-    }
+    for (int i = 0; i < N; ++i) u[i] = gelu<T>(u[i]);
   }
 }
 
@@ -76,11 +104,7 @@ __device__ __forceinline__ void times_slope(float (&j)[T::E], const float (&u)[T
     }
   } else if (act == PGCN_ACT_GELU) {
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-      float e;
-      const float c = normal_cdf<T>(u[i], e);
-      j[i] *= c + u[i] * e * 0.39894228040143268f;
-    }
+    for (int i = 0; i < N; ++i) j[i] *= gelu_slope<T>(u[i]);
   }
 }
 
@@ -726,7 +750,7 @@ __device__ __forceinline__ void load_rows(const void *base, int64_t row0, int64_
 }
 
 template <class T, int kLanes, int kVecs, Sum kSum>
-__global__ __launch_bounds__(kThreads) void rows_fwd_kernel(pgcn_group_norm_fwd_args a, RowShape sp) {
+__global__ __launch_bounds__(kThreads, T::E == 4 && kVecs == 2 ? 8 : 1) void rows_fwd_kernel(pgcn_group_norm_fwd_args a, RowShape sp) {
   __shared__ float lds[kThreads / 64];
   const int slot = threadIdx.x / kLanes;
   int c0[kVecs], row[kVecs];
@@ -824,7 +848,7 @@ __device__ __forceinline__ void write_channel_sums(const RowShape &sp, const int
 
 // The backward of those rows; a workgroup's channel sums go to part[workgroup][2][channels].
 template <class T, int kLanes, int kVecs, Sum kSum>
-__global__ __launch_bounds__(kThreads, kVecs * T::E <= 4 ? 4 : kVecs <= 4 ? 2 : 1) void rows_bwd_kernel(pgcn_group_norm_bwd_args a, RowShape sp, float *part) {
+__global__ __launch_bounds__(kThreads, kVecs * T::E <= 4 ? 4 : T::E == 4 && kVecs == 2 && kSum == Sum::LANES ? 5 : kVecs <= 4 ? 2 : 1) void rows_bwd_kernel(pgcn_group_norm_bwd_args a, RowShape sp, float *part) {
   extern __shared__ float lds_all[];
   const int slot = threadIdx.x / kLanes;
   int c0[kVecs], row[kVecs];
