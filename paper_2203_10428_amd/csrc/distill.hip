@@ -12,8 +12,8 @@
 // loss are fp32 over a row, fp64 over the rows.
 //
 // Bound by one read of Z and one write of J.  A row stays in registers between its sums and
-// its gradient: in a few lanes of a wave (up to 2,048 classes), in a workgroup (up to 65,536
-// fp32 or 131,072 bf16 classes).  Longer rows, and few long ones, are cut into parts and read twice.
+// its gradient: in a few lanes of a wave (up to 2,048 classes), in a workgroup (up to 32,768
+// fp32 or 65,536 bf16 classes).  Longer rows, and few long ones, are cut into parts and read twice.
 #include <algorithm>
 
 #include "ops.h"

@@ -90,17 +90,8 @@ constexpr float kNegInf = -INFINITY;
 struct LogSum {
   float m, s;
 };
-constexpr LogSum kNothing = {kNegInf, 0.f};
 
 __device__ __forceinline__ float exp_diff(float x, float m, float a) { return x == kNegInf ? 0.f : __expf((x - m) * a); }
-
-// A NaN leaves m and makes s NaN.
-__device__ __forceinline__ void add(LogSum &l, float x, float a) {
-  if (x == kNegInf) return;
-  const float m = fmaxf(l.m, x);
-  l.s = l.s * exp_diff(l.m, m, a) + __expf((x - m) * a);
-  l.m = m;
-}
 
 __device__ __forceinline__ LogSum merge(const LogSum &x, const LogSum &y, float a) {
   LogSum r;
