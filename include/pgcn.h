@@ -591,8 +591,10 @@ int pgcn_top_logits(const pgcn_top_logits_args *args, hipStream_t stream);
  *   - A scale of 0 takes its term out, whatever it would have been.
  *   - An id or label >= classes (a label < -1 too) makes the loss NaN; the id is otherwise
  *     ignored.  A row without any finite logit that has a soft or hard term makes it NaN.
- *   - A NaN among a row's logits makes the row's J NaN, and the loss if the row has a term; a NaN
- *     among its listed values makes both NaN.
+ *   - A NaN among the logits of a row that has a term makes the loss NaN, and J at each of the
+ *     row's classes whose logit is not -inf; in a row without a term J may be NaN at the NaN
+ *     itself, and is 0 elsewhere.  A NaN among a row's listed values makes its J NaN (a masked
+ *     class's may be 0), and the loss.
  * J: [rows, ld], the dtype and stride of Z.  loss_out: one device float, written (not
  * accumulated), reduced in a fixed order.
  */
