@@ -100,9 +100,9 @@ __device__ __forceinline__ float row_loss(const RowStats &st, float listed, floa
 // lanes take a row: about 16 elements each, down to 4 lanes.  The row's image in LDS serves the
 // listed classes, kSlots to a lane: their logits are read from it, and their gradients written
 // into it for the lane that holds the class.
-// Bound by instructions, up to about 100 classes by a row's fixed ones: 58,000 x 41 top 8 fp32
-// 11.7 us (2.0 TB/s), 306,000 x 47 top 16 bf16 34.4 (2.8), 100,000 x 128 top 8 fp32 24.4 (4.5),
-// 10,000 x 2,000 top 64 fp32 40 (4.1), bf16 31 (2.7).
+// Bound by instructions, up to about 100 classes by a row's fixed ones: vector instructions are issued in
+// 0.80 of all cycles of 306,000 x 47 top 16 bf16, 34 us (2.8 TB/s), 0.60 in fp32, 43.5 us (3.6), and 0.46 of
+// 58,000 x 41 top 8 fp32, 11.7 us (2.0), at 3.5 waves to a SIMD.  100,000 x 128 top 8 fp32 24.4 (4.5), 10,000 x 2,000 top 64 fp32 40 (4.1), bf16 31 (2.7).
 
 template <class T, int kLanes, int kVecs, int kSlots>
 __global__ __launch_bounds__(256) void distill_short_kernel(pgcn_distill_args a, double *part) {
@@ -288,7 +288,8 @@ __global__ __launch_bounds__(256) void distill_short_kernel(pgcn_distill_args a,
 //
 // The listed classes have a bit each in LDS and are taken out of the threads' vectors (-inf);
 // thread k takes slot k, and writes its class's gradient over the one that the vector left.
-// Bound by memory: 4,096 x 32,000 top 64 fp32 207 us, 5.1 TB/s; 1,024 x 32,000 bf16 36 us, 3.6 TB/s.
+// Bound by memory: 4,096 x 32,000 top 64 fp32 207 us, 5.1 TB/s, vector instructions in 0.34 of the cycles;
+// 1,024 x 32,000 bf16 32 us, 4.1 TB/s, 0.60.
 // Without the bound of four waves to a SIMD the scheduler holds more than it has and spills (516 us).
 
 template <int kThreads>

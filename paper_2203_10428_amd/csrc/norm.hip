@@ -147,9 +147,11 @@ __device__ __forceinline__ int group_of(uint32_t magic, int c) { return magic ? 
 // chunks in every workgroup and writes the rows.  Few long samples are cut into enough chunks
 // to fill the chip.
 //
-// Bound by memory, in bf16 with SiLU as much by its instructions: the second launch reads the sample
-// again, mostly out of the caches.  us of the two launches: forward 1 x 58,000 x 256 fp32 in 8 groups,
-// GELU, 12.4 (4.8 TB/s) and 25.0; backward 8 x 4,096 x 320 bf16 in 32 groups, SiLU, 17.5 (2.4) and 20.0.
+// The second launch reads the sample again, all of it from beyond L2 (fetched bytes).  us of the two launches:
+// forward 1 x 58,000 x 256 fp32 in 8 groups, GELU, 12.4 (4.8 TB/s) and 25.7 (4.6), backward with SiLU 26.6 (4.5)
+// and 33.6 (5.3): memory.  Backward 8 x 4,096 x 320 bf16 in 32 groups, SiLU, 17.4 (2.4) and 20.0 (3.1): neither
+// memory nor instructions (issued in 0.37 and 0.40 of the cycles), but the chain of a workgroup at two or
+// three waves to a SIMD: its parameters one by one, about 12 rows to a thread, the join.
 //
 // A workgroup's threads: lx side by side on a row's vectors (all of them where a row has at most
 // 256), ty row slots above one another, the rest idle.
@@ -653,8 +655,9 @@ __global__ __launch_bounds__(kThreads) void grad_rows_kernel(pgcn_group_norm_bwd
 // of all its rows' vectors), so that X (and J) cross the memory once and both passes over the
 // sample stay in registers.  A workgroup walks samples at a fixed stride: gamma, beta and the
 // backward's channel sums stay in registers too.  Bound by memory in fp32 (30,000 x 1,024: forward
-// 4.97, backward 4.6 TB/s, 2,048 channels 4.6 and 4.8), by the activation's exponents and
-// reciprocals in bf16, where a byte carries twice the elements (2.9 and 2.5, 3.9 and 3.2).
+// 4.97, backward 4.6 TB/s, 2,048 channels 4.6 and 4.8).  In bf16, where a byte carries twice the elements, a
+// sample's chain of load, sums and activation is as long again for half the bytes (2.9 and 2.5 TB/s, 3.9 and 3.2):
+// 30,000 x 1,024 with SiLU 41.6 and 64 us, instructions in 0.49 and 0.42 of the cycles, at 5 and 3 waves to a SIMD.
 // How a group's sum is formed:
 enum class Sum {
   ROW,     // one group: all the sample's threads
@@ -910,9 +913,10 @@ __global__ __launch_bounds__(kThreads, kVecs * T::E <= 4 ? 4 : T::E == 4 && kVec
 //
 // The sample's values go through LDS, where a team of lanes takes each group; what is needed after
 // the sums is read from there again and not held in registers.  gamma and beta lie in LDS too.
-// Bound by LDS instructions: an element is written once and read once (forward: twice) as a single
-// float, gamma, beta and the group's values come from LDS again.  30,000 x 1,000 fp32 in 8 groups:
-// forward 103 us (2.4 TB/s), backward 115 (3.1); 1,024 channels in 32 groups by shuffles 52 and 80.
+// An element is written once and read once (forward: twice) as a single float, gamma, beta and the group's
+// values come from LDS again, one phase after another: LDS instructions are under way in 0.41 of the cycles
+// forward and 0.55 backward, vector instructions issued in half.  30,000 x 1,000 fp32 in 8 groups: forward
+// 102 us (2.4 TB/s), backward 114 (3.2); 1,024 channels in 32 groups by shuffles 52 and 80.
 
 // Calls f(offset into the image) for the part of group g that lane t of its team takes.
 template <class F>
@@ -1040,7 +1044,8 @@ __global__ __launch_bounds__(kThreads, kVecs * T::E <= 16 ? 4 : 2) void any_fwd_
 
 // Four waves to a SIMD are worth the four registers spilt outside the loop (128 of 136), us at three
 // and at four: 100,000 x 300 in 4 groups fp32 189 and 135, bf16 157 and 123; 10,000 x 2 x 1,024 in
-// 8 groups 98 and 69, 82 and 61.
+// 8 groups 98 and 69, 82 and 61.  A kernel for samples of one row that kept all but the sums in registers
+// took 115 for the first.
 template <class T, int kLanes, int kVecs>
 __global__ __launch_bounds__(kThreads, kVecs * T::E <= 8 ? 4 : kVecs * T::E <= 16 ? 2 : 1) void any_bwd_kernel(
     pgcn_group_norm_bwd_args a, RowShape sp, float *part) {

@@ -12,8 +12,10 @@
 //   - rows longer than that: parts of a row first, then the lists of its parts.
 // The log-sum is one more pass over the registers, with no test for what is listed: an exponential's
 // clamp makes 1 of each listed one, and their number is taken off the sum.
-// The instructions for an element (unpack, maximum, compare, product-sum, exponential, sum) bound bf16:
-// 2,048 x 65,536 top 64 fp32 151 us, 3.6 TB/s, bf16 109 us, 2.5 TB/s; top 8 126 and 83 us.
+// Bound by the instructions for an element (unpack, maximum, compare, product-sum, exponential, sum) where
+// rows fill the chip: vector instructions are issued in 0.8 of all cycles of 2,048 x 65,536 top 64, fp32 148 us
+// (3.6 TB/s), bf16 101 us (2.7 TB/s), and of 20,000 x 250 top 128, 56 us, most of it ranking; joining 2,048
+// rows' parts takes 17 us.
 #include <algorithm>
 #include <cfloat>
 #include <type_traits>
@@ -172,7 +174,9 @@ __global__ __launch_bounds__(kThreads < 256 ? 256 : kThreads, kVecs <= 2 ? 8 : T
   int turn = 0;
   const int most = K + (kWaves > 1 ? 128 : 63);    // candidates to rank
   const int vecs = (n_all + T::E - 1) / T::E, maxima = vecs < kThreads ? vecs : kThreads;
-  const int r = (64 * K + maxima - 1) / maxima;    // the wave's share of K lane maxima
+  // The wave's share of K lane maxima.  Above 64 there is no threshold: more slots than maxima, or a short row
+  // in one wave, whose idle lanes count in 64 too; its list is found by bisection.
+  const int r = (64 * K + maxima - 1) / maxima;
   float v = kNegInf;                               // a short row is its own list of candidates
   if (n_all > most && r <= 64) v = reached_by(top, r);
   if (kWaves > 1 && n_all > most && r <= 64) {
@@ -406,8 +410,9 @@ __global__ __launch_bounds__(kThreads < 256 ? 256 : kThreads, kVecs <= 2 ? 8 : T
 // v_i, its class the one that goes with it.  Classes come in ascending order, so of equal values the
 // one that is there stays in front.  What falls out at the end is no part of the list any more and
 // goes into the log-sum.  A wave's rows pass through LDS in tiles of kTile classes.  Bound by the
-// list's instructions, 3 kSlots for a class: 58,000 x 41 top 8 fp32 10.7 us, 306,000 x 47 31 us
-// (2.5 TB/s), bf16 29.
+// list's instructions, 3 kSlots for a class, and their chain: 58,000 x 41 top 8 fp32 10.7 us, at under one wave
+// to a SIMD, which issues vector instructions in 0.44 of its cycles; 306,000 x 47 31 us (2.5 TB/s, 0.65 of all
+// cycles), bf16 29.
 
 constexpr int kTile = 32, kStep = 4;
 
@@ -579,6 +584,9 @@ int unit_go(const TopArgs &all, hipStream_t s) {
 // More lane maxima than slots keep the threshold tight; more threads than that are more to bring together.
 // A workgroup and a wave to a row of up to 256 vectors, us of 20,000 rows, fp32 and bf16: 500 classes
 // top 65 99 and 47, 150 and 47; 1,000 top 100 114 and 74, 135 and 69; 250 top 128 141 and 57, 152 and 61.
+// Lists of parts are joined by a workgroup, which is faster for one row of many entries and slower from some
+// hundred rows on, workgroup and wave: 1 x 100,003 top 50 7.7 and 9.6, top 8 5.8 and 5.6; 16 rows top 50 9.6 and
+// 10.2; 2,048 x 65,536 top 64 17 and 11, top 8 9.2 and 5.9, beside a first launch of 100 to 150 us.
 template <class T>
 int units(const TopArgs &a, hipStream_t s) {
   const int vecs = (std::min(a.range, a.classes) + T::E - 1) / T::E;
