@@ -102,7 +102,8 @@ __device__ __forceinline__ float row_loss(const RowStats &st, float listed, floa
 // into it for the lane that holds the class.
 // Bound by instructions, up to about 100 classes by a row's fixed ones: vector instructions are issued in
 // 0.80 of all cycles of 306,000 x 47 top 16 bf16, 34 us (2.8 TB/s), 0.60 in fp32, 43.5 us (3.6), and 0.46 of
-// 58,000 x 41 top 8 fp32, 11.7 us (2.0), at 3.5 waves to a SIMD.  100,000 x 128 top 8 fp32 24.4 (4.5), 10,000 x 2,000 top 64 fp32 40 (4.1), bf16 31 (2.7).
+// 58,000 x 41 top 8 fp32, 11.7 us (2.0), at 3.5 waves to a SIMD.  100,000 x 128 top 8 fp32 24.4 (4.5),
+// 10,000 x 2,000 top 64 fp32 40 (4.1), bf16 31 (2.7).
 
 template <class T, int kLanes, int kVecs, int kSlots>
 __global__ __launch_bounds__(256) void distill_short_kernel(pgcn_distill_args a, double *part) {

@@ -752,6 +752,9 @@ __device__ __forceinline__ void load_rows(const void *base, int64_t row0, int64_
   }
 }
 
+// Two fp32 vectors a thread fit eight waves to a SIMD, backward five where shuffles add up the groups: the bounds keep
+// GELU's temporaries from taking two registers more, and a wave with them from every activation: 239,000 x 512 in 32
+// groups, SiLU, backward at four 300 us, at five 295 to 297.
 template <class T, int kLanes, int kVecs, Sum kSum>
 __global__ __launch_bounds__(kThreads, T::E == 4 && kVecs == 2 ? 8 : 1) void rows_fwd_kernel(pgcn_group_norm_fwd_args a, RowShape sp) {
   __shared__ float lds[kThreads / 64];
