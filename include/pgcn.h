@@ -677,6 +677,113 @@ int pgcn_group_norm_bwd(const pgcn_group_norm_bwd_args *args, hipStream_t stream
 size_t pgcn_group_norm_workspace_size(int32_t dtype, int32_t channels, int32_t groups, int64_t samples,
                                       int64_t sample_rows);
 
+/*
+ * Rows in 8 and 4 bits.  A row is held in blocks of PGCN_MX_BLOCK neighbouring elements (the last one
+ * filled up with zeros), each with a power of two as scale:
+ *     Q  [rows, ld_q] bytes: PGCN_MX_INT8 a signed byte q for q / 64 (32 bytes a block); PGCN_MX_FP4 a sign
+ *        (bit 3) and one of 0, 0.5, 1, 1.5, 2, 3, 4, 6 (bits 0 .. 2), the even element of a pair in the low
+ *        half of its byte (16 bytes a block)
+ *     S  [rows, ld_s] bytes: s for the scale 2^(s - 127); 255 makes the block's elements NaN
+ * which are the element and scale types of the OCP microscaling formats MXINT8 and MXFP4.  Q is 16-byte
+ * aligned with ld_q a multiple of 16, S 4-byte aligned with ld_s a multiple of 4; bytes past a row's
+ * blocks are neither used nor written.  Every finite value is exact in bf16.
+ *
+ * The calls below take up to PGCN_MAX_MX_COLS elements a row.  Their other matrices, outputs, workspaces and
+ * streams are as for the operators above (top logits, distillation loss, group norm).
+ */
+enum pgcn_mx_format { PGCN_MX_INT8 = 0, PGCN_MX_FP4 = 1 };
+#define PGCN_MX_BLOCK 32
+#define PGCN_MAX_MX_COLS 16777216
+
+/*
+ * Rows quantised as they are written.  Per block, s is the smallest for which the block's largest
+ * magnitude rounds to at most 127 / 64 (INT8) or 6 (FP4), at most 254 and 252 (what is larger then
+ * takes the format's largest value); every element is rounded once, to nearest, ties to even: it is off
+ * by at most half a step.  A NaN or an infinity makes its block NaN (s = 255, elements 0).  An FP4
+ * element that rounds to 0 keeps its sign.
+ *   transpose 0: row k of Q is row index[k] of X, or row k where index is NULL (rows <= src_rows).  A
+ *       negative index gives a row of zeros, one >= src_rows a row of NaN.  With a partition's send list
+ *       as index this packs the rows that it sends.
+ *   transpose 1: Q holds the transpose of X, [cols rows of `rows` elements each] (rows == src_rows, index
+ *       NULL): weights [f_in, f_out] laid out for a product over f_in.
+ */
+typedef struct {
+  int32_t format;              /* pgcn_mx_format                                 */
+  int32_t dtype;               /* pgcn_dtype of X                                */
+  int32_t transpose;           /* 0 or 1                                         */
+  int32_t cols;                /* of X: 1 .. PGCN_MAX_MX_COLS                    */
+  int64_t rows;                /* transpose: up to PGCN_MAX_MX_COLS              */
+  int64_t src_rows;            /* rows of X                                      */
+  int64_t ld_x, ld_q, ld_s;
+  const void *X;               /* [src_rows, ld_x]                               */
+  const int32_t *index;        /* [rows] or NULL                                 */
+  uint8_t *Q;                  /* [rows, ld_q] out; transpose: [cols, ld_q]      */
+  uint8_t *S;                  /* [rows, ld_s] out; transpose: [cols, ld_s]      */
+} pgcn_mx_quantize_args;
+int pgcn_mx_quantize(const pgcn_mx_quantize_args *args, hipStream_t stream);
+
+/*
+ * Rows read back: out = v, the values that Q and S stand for, or with 0 < gamma <= 1 the moving average of
+ * Section 3.4 over them, out = gamma out + (1 - gamma) v (fp32 only; a NaN in out stays one).
+ */
+typedef struct {
+  int32_t format;              /* pgcn_mx_format                                 */
+  int32_t dtype;               /* pgcn_dtype of out                              */
+  int32_t cols;                /* 1 .. PGCN_MAX_MX_COLS                          */
+  float gamma;                 /* 0 .. 1; 0: out is not read                     */
+  int64_t rows;
+  int64_t ld_q, ld_s, ld_out;
+  const uint8_t *Q;            /* [rows, ld_q]                                   */
+  const uint8_t *S;            /* [rows, ld_s]                                   */
+  void *out;                   /* [rows, ld_out] out (in and out where gamma > 0) */
+} pgcn_mx_dequantize_args;
+int pgcn_mx_dequantize(const pgcn_mx_dequantize_args *args, hipStream_t stream);
+
+/*
+ * Weight gradient of a layer from its input or aggregate held in 8 bits (PGCN_MX_INT8, values v):
+ *     dW = v^T (J o 1[H > 0])             [f_in, f_out], a sum over the rows in a fixed order
+ * H NULL: no mask.  PGCN_F32: J in three bf16 parts that add up to it (v is exact in one), three exact
+ * products each, fp32 sums: fp32 accuracy.  PGCN_BF16: J o mask rounded once to bf16, fp32 sums.  No rows: dW = 0.
+ * A masked place of J adds nothing, whatever it holds.  A non-finite value among the others gives non-finite
+ * or NaN results.
+ */
+typedef struct {
+  int32_t dtype;               /* pgcn_dtype: the arithmetic, as for the update GEMMs */
+  int32_t f_in, f_out;         /* 1 .. PGCN_MAX_WIDTH                            */
+  int64_t rows;
+  int64_t ld_q, ld_s, ld_j, ld_h;
+  const uint8_t *Q;            /* [rows, ld_q] PGCN_MX_INT8                      */
+  const uint8_t *S;            /* [rows, ld_s]                                   */
+  const float *J;              /* [rows, ld_j], ld_j % 4 == 0                    */
+  const float *H;              /* [rows, ld_h], ld_h % 4 == 0, or NULL           */
+  float *dW;                   /* [f_in, f_out] out, compact                     */
+  void *workspace;
+  size_t workspace_bytes;
+} pgcn_mx_wgrad_args;
+size_t pgcn_mx_wgrad_workspace_size(int32_t dtype, int64_t rows, int32_t f_in, int32_t f_out);
+int pgcn_mx_wgrad(const pgcn_mx_wgrad_args *args, hipStream_t stream);
+
+/*
+ * Product of two matrices of FP4 rows (PGCN_MX_FP4, values a and b) on the scaled matrix instructions:
+ *     C[i, j] = sum over t of a[i, t] b[j, t],  relu: where negative 0           [m, n]
+ * in fp32, sums in a fixed order.  The elements that fill up a row's last block count: zeros, as
+ * pgcn_mx_quantize writes them.  Terms or sums below 2^-126 may be taken for 0.  No rows of A: nothing to do.
+ */
+typedef struct {
+  int32_t dtype;               /* pgcn_dtype of C                                */
+  int32_t relu;                /* 0 or 1                                         */
+  int64_t m;                   /* rows of A and C                                */
+  int32_t n, k;                /* rows of B; elements a row: 1 .. PGCN_MAX_MX_COLS */
+  int64_t ld_a, ld_a_scales, ld_b, ld_b_scales, ld_c;
+  const uint8_t *A, *A_scales; /* [m, ld_a], [m, ld_a_scales] PGCN_MX_FP4        */
+  const uint8_t *B, *B_scales; /* [n, ld_b], [n, ld_b_scales] PGCN_MX_FP4        */
+  void *C;                     /* [m, ld_c] out                                  */
+  void *workspace;
+  size_t workspace_bytes;
+} pgcn_mx_matmul_args;
+size_t pgcn_mx_matmul_workspace_size(int32_t dtype, int64_t m, int32_t n, int32_t k);
+int pgcn_mx_matmul(const pgcn_mx_matmul_args *args, hipStream_t stream);
+
 /* Refill of a stale buffer (Algorithm 1's send/receive threads; the paper runs
  * them on a second stream): an asynchronous copy of `bytes` bytes into device
  * memory `dst`, enqueued on `stream`.  flags = 0: device-to-device on the
@@ -716,7 +823,8 @@ enum pgcn_trace_kind {
   PGCN_TK_PACK = 8, PGCN_TK_ACCUM = 9, PGCN_TK_LOSS = 10, PGCN_TK_SGD = 11, PGCN_TK_REFILL = 12,
   PGCN_TK_GEMM_PACK = 13, PGCN_TK_DROPOUT = 14, PGCN_TK_ADAM = 15, PGCN_TK_MASK_SCALE = 16,
   PGCN_TK_ACCUM_EMA = 17, PGCN_TK_TOP_LOGITS = 18, PGCN_TK_DISTILL = 19, PGCN_TK_GROUP_NORM = 20,
-  PGCN_TK_GROUP_NORM_BWD = 21
+  PGCN_TK_GROUP_NORM_BWD = 21, PGCN_TK_MX_QUANTIZE = 22, PGCN_TK_MX_DEQUANTIZE = 23,
+  PGCN_TK_MX_WGRAD = 24, PGCN_TK_MX_MATMUL = 25
 };
 int pgcn_trace_enable(int32_t capacity);
 int pgcn_trace_filter(uint32_t kind_mask);

@@ -31,7 +31,10 @@ PGCN_ORDER_AGG, PGCN_ORDER_TRANSFORM = 0, 1
 PGCN_NOALLOC_SCRATCH_BYTES = 32 << 20
 PGCN_ACT_NONE, PGCN_ACT_RELU, PGCN_ACT_SILU, PGCN_ACT_GELU = range(4)
 PGCN_MAX_TOP, PGCN_MAX_CLASSES, PGCN_MAX_CHANNELS = 256, 262144, 8192
+PGCN_MX_INT8, PGCN_MX_FP4 = 0, 1
+PGCN_MX_BLOCK, PGCN_MAX_MX_COLS = 32, 16777216
 
+_byref = C.byref
 _vp = C.c_void_p
 _i32, _i64, _u32, _f32, _sz = C.c_int32, C.c_int64, C.c_uint32, C.c_float, C.c_size_t
 
@@ -114,6 +117,29 @@ class pgcn_group_norm_bwd_args(C.Structure):
                 ("dgamma", _vp), ("dbeta", _vp), ("workspace", _vp), ("workspace_bytes", _sz)]
 
 
+class pgcn_mx_quantize_args(C.Structure):
+    _fields_ = [("format", _i32), ("dtype", _i32), ("transpose", _i32), ("cols", _i32), ("rows", _i64), ("src_rows", _i64),
+                ("ld_x", _i64), ("ld_q", _i64), ("ld_s", _i64), ("X", _vp), ("index", _vp), ("Q", _vp), ("S", _vp)]
+
+
+class pgcn_mx_dequantize_args(C.Structure):
+    _fields_ = [("format", _i32), ("dtype", _i32), ("cols", _i32), ("gamma", _f32), ("rows", _i64), ("ld_q", _i64),
+                ("ld_s", _i64), ("ld_out", _i64), ("Q", _vp), ("S", _vp), ("out", _vp)]
+
+
+class pgcn_mx_wgrad_args(C.Structure):
+    _fields_ = [("dtype", _i32), ("f_in", _i32), ("f_out", _i32), ("rows", _i64), ("ld_q", _i64), ("ld_s", _i64),
+                ("ld_j", _i64), ("ld_h", _i64), ("Q", _vp), ("S", _vp), ("J", _vp), ("H", _vp), ("dW", _vp),
+                ("workspace", _vp), ("workspace_bytes", _sz)]
+
+
+class pgcn_mx_matmul_args(C.Structure):
+    _fields_ = [("dtype", _i32), ("relu", _i32), ("m", _i64), ("n", _i32), ("k", _i32), ("ld_a", _i64),
+                ("ld_a_scales", _i64), ("ld_b", _i64), ("ld_b_scales", _i64), ("ld_c", _i64), ("A", _vp),
+                ("A_scales", _vp), ("B", _vp), ("B_scales", _vp), ("C", _vp), ("workspace", _vp),
+                ("workspace_bytes", _sz)]
+
+
 # every symbol include/pgcn.h declares, with its ctypes signature
 SIGNATURES = {
     "pgcn_partition_setup": (_i32, [C.POINTER(pgcn_csr), C.POINTER(pgcn_boundary_map), _u32, C.POINTER(_vp)]),
@@ -144,6 +170,12 @@ SIGNATURES = {
     "pgcn_group_norm_workspace_size": (_sz, [_i32, _i32, _i32, _i64, _i64]),
     "pgcn_group_norm_fwd": (_i32, [C.POINTER(pgcn_group_norm_fwd_args), _vp]),
     "pgcn_group_norm_bwd": (_i32, [C.POINTER(pgcn_group_norm_bwd_args), _vp]),
+    "pgcn_mx_quantize": (_i32, [C.POINTER(pgcn_mx_quantize_args), _vp]),
+    "pgcn_mx_dequantize": (_i32, [C.POINTER(pgcn_mx_dequantize_args), _vp]),
+    "pgcn_mx_wgrad_workspace_size": (_sz, [_i32, _i64, _i32, _i32]),
+    "pgcn_mx_wgrad": (_i32, [C.POINTER(pgcn_mx_wgrad_args), _vp]),
+    "pgcn_mx_matmul_workspace_size": (_sz, [_i32, _i64, _i32, _i32]),
+    "pgcn_mx_matmul": (_i32, [C.POINTER(pgcn_mx_matmul_args), _vp]),
     "pgcn_trace_enable": (_i32, [_i32]),
     "pgcn_trace_filter": (_i32, [C.c_uint32]),
     "pgcn_trace_collect": (_i32, [_vp, _vp, _vp, _i32, C.POINTER(_i32)]),
@@ -408,9 +440,51 @@ def pgcn_group_norm_bwd(*, dtype, act, channels, groups, samples, sample_rows, l
     _check(lib.pgcn_group_norm_bwd(C.byref(a), _stream(stream)), "pgcn_group_norm_bwd")
 
 
+def mx_strides(format: int, cols: int) -> tuple:
+    """(ld_q, ld_s): the smallest strides of rows of `cols` elements in blocks."""
+    blocks = (cols + PGCN_MX_BLOCK - 1) // PGCN_MX_BLOCK
+    return blocks * (32 if format == PGCN_MX_INT8 else 16), (blocks + 3) // 4 * 4
+
+
+def pgcn_mx_quantize(*, format, dtype, rows, cols, src_rows, ld_x, ld_q, ld_s, X, Q, S, transpose=False, index=None,
+                     stream=None):
+    a = pgcn_mx_quantize_args(format, dtype, int(transpose), cols, rows, src_rows, ld_x, ld_q, ld_s,
+                              *_ptrs(X, index, Q, S))
+    _check(lib.pgcn_mx_quantize(C.byref(a), _stream(stream)), "pgcn_mx_quantize")
+
+
+def pgcn_mx_dequantize(*, format, dtype, rows, cols, ld_q, ld_s, ld_out, Q, S, out, gamma=0.0, stream=None):
+    a = pgcn_mx_dequantize_args(format, dtype, cols, gamma, rows, ld_q, ld_s, ld_out, *_ptrs(Q, S, out))
+    _check(lib.pgcn_mx_dequantize(C.byref(a), _stream(stream)), "pgcn_mx_dequantize")
+
+
+def pgcn_mx_wgrad_workspace_size(dtype: int, rows: int, f_in: int, f_out: int) -> int:
+    return int(lib.pgcn_mx_wgrad_workspace_size(dtype, rows, f_in, f_out))
+
+
+def pgcn_mx_wgrad(*, dtype, rows, f_in, f_out, ld_q, ld_s, ld_j, Q, S, J, dW, ld_h=0, H=None, workspace=None,
+                  workspace_bytes=0, stream=None):
+    a = pgcn_mx_wgrad_args(dtype, f_in, f_out, rows, ld_q, ld_s, ld_j, ld_h, *_ptrs(Q, S, J, H, dW, workspace),
+                           workspace_bytes)
+    _check(lib.pgcn_mx_wgrad(C.byref(a), _stream(stream)), "pgcn_mx_wgrad")
+
+
+def pgcn_mx_matmul_workspace_size(dtype: int, m: int, n: int, k: int) -> int:
+    return int(lib.pgcn_mx_matmul_workspace_size(dtype, m, n, k))
+
+
+def pgcn_mx_matmul(*, dtype, m, n, k, ld_a, ld_a_scales, ld_b, ld_b_scales, ld_c, A, A_scales, B, B_scales, C,
+                   relu=False, workspace=None, workspace_bytes=0, stream=None):
+    a = pgcn_mx_matmul_args(dtype, int(relu), m, n, k, ld_a, ld_a_scales, ld_b, ld_b_scales, ld_c,
+                            *_ptrs(A, A_scales, B, B_scales, C, workspace), workspace_bytes)
+    _check(lib.pgcn_mx_matmul(_byref(a), _stream(stream)), "pgcn_mx_matmul")
+
+
 TRACE_KINDS = ["agg_fwd", "agg_bwd", "agg_fixup", "gemm_fwd", "gemm_dgrad", "gemm_wgrad", "wgrad_reduce", "ema",
                "pack", "accum", "loss", "sgd", "refill", "gemm_pack", "dropout", "adam", "mask_scale",
                "accum_ema", "top_logits", "distill", "group_norm", "group_norm_bwd"]
+# the kinds that follow them: the operators in 8 and 4 bits
+MX_TRACE_KINDS = ["mx_quantize", "mx_dequantize", "mx_wgrad", "mx_matmul"]
 
 
 def pgcn_trace_enable(capacity: int):
@@ -418,8 +492,8 @@ def pgcn_trace_enable(capacity: int):
 
 
 def pgcn_trace_filter(kinds=None):
-    """Record only the named kinds (names of TRACE_KINDS); None records all."""
-    mask = 0xFFFFFFFF if kinds is None else sum(1 << TRACE_KINDS.index(k) for k in kinds)
+    """Record only the named kinds (names of TRACE_KINDS and MX_TRACE_KINDS); None records all."""
+    mask = 0xFFFFFFFF if kinds is None else sum(1 << (TRACE_KINDS + MX_TRACE_KINDS).index(k) for k in kinds)
     _check(lib.pgcn_trace_filter(mask), "pgcn_trace_filter")
 
 
@@ -432,8 +506,8 @@ def pgcn_trace_collect(max_records: int = 1 << 16):
     cnt = C.c_int32(0)
     _check(lib.pgcn_trace_collect(kinds.ctypes.data, ms.ctypes.data, nl.ctypes.data, max_records, C.byref(cnt)),
            "pgcn_trace_collect")
-    n = cnt.value
-    return [(TRACE_KINDS[k], float(v), int(c)) for k, v, c in zip(kinds[:n], ms[:n], nl[:n])]
+    n, names = cnt.value, TRACE_KINDS + MX_TRACE_KINDS
+    return [(names[k], float(v), int(c)) for k, v, c in zip(kinds[:n], ms[:n], nl[:n])]
 
 
 def pgcn_trace_disable():

@@ -755,6 +755,24 @@ static void tn_launch(TNParams p, bool bf16, bool a32, bool parts, int splits, h
   else hipLaunchKernelGGL((gemm_tn_f32<BM, BN>), grid, dim3(256), 0, s, p);
 }
 
+// out[i] = sum of splits' partials ws[z mn + i] in a fixed order.
+int launch_splitk_reduce(const float *ws, int splits, int64_t mn, float *out, hipStream_t s) {
+  TraceScope ts(PGCN_TK_WGRAD_REDUCE, s);
+  // 64 outputs per workgroup, or 16 (64 split ranges each) when that would
+  // leave fewer than four workgroups per CU: the sums stay short and many
+  const bool narrow = (mn + 63) / 64 < 1024;
+  const dim3 rgrid((unsigned)(narrow ? (mn + 15) / 16 : (mn + 63) / 64));
+  if (mn % 4 == 0 && ((uintptr_t)ws & 15u) == 0) {   // every partial [M x N] starts 16-byte aligned
+    if (narrow) hipLaunchKernelGGL((splitk_reduce_kernel<4, 16>), rgrid, dim3(256), 0, s, ws, splits, mn, out);
+    else hipLaunchKernelGGL((splitk_reduce_kernel<4, 64>), rgrid, dim3(256), 0, s, ws, splits, mn, out);
+  } else {
+    if (narrow) hipLaunchKernelGGL((splitk_reduce_kernel<1, 16>), rgrid, dim3(256), 0, s, ws, splits, mn, out);
+    else hipLaunchKernelGGL((splitk_reduce_kernel<1, 64>), rgrid, dim3(256), 0, s, ws, splits, mn, out);
+  }
+  PGCN_HIP(hipGetLastError());
+  return PGCN_OK;
+}
+
 int launch_gemm(Gemm kind, const GemmArgs &g, hipStream_t s) {
   if (kind != Gemm::TN_MASK_SPLITK) return set_error(PGCN_EINVAL, "launch_gemm: only the weight-gradient GEMM");
   if (g.M <= 0 || g.N <= 0) return PGCN_OK;
@@ -798,22 +816,7 @@ int launch_gemm(Gemm kind, const GemmArgs &g, hipStream_t s) {
     else tn_launch<128, 128>(p, bf16, a32, parts, splits, s);
     PGCN_HIP(hipGetLastError());
   }
-  const int64_t mn = (int64_t)g.M * g.N;
-  TraceScope ts(PGCN_TK_WGRAD_REDUCE, s);
-  // 64 outputs per workgroup, or 16 (64 split ranges each) when that would
-  // leave fewer than four workgroups per CU: the sums stay short and many
-  const bool narrow = (mn + 63) / 64 < 1024;
-  const dim3 rgrid((unsigned)(narrow ? (mn + 15) / 16 : (mn + 63) / 64));
-  const float *ws = (const float *)g.workspace;
-  if (mn % 4 == 0 && ((uintptr_t)g.workspace & 15u) == 0) {   // every partial [M x N] starts 16-byte aligned
-    if (narrow) hipLaunchKernelGGL((splitk_reduce_kernel<4, 16>), rgrid, dim3(256), 0, s, ws, splits, mn, g.C);
-    else hipLaunchKernelGGL((splitk_reduce_kernel<4, 64>), rgrid, dim3(256), 0, s, ws, splits, mn, g.C);
-  } else {
-    if (narrow) hipLaunchKernelGGL((splitk_reduce_kernel<1, 16>), rgrid, dim3(256), 0, s, ws, splits, mn, g.C);
-    else hipLaunchKernelGGL((splitk_reduce_kernel<1, 64>), rgrid, dim3(256), 0, s, ws, splits, mn, g.C);
-  }
-  PGCN_HIP(hipGetLastError());
-  return PGCN_OK;
+  return launch_splitk_reduce((const float *)g.workspace, splits, (int64_t)g.M * g.N, g.C, s);
 }
 
 }  // namespace pgcn

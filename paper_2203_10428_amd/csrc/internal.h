@@ -314,6 +314,7 @@ inline TnSplit tn_split(int K, int tiles, int splits, int slab) {
 }
 int launch_gemm(Gemm kind, const GemmArgs &g, hipStream_t s);
 size_t gemm_workspace(Gemm kind, int32_t M, int32_t N, int32_t K);
+int launch_splitk_reduce(const float *ws, int splits, int64_t mn, float *out, hipStream_t s);
 // forward and feature-gradient GEMMs: weights packed into g.workspace first
 int launch_gemm_nk(Gemm kind, const GemmArgs &g, hipStream_t s);
 size_t gemm_nk_workspace(int32_t N, int32_t K, int32_t dtype);

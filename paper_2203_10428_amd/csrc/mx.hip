@@ -1,0 +1,144 @@
+// Rows in 8 and 4 bits: quantised as they are written (gathered or transposed), and read back with a moving
+// average.  Per block of 32 elements: s from the largest magnitude, q = round(x / 2^(s - 127) 64) or the nearest
+// of the 4-bit magnitudes.  All of it is exact but the one rounding of an element.
+#include "mx.h"
+
+namespace pgcn {
+
+namespace {
+
+constexpr int kThreads = 256;
+
+struct QuantArgs {
+  const void *X;
+  const int32_t *index;
+  uint8_t *Q, *S;
+  int64_t rows, src_rows, ld_x, ld_q, ld_s;
+  int32_t cols;
+  Chunks chunks;        // of 8 elements, four to a block
+};
+
+// Four neighbouring lanes to a block, eight elements each.
+template <class T, class F>
+__global__ __launch_bounds__(kThreads) void quantize_rows(QuantArgs a) {
+  const int64_t first = (int64_t)blockIdx.x * kThreads;
+  const int64_t row0 = first / a.chunks.per;
+  const uint32_t at = (uint32_t)(first - row0 * a.chunks.per) + threadIdx.x;
+  if (first + threadIdx.x >= a.chunks.total) return;     // whole blocks: a row's chunks are a multiple of four
+  const uint32_t down = chunk_row(a.chunks, at), c = at - down * a.chunks.per;
+  const int64_t row = row0 + down;
+  const int64_t src = a.index ? a.index[row] : row;
+  float x[8];
+  const bool some = src >= 0 && src < a.src_rows;
+  load8(T{}, (const typename T::type *)a.X + (some ? src * a.ld_x + 8 * (int64_t)c : 0), some ? a.cols - 8 * (int64_t)c : 0, x);
+  uint32_t m = 0u;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) m = max(m, __float_as_uint(x[e]) & 0x7fffffffu);
+  m = max(m, __float_as_uint(lane_move<0xB1>(__uint_as_float(m))));
+  m = max(m, __float_as_uint(lane_move<0x4E>(__uint_as_float(m))));
+  const uint32_t s = src >= a.src_rows ? 255u : scale_byte<F>(m);
+  *reinterpret_cast<typename Bits8<F>::type *>(a.Q + row * a.ld_q + (int64_t)c * (F::kBytes / 4)) = pack8(F{}, x, s);
+  if (c % 4 == 0) a.S[row * a.ld_s + c / 4] = (uint8_t)s;
+}
+
+// The transpose: a thread to a block, 32 rows of one column.
+template <class T, class F>
+__global__ __launch_bounds__(kThreads) void quantize_cols(QuantArgs a, uint32_t col_groups) {
+  const int64_t block = blockIdx.x / col_groups;
+  const int64_t col = (int64_t)(blockIdx.x - block * col_groups) * kThreads + threadIdx.x;
+  if (col >= a.cols) return;
+  const typename T::type *X = (const typename T::type *)a.X + col;
+  uint32_t m = 0u;
+  for (int64_t r = 32 * block; r < min(a.rows, 32 * block + 32); ++r) m = max(m, __float_as_uint(T::get(X + r * a.ld_x)) & 0x7fffffffu);
+  const uint32_t s = scale_byte<F>(m);
+  for (int i = 0; i < 4; ++i) {
+    float x[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const int64_t r = 32 * block + 8 * i + e;
+      x[e] = r < a.rows ? T::get(X + r * a.ld_x) : 0.f;
+    }
+    *reinterpret_cast<typename Bits8<F>::type *>(a.Q + col * a.ld_q + (4 * block + i) * (F::kBytes / 4)) = pack8(F{}, x, s);
+  }
+  a.S[col * a.ld_s + block] = (uint8_t)s;
+}
+
+struct ReadArgs {
+  const uint8_t *Q, *S;
+  void *out;
+  int64_t ld_q, ld_s, ld_out;
+  int32_t cols;
+  float gamma, rest;       // rest = 1 - gamma
+  Chunks chunks;           // of 8 elements that hold some of a row's
+};
+
+template <class T, class F, bool kAverage>
+__global__ __launch_bounds__(kThreads) void read_rows(ReadArgs a) {
+  const int64_t first = (int64_t)blockIdx.x * kThreads;
+  const int64_t row0 = first / a.chunks.per;
+  const uint32_t at = (uint32_t)(first - row0 * a.chunks.per) + threadIdx.x;
+  if (first + threadIdx.x >= a.chunks.total) return;
+  const uint32_t down = chunk_row(a.chunks, at), c = at - down * a.chunks.per;
+  const int64_t row = row0 + down;
+  float v[8];
+  unpack8(F{}, *reinterpret_cast<const typename Bits8<F>::type *>(a.Q + row * a.ld_q + (int64_t)c * (F::kBytes / 4)),
+          a.S[row * a.ld_s + c / 4], v);
+  typename T::type *out = (typename T::type *)a.out + row * a.ld_out + 8 * (int64_t)c;
+  const int n = a.cols - 8 * (int)c;
+  if (kAverage) {
+    float x[8];
+    load8(T{}, out, n, x);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = __builtin_fmaf(a.gamma, x[e], a.rest * v[e]);
+  }
+#pragma unroll
+  for (int i = 0; i < 8 / T::E; ++i) {
+    float w[T::E];
+#pragma unroll
+    for (int e = 0; e < T::E; ++e) w[e] = v[i * T::E + e];
+    if (n > i * T::E) store_some<T>(out + i * T::E, w, n - i * T::E);
+  }
+}
+
+template <class T, class F>
+void quantize(const QuantArgs &a, bool transpose, hipStream_t s) {
+  if (transpose) {
+    const int64_t groups = (a.cols + kThreads - 1) / kThreads, blocks = mx_blocks(a.rows);
+    hipLaunchKernelGGL((quantize_cols<T, F>), dim3((unsigned)(groups * blocks)), dim3(kThreads), 0, s, a, (uint32_t)groups);
+  } else {
+    hipLaunchKernelGGL((quantize_rows<T, F>), dim3((unsigned)((a.chunks.total + kThreads - 1) / kThreads)), dim3(kThreads), 0, s, a);
+  }
+}
+
+}  // namespace
+
+int launch_mx_quantize(const pgcn_mx_quantize_args &x, hipStream_t s) {
+  QuantArgs a{x.X, x.index, x.Q, x.S, x.rows, x.src_rows, x.ld_x, x.ld_q, x.ld_s, x.cols, chunks_of(x.rows, 4 * mx_blocks(x.cols))};
+  TraceScope ts(PGCN_TK_MX_QUANTIZE, s);
+  const bool int8 = x.format == PGCN_MX_INT8;
+  if (x.dtype == PGCN_BF16) int8 ? quantize<BF16, Int8>(a, x.transpose, s) : quantize<BF16, Fp4>(a, x.transpose, s);
+  else int8 ? quantize<F32, Int8>(a, x.transpose, s) : quantize<F32, Fp4>(a, x.transpose, s);
+  PGCN_HIP(hipGetLastError());
+  return PGCN_OK;
+}
+
+int launch_mx_dequantize(const pgcn_mx_dequantize_args &x, hipStream_t s) {
+  const ReadArgs a{x.Q, x.S, x.out, x.ld_q, x.ld_s, x.ld_out, x.cols, x.gamma, 1.f - x.gamma, chunks_of(x.rows, (x.cols + 7) / 8)};
+  const dim3 grid((unsigned)((a.chunks.total + kThreads - 1) / kThreads)), block(kThreads);
+  TraceScope ts(PGCN_TK_MX_DEQUANTIZE, s);
+  const bool int8 = x.format == PGCN_MX_INT8;
+  if (x.dtype == PGCN_BF16) {
+    if (int8) hipLaunchKernelGGL((read_rows<BF16, Int8, false>), grid, block, 0, s, a);
+    else hipLaunchKernelGGL((read_rows<BF16, Fp4, false>), grid, block, 0, s, a);
+  } else if (x.gamma > 0.f) {
+    if (int8) hipLaunchKernelGGL((read_rows<F32, Int8, true>), grid, block, 0, s, a);
+    else hipLaunchKernelGGL((read_rows<F32, Fp4, true>), grid, block, 0, s, a);
+  } else {
+    if (int8) hipLaunchKernelGGL((read_rows<F32, Int8, false>), grid, block, 0, s, a);
+    else hipLaunchKernelGGL((read_rows<F32, Fp4, false>), grid, block, 0, s, a);
+  }
+  PGCN_HIP(hipGetLastError());
+  return PGCN_OK;
+}
+
+}  // namespace pgcn

@@ -18,12 +18,24 @@ int launch_group_norm_fwd(const pgcn_group_norm_fwd_args &a, hipStream_t s);
 int launch_group_norm_bwd(const pgcn_group_norm_bwd_args &a, hipStream_t s);
 size_t group_norm_workspace(int32_t dtype, int32_t channels, int32_t groups, int64_t samples, int64_t sample_rows);
 
+int launch_mx_quantize(const pgcn_mx_quantize_args &a, hipStream_t s);
+int launch_mx_dequantize(const pgcn_mx_dequantize_args &a, hipStream_t s);
+int launch_mx_wgrad(const pgcn_mx_wgrad_args &a, hipStream_t s);
+size_t mx_wgrad_workspace(int32_t dtype, int64_t rows, int32_t f_in, int32_t f_out);
+int launch_mx_matmul(const pgcn_mx_matmul_args &a, hipStream_t s);
+size_t mx_matmul_workspace(int32_t dtype, int64_t m, int32_t n, int32_t k);
+
+// Blocks of a row in 8 or 4 bits, and the bytes that its elements take.
+inline int64_t mx_blocks(int64_t cols) { return (cols + PGCN_MX_BLOCK - 1) / PGCN_MX_BLOCK; }
+inline int64_t mx_row_bytes(int32_t format, int64_t cols) { return mx_blocks(cols) * (format == PGCN_MX_INT8 ? 32 : 16); }
+
 #ifdef __HIPCC__
 // ---- device helpers ---------------------------------------------------------
 
 // A row's elements in 16-byte vectors: 4 floats or 8 bf16 values, computed on as floats.
 typedef float op_f32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t op_u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t op_u32x2 __attribute__((ext_vector_type(2)));
 
 struct F32 {
   typedef float type;
