@@ -42,6 +42,13 @@ def test_product(m, n, k, dtype):
     check(matmul(A, SA, Bq, SB, m, n, k, dtype, relu), a, b, m, n, k, dtype, relu)
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("m,n,k", [(2050, 2100, 290), (4100, 4000, 70), (4090, 4200, 300)])
+def test_many_tiles(m, n, k, dtype):
+    """Enough rows and columns for the larger tiles, with ragged edges; an even and an odd number of slabs, part of one."""
+    test_product(m, n, k, dtype)
+
+
 @pytest.mark.parametrize("m", [1, 20, 300])
 def test_scales_far_apart(m):
     rng = np.random.default_rng(m)
