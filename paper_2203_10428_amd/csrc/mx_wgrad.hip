@@ -1,6 +1,12 @@
-// Weight gradient from a layer's input held in 8 bits: dW = v^T (J o 1[H > 0]), a sum over the rows.  The rows
-// are cut into splits; a workgroup adds one tile over one split, and a second launch adds the splits' partial
-// tiles in a fixed order.
+// Weight gradient from a layer's input held in 8 bits: dW = v^T (J o 1[H > 0]), a sum over the rows (nodes).
+//
+// Every v is exact in bf16, so the product runs on the bf16 matrix cores: with J o mask in three exact bf16 parts
+// (fp32 arithmetic: three products where two fp32 operands take six), or rounded to bf16 once.
+// The rows are cut into splits; a workgroup adds one BM x BN tile over one split in slabs of 16 rows, and a second
+// launch adds the splits' partial tiles in a fixed order.  A slab goes through registers into LDS as it lies in
+// memory, a row of features after another, and the transposing LDS reads give each lane the four rows' values of one
+// feature that the matrix instruction wants.  Two LDS stages and two register sets: loads have two slabs of
+// products to arrive.
 #include <algorithm>
 
 #include "mx.h"
@@ -9,7 +15,11 @@ namespace pgcn {
 
 namespace {
 
-constexpr int kTile = 64, kSlab = 16;
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef short i16x4 __attribute__((ext_vector_type(4)));
+
+constexpr int kSlab = 16, kPad = 32;       // rows; bf16 elements behind a row in LDS: four rows read together are on other banks
 
 struct WgradArgs {
   const uint8_t *Q, *S;
@@ -19,89 +29,253 @@ struct WgradArgs {
   int32_t f_in, f_out, tiles_n, tiles;
 };
 
-struct Split {
-  int64_t chunk;
-  int splits;
-};
-Split wgrad_split(int64_t rows, int32_t f_in, int32_t f_out) {
-  const int64_t tiles = (int64_t)((f_in + kTile - 1) / kTile) * ((f_out + kTile - 1) / kTile);
-  int64_t s = std::max<int64_t>(1, std::min<int64_t>(1024 / tiles, (rows + 63) / 64));
-  const int64_t chunk = std::max<int64_t>(kSlab, ((rows + s - 1) / s + kSlab - 1) / kSlab * kSlab);
-  return Split{chunk, (int)std::max<int64_t>(1, (rows + chunk - 1) / chunk)};
+// Eight INT8 elements as bf16: (u - 128) step, u = q + 128, is exact, so its high half is the value.
+__device__ __forceinline__ op_u32x4 bf16_of(const op_u32x2 &q, float step) {
+  op_u32x4 w;
+  const float off = -128.f * step;
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const uint32_t u = q[i] ^ 0x80808080u;
+    const float a = __builtin_fmaf((float)(u & 0xffu), step, off), b = __builtin_fmaf((float)((u >> 8) & 0xffu), step, off);
+    const float c = __builtin_fmaf((float)((u >> 16) & 0xffu), step, off), d = __builtin_fmaf((float)(u >> 24), step, off);
+    w[2 * i] = __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u);
+    w[2 * i + 1] = __builtin_amdgcn_perm(__float_as_uint(d), __float_as_uint(c), 0x07060302u);
+  }
+  return w;
 }
 
-template <bool kBf16>
-__global__ __launch_bounds__(256) void wgrad(WgradArgs a) {
-  __shared__ float As[kSlab][kTile + 4], Bs[kSlab][kTile + 4];
-  const int t = threadIdx.x, tile = blockIdx.x % a.tiles;
-  const int64_t split = blockIdx.x / a.tiles;
-  const int m0 = tile / a.tiles_n * kTile, n0 = tile % a.tiles_n * kTile;
-  const int64_t begin = split * a.chunk, end = min(a.rows, begin + a.chunk);
-  const int r = t / 16, c = 4 * (t % 16);               // staging: a row of the slab, four columns
-  float acc[4][4] = {};
-  for (int64_t k = begin; k < end; k += kSlab) {
-    const int64_t row = k + r;
-    float x[4] = {0.f, 0.f, 0.f, 0.f}, y[4] = {0.f, 0.f, 0.f, 0.f};
-    if (row < end && m0 + c < a.f_in) {
-      const uint32_t q = *reinterpret_cast<const uint32_t *>(a.Q + row * a.ld_q + m0 + c);
-      const float step = int8_step(a.S[row * a.ld_s + (m0 + c) / 32]);
+// Two floats in three bf16 parts each: the high half, what is left rounded to nearest, and the rest.
+__device__ __forceinline__ void parts2(float x, float y, uint32_t (&p)[3]) {
+  const uint32_t a = __float_as_uint(x), b = __float_as_uint(y);
+  p[0] = __builtin_amdgcn_perm(b, a, 0x07060302u);
+  const float r = x - __uint_as_float(a & 0xffff0000u), s = y - __uint_as_float(b & 0xffff0000u);
+  p[1] = BF16::two(r, s);
+  p[2] = BF16::two(r - __uint_as_float(p[1] << 16), s - __uint_as_float(p[1] & 0xffff0000u));
+}
+
+// Four rows' values of this lane's feature, from a place of its own in four rows of 16 neighbouring features.
+__device__ __forceinline__ bf16x8 transposed(const uint16_t *lo, const uint16_t *hi) {
+  typedef __attribute__((address_space(3))) i16x4 *lds;
+  const i16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds)lo), b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds)hi);
+  typedef short i16x8 __attribute__((ext_vector_type(8)));
+  return __builtin_bit_cast(bf16x8, (i16x8){a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]});
+}
+
+template <int BM, int BN, int kParts, bool kMasked>
+__global__ __launch_bounds__(256, 2) void wgrad(WgradArgs p) {
+  constexpr int LA = BM + kPad, LB = BN + kPad;
+  constexpr int CA = BM / 8, CB = BN / 4, RA = 256 / CA, RB = 256 / CB, VA = kSlab / RA, VB = kSlab / RB;
+  constexpr int WM = BM / 2, WN = BN / 2, TM = WM / 32, TN = WN / 32;
+  static_assert(VA >= 1 && VB >= 1, "a slab holds an item for every thread");
+  __shared__ __attribute__((aligned(16))) uint16_t As[2][kSlab * LA];
+  __shared__ __attribute__((aligned(16))) uint16_t Bs[2][kParts][kSlab * LB];
+
+  const int t = threadIdx.x, lane = t % 64, wave = __builtin_amdgcn_readfirstlane(t / 64);
+  // a split's tiles are neighbours on one XCD: its rows are read there several times
+  const uint32_t g = blockIdx.x, l = gridDim.x % 8 == 0 ? (g % 8) * (gridDim.x / 8) + g / 8 : g;
+  const uint32_t split = l / (uint32_t)p.tiles, tile = l - split * (uint32_t)p.tiles;
+  const int m0 = (int)(tile / p.tiles_n) * BM, n0 = (int)(tile % p.tiles_n) * BN;
+  const int64_t begin = split * p.chunk, end = min(p.rows, begin + p.chunk);
+
+  // staging: row ra + RA i and eight features of v, row rb + RB i and four of J
+  const int ca = 8 * (t % CA), ra = t / CA, cb = 4 * (t % CB), rb = t / CB;
+  struct Regs {
+    op_u32x2 q[VA];
+    uint32_t s[VA];
+    op_f32x4 j[VB], h[VB];
+  };
+  // Columns past the matrix read its first ones: their products are not stored.
+  const int64_t col_q = m0 + ca < p.f_in ? m0 + ca : 0, col_j = n0 + cb < p.f_out ? n0 + cb : 0;
+  const int64_t off_q = ra * p.ld_q + col_q, off_s = ra * p.ld_s + col_q / 32, off_j = rb * p.ld_j + col_j, off_h = rb * p.ld_h + col_j;
+  auto load = [&](Regs &R, int64_t k) __attribute__((always_inline)) {
 #pragma unroll
-      for (int e = 0; e < 4; ++e) x[e] = (float)(int)(int8_t)(q >> (8 * e)) * step;
+    for (int i = 0; i < VA; ++i) {
+      R.q[i] = *reinterpret_cast<const op_u32x2 *>(p.Q + (k + RA * i) * p.ld_q + off_q);
+      R.s[i] = (p.S + (k + RA * i) * p.ld_s)[off_s];
     }
-    if (row < end && n0 + c < a.f_out) {
-      const op_f32x4 j = *reinterpret_cast<const op_f32x4 *>(a.J + row * a.ld_j + n0 + c);
-      op_f32x4 h = {1.f, 1.f, 1.f, 1.f};
-      if (a.H) h = *reinterpret_cast<const op_f32x4 *>(a.H + row * a.ld_h + n0 + c);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        y[e] = h[e] > 0.f ? j[e] : 0.f;
-        if (kBf16) y[e] = (float)(__bf16)y[e];
+    for (int i = 0; i < VB; ++i) {
+      R.j[i] = *reinterpret_cast<const op_f32x4 *>(p.J + (k + RB * i) * p.ld_j + off_j);
+      if (kMasked) R.h[i] = *reinterpret_cast<const op_f32x4 *>(p.H + (k + RB * i) * p.ld_h + off_h);
+    }
+  };
+  auto load_last = [&](Regs &R, int64_t k) __attribute__((always_inline)) {      // zeros for rows past the last one
+#pragma unroll
+    for (int i = 0; i < VA; ++i) {
+      const int64_t row = k + ra + RA * i;
+      const bool in = row < p.rows;
+      R.q[i] = in ? *reinterpret_cast<const op_u32x2 *>(p.Q + row * p.ld_q + col_q) : op_u32x2{0u, 0u};
+      R.s[i] = in ? p.S[row * p.ld_s + col_q / 32] : 0u;
+    }
+#pragma unroll
+    for (int i = 0; i < VB; ++i) {
+      const int64_t row = k + rb + RB * i;
+      const bool in = row < p.rows;
+      R.j[i] = in ? *reinterpret_cast<const op_f32x4 *>(p.J + row * p.ld_j + col_j) : op_f32x4{0.f, 0.f, 0.f, 0.f};
+      if (kMasked) R.h[i] = in ? *reinterpret_cast<const op_f32x4 *>(p.H + row * p.ld_h + col_j) : op_f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+  };
+  auto store = [&](const Regs &R, int buf) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < VA; ++i)
+      *reinterpret_cast<op_u32x4 *>(&As[buf][(ra + RA * i) * LA + ca]) = bf16_of(R.q[i], int8_step(R.s[i]));
+#pragma unroll
+    for (int i = 0; i < VB; ++i) {
+      float x[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[e] = !kMasked || R.h[i][e] > 0.f ? R.j[i][e] : 0.f;
+      const int at = (rb + RB * i) * LB + cb;
+      if constexpr (kParts == 1) {
+        *reinterpret_cast<op_u32x2 *>(&Bs[buf][0][at]) = op_u32x2{BF16::two(x[0], x[1]), BF16::two(x[2], x[3])};
+      } else {
+        uint32_t u[3], v[3];
+        parts2(x[0], x[1], u);
+        parts2(x[2], x[3], v);
+#pragma unroll
+        for (int part = 0; part < 3; ++part) *reinterpret_cast<op_u32x2 *>(&Bs[buf][part][at]) = op_u32x2{u[part], v[part]};
       }
     }
-    __syncthreads();
+  };
+
+  f32x16 acc[TM][TN];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      As[r][c + e] = x[e];
-      Bs[r][c + e] = y[e];
+  for (int i = 0; i < TM; ++i)
+#pragma unroll
+    for (int j = 0; j < TN; ++j) acc[i][j] = (f32x16){};
+  // operand of the matrix instruction: feature lane % 32, rows 8 (lane / 32) + 0 .. 7 of the slab; 16 lanes read
+  // rows 0 .. 3 and then 4 .. 7 of those, four lanes to a row
+  const int h = lane / 32, wm0 = (wave / 2) * WM, wn0 = (wave % 2) * WN;
+  const int tr = 8 * h + (lane % 16) / 4, tc = 16 * ((lane / 16) % 2) + 4 * (lane % 4);
+  auto compute = [&](int buf) __attribute__((always_inline)) {
+    bf16x8 a[TM], b[2][TN];
+    auto read = [&](int part) __attribute__((always_inline)) {
+#pragma unroll
+      for (int j = 0; j < TN; ++j) {
+        const uint16_t *at = &Bs[buf][part][tr * LB + wn0 + 32 * j + tc];
+        b[part & 1][j] = transposed(at, at + 4 * LB);
+      }
+    };
+    read(kParts - 1);
+#pragma unroll
+    for (int i = 0; i < TM; ++i) {
+      const uint16_t *at = &As[buf][tr * LA + wm0 + 32 * i + tc];
+      a[i] = transposed(at, at + 4 * LA);
     }
+#pragma unroll
+    for (int part = kParts - 1; part >= 0; --part) {      // smallest first; the next part is read meanwhile
+      if (part > 0) read(part - 1);
+#pragma unroll
+      for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int j = 0; j < TN; ++j)
+          acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[i], b[part & 1][j], acc[i][j], 0, 0, 0);
+    }
+  };
+
+  const int64_t full = begin < end ? (end - begin) / kSlab : 0, last = begin + (full - 1) * kSlab;
+  Regs R0, R1;
+  if (full > 0) {
+    load(R0, begin);
+    load(R1, min(begin + kSlab, last));                   // past the last full slab: it again, not used
+    store(R0, 0);
     __syncthreads();
-    for (int i = 0; i < kSlab; ++i)
-#pragma unroll
-      for (int u = 0; u < 4; ++u)
-#pragma unroll
-        for (int v = 0; v < 4; ++v) acc[u][v] = __builtin_fmaf(As[i][4 * (t / 16) + u], Bs[i][4 * (t % 16) + v], acc[u][v]);
+    int64_t k = begin;
+    for (; k < last; k += 2 * kSlab) {
+      load(R0, min(k + 2 * kSlab, last));
+      compute(0);
+      store(R1, 1);
+      __syncthreads();
+      load(R1, min(k + 3 * kSlab, last));
+      compute(1);
+      store(R0, 0);
+      __syncthreads();
+    }
+    if (k == last) compute(0);
   }
-  float *out = a.out + split * a.f_in * a.f_out;
+  if (begin + full * kSlab < end) {                       // the rows that are left, fewer than a slab
+    load_last(R0, begin + full * kSlab);
+    store(R0, 1);
+    __syncthreads();
+    compute(1);
+  }
+
+  float *out = p.out + (int64_t)split * p.f_in * p.f_out;
+  const bool whole = m0 + BM <= p.f_in && n0 + BN <= p.f_out;
 #pragma unroll
-  for (int u = 0; u < 4; ++u)
+  for (int i = 0; i < TM; ++i)
 #pragma unroll
-    for (int v = 0; v < 4; ++v) {
-      const int m = m0 + 4 * (t / 16) + u, n = n0 + 4 * (t % 16) + v;
-      if (m < a.f_in && n < a.f_out) out[(int64_t)m * a.f_out + n] = acc[u][v];
-    }
+    for (int j = 0; j < TN; ++j)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        const int m = m0 + wm0 + 32 * i + 8 * (e / 4) + 4 * h + e % 4, n = n0 + wn0 + 32 * j + lane % 32;
+        if (whole || (m < p.f_in && n < p.f_out)) out[(int64_t)m * p.f_out + n] = acc[i][j][e];
+      }
+}
+
+struct Shape {
+  int bm, bn, splits;
+  int64_t chunk;
+};
+
+// Tile: 256 features of v where that fills up no more than 128 do, since a slab's J is split into its parts by
+// every tile row (239,000 x 512 x 512 fp32: 335 us with 256, 353 with 128; 58,000 x 602 x 256, which 256 would
+// fill up to 768: 93 against 76).
+// Splits: as many workgroups as are resident at once.  256-row tiles two to a compute unit, 128-row tiles three
+// (58,000 x 602 x 256: 76 us and 8 for adding the partial tiles, at two 85 and 6); bf16, which waits for memory, two
+// (58,000 x 602 x 256: 67, at three 65 and 2 more for the partial tiles), and where one tile is all there is, one:
+// half as many partial tiles (306,000 x 128 x 128: 68 + 7, at two 70 + 12).  At least 64 rows to a split; where that
+// leaves compute units idle down to 32, as a workgroup's slabs are a chain.  Partial tiles stay below 64 MB a matrix.
+Shape shape_of(int32_t dtype, int64_t rows, int32_t f_in, int32_t f_out) {
+  Shape c;
+  c.bn = f_out <= 64 ? 64 : 128;
+  c.bm = f_in <= 128 || c.bn == 64 || (f_in + 255) / 256 * 256 > (f_in + 127) / 128 * 128 ? 128 : 256;
+  const int64_t tiles = (int64_t)((f_in + c.bm - 1) / c.bm) * ((f_out + c.bn - 1) / c.bn);
+  const int64_t slots = c.bm == 256 ? 512 : dtype == PGCN_F32 ? 768 : tiles == 1 && c.bn == 128 ? 256 : 512;
+  const int64_t by_bytes = std::max<int64_t>(1, ((int64_t)64 << 20) / ((int64_t)f_in * f_out * 4));
+  int64_t s = std::max<int64_t>(1, std::min({slots / tiles, (rows + 63) / 64, by_bytes}));
+  if (tiles * s < 256) s = std::max(s, std::min({(rows + 31) / 32, (256 + tiles - 1) / tiles, by_bytes}));
+  int64_t e = s;                                          // a multiple of 8 workgroups: see the order of tiles
+  while (e > 1 && tiles * e % 8 != 0) --e;
+  if (tiles * e % 8 == 0 && 2 * e >= s) s = e;
+  c.chunk = std::max<int64_t>(kSlab, ((rows + s - 1) / s + kSlab - 1) / kSlab * kSlab);
+  c.splits = (int)std::max<int64_t>(1, (rows + c.chunk - 1) / c.chunk);
+  return c;
+}
+
+template <int BM, int BN>
+void launch_tile(const WgradArgs &a, int splits, bool bf16, hipStream_t s) {
+  const dim3 grid((unsigned)((int64_t)a.tiles * splits));
+  if (a.H) {
+    if (bf16) hipLaunchKernelGGL((wgrad<BM, BN, 1, true>), grid, dim3(256), 0, s, a);
+    else hipLaunchKernelGGL((wgrad<BM, BN, 3, true>), grid, dim3(256), 0, s, a);
+  } else {
+    if (bf16) hipLaunchKernelGGL((wgrad<BM, BN, 1, false>), grid, dim3(256), 0, s, a);
+    else hipLaunchKernelGGL((wgrad<BM, BN, 3, false>), grid, dim3(256), 0, s, a);
+  }
 }
 
 }  // namespace
 
-size_t mx_wgrad_workspace(int32_t, int64_t rows, int32_t f_in, int32_t f_out) {
-  const Split sp = wgrad_split(rows, f_in, f_out);
-  return sp.splits > 1 ? (size_t)sp.splits * f_in * f_out * sizeof(float) : 0;
+size_t mx_wgrad_workspace(int32_t dtype, int64_t rows, int32_t f_in, int32_t f_out) {
+  const Shape c = shape_of(dtype, rows, f_in, f_out);
+  return c.splits > 1 ? (size_t)c.splits * f_in * f_out * sizeof(float) : 0;
 }
 
 int launch_mx_wgrad(const pgcn_mx_wgrad_args &x, hipStream_t s) {
-  const Split sp = wgrad_split(x.rows, x.f_in, x.f_out);
-  WgradArgs a{x.Q, x.S, x.J, x.H, sp.splits > 1 ? (float *)x.workspace : x.dW, x.rows, x.ld_q, x.ld_s, x.ld_j, x.ld_h, sp.chunk,
-              x.f_in, x.f_out, (x.f_out + kTile - 1) / kTile, 0};
-  a.tiles = (x.f_in + kTile - 1) / kTile * a.tiles_n;
+  const Shape c = shape_of(x.dtype, x.rows, x.f_in, x.f_out);
+  WgradArgs a{x.Q, x.S, x.J, x.H, c.splits > 1 ? (float *)x.workspace : x.dW, x.rows, x.ld_q, x.ld_s, x.ld_j, x.ld_h, c.chunk,
+              x.f_in, x.f_out, (x.f_out + c.bn - 1) / c.bn, 0};
+  a.tiles = (x.f_in + c.bm - 1) / c.bm * a.tiles_n;
   {
     TraceScope ts(PGCN_TK_MX_WGRAD, s);
-    const dim3 grid((unsigned)(a.tiles * sp.splits));
-    if (x.dtype == PGCN_BF16) hipLaunchKernelGGL((wgrad<true>), grid, dim3(256), 0, s, a);
-    else hipLaunchKernelGGL((wgrad<false>), grid, dim3(256), 0, s, a);
+    const bool bf16 = x.dtype == PGCN_BF16;
+    if (c.bn == 64) launch_tile<128, 64>(a, c.splits, bf16, s);
+    else if (c.bm == 128) launch_tile<128, 128>(a, c.splits, bf16, s);
+    else launch_tile<256, 128>(a, c.splits, bf16, s);
     PGCN_HIP(hipGetLastError());
   }
-  if (sp.splits == 1) return PGCN_OK;
-  return launch_splitk_reduce((const float *)x.workspace, sp.splits, (int64_t)x.f_in * x.f_out, x.dW, s);
+  if (c.splits == 1) return PGCN_OK;
+  return launch_splitk_reduce((const float *)x.workspace, c.splits, (int64_t)x.f_in * x.f_out, x.dW, s);
 }
 
 }  // namespace pgcn
