@@ -67,8 +67,12 @@ enum pgcn_status {
  * PGCN_GEMM_F32=native (read per call) selects the fp32 matrix cores
  * instead.  A non-finite operand gives a non-finite (NaN) result.
  * PGCN_BF16: operands rounded once to bf16 (nearest even), products
- * accumulated in fp32. */
-enum pgcn_dtype { PGCN_F32 = 0, PGCN_BF16 = 1 };
+ * accumulated in fp32.
+ * PGCN_MXFP4 (pgcn_layer_fwd alone, aggregate first): both operands in the
+ * 4 bits of PGCN_MX_FP4, quantised along f_in in the call, products
+ * accumulated in fp32.  The layer's backward then runs in one of the others,
+ * with A as it was before it was quantised. */
+enum pgcn_dtype { PGCN_F32 = 0, PGCN_BF16 = 1, PGCN_MXFP4 = 2 };
 
 enum pgcn_setup_flags {
   PGCN_SETUP_HOST_ONLY = 1,     /* build the index structures on the host only: no
@@ -265,6 +269,8 @@ size_t pgcn_layer_workspace_size(const pgcn_partition *part, int32_t f_in, int32
  * a_given == 1 (aggregate first only) skips the aggregation: A is an input
  * holding P_i [H_in ; H_bd], e.g. a layer-1 aggregate kept across iterations
  * (the input features are constant); H_in / H_bd are then not read.
+ * With PGCN_MXFP4, A is required, A_bf16 ignored, H_out and W are 16-byte
+ * aligned, and the sent rows are copied after the product.
  */
 typedef struct {
   int32_t f_in, f_out;         /* 1 .. PGCN_MAX_WIDTH                            */
@@ -745,7 +751,7 @@ int pgcn_mx_dequantize(const pgcn_mx_dequantize_args *args, hipStream_t stream);
  * H NULL: no mask.  PGCN_F32: J in three bf16 parts that add up to it (v is exact in one), three exact
  * products each, fp32 sums: fp32 accuracy.  PGCN_BF16: J o mask rounded once to bf16, fp32 sums.  No rows: dW = 0.
  * A masked place of J adds nothing, whatever it holds.  A non-finite value among the others gives non-finite
- * or NaN results.
+ * or NaN results.  Values and parts below 2^-126 may be taken for 0.
  */
 typedef struct {
   int32_t dtype;               /* pgcn_dtype: the arithmetic, as for the update GEMMs */
@@ -764,9 +770,22 @@ size_t pgcn_mx_wgrad_workspace_size(int32_t dtype, int64_t rows, int32_t f_in, i
 int pgcn_mx_wgrad(const pgcn_mx_wgrad_args *args, hipStream_t stream);
 
 /*
+ * A layer's backward whose kept operands are held in 8 bits: pgcn_layer_bwd and pgcn_sage_layer_bwd, aggregate
+ * first, with dW from pgcn_mx_wgrad's product over A (for GraphSAGE: z, and X_in where it is given too).  The args'
+ * A, A_bf16 (and X_in, X_in_bf16) are then not read; everything else, the workspace among it, is as there.
+ */
+typedef struct {
+  const uint8_t *Q, *S;        /* [n_inner, ld_q], [n_inner, ld_s] PGCN_MX_INT8 of f_in elements */
+  int64_t ld_q, ld_s;
+} pgcn_mx_rows;
+int pgcn_layer_bwd_mx(const pgcn_partition *part, const pgcn_bwd_args *args, const pgcn_mx_rows *A, hipStream_t stream);
+int pgcn_sage_layer_bwd_mx(const pgcn_partition *part, const pgcn_sage_bwd_args *args, const pgcn_mx_rows *A,
+                           const pgcn_mx_rows *X_in, hipStream_t stream);
+
+/*
  * Product of two matrices of FP4 rows (PGCN_MX_FP4, values a and b) on the scaled matrix instructions:
  *     C[i, j] = sum over t of a[i, t] b[j, t],  relu: where negative 0           [m, n]
- * in fp32, sums in a fixed order.  The elements that fill up a row's last block count: zeros, as
+ * in fp32, sums in a fixed order: PGCN_MXFP4's product.  The elements that fill up a row's last block count: zeros, as
  * pgcn_mx_quantize writes them.  Terms or sums below 2^-126 may be taken for 0.  No rows of A: nothing to do.
  */
 typedef struct {

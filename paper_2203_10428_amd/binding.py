@@ -21,7 +21,7 @@ _PKG = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_PKG, "libpgcn.so")
 
 PGCN_OK, PGCN_EINVAL, PGCN_ENOMEM, PGCN_EHIP, PGCN_EUNSUPPORTED, PGCN_EWORKSPACE = range(6)
-PGCN_F32, PGCN_BF16 = 0, 1
+PGCN_F32, PGCN_BF16, PGCN_MXFP4 = 0, 1, 2
 PGCN_SETUP_HOST_ONLY, PGCN_SETUP_NO_SELF_LOOP, PGCN_SETUP_SYMMETRIC = 1, 2, 4
 PGCN_PACK_FEAT, PGCN_ACCUM_GRAD = 0, 1
 PGCN_MAX_WIDTH = 63740
@@ -133,6 +133,10 @@ class pgcn_mx_wgrad_args(C.Structure):
                 ("workspace", _vp), ("workspace_bytes", _sz)]
 
 
+class pgcn_mx_rows(C.Structure):
+    _fields_ = [("Q", _vp), ("S", _vp), ("ld_q", _i64), ("ld_s", _i64)]
+
+
 class pgcn_mx_matmul_args(C.Structure):
     _fields_ = [("dtype", _i32), ("relu", _i32), ("m", _i64), ("n", _i32), ("k", _i32), ("ld_a", _i64),
                 ("ld_a_scales", _i64), ("ld_b", _i64), ("ld_b_scales", _i64), ("ld_c", _i64), ("A", _vp),
@@ -174,6 +178,9 @@ SIGNATURES = {
     "pgcn_mx_dequantize": (_i32, [C.POINTER(pgcn_mx_dequantize_args), _vp]),
     "pgcn_mx_wgrad_workspace_size": (_sz, [_i32, _i64, _i32, _i32]),
     "pgcn_mx_wgrad": (_i32, [C.POINTER(pgcn_mx_wgrad_args), _vp]),
+    "pgcn_layer_bwd_mx": (_i32, [_vp, C.POINTER(pgcn_bwd_args), C.POINTER(pgcn_mx_rows), _vp]),
+    "pgcn_sage_layer_bwd_mx": (_i32, [_vp, C.POINTER(pgcn_sage_bwd_args), C.POINTER(pgcn_mx_rows),
+                                      C.POINTER(pgcn_mx_rows), _vp]),
     "pgcn_mx_matmul_workspace_size": (_sz, [_i32, _i64, _i32, _i32]),
     "pgcn_mx_matmul": (_i32, [C.POINTER(pgcn_mx_matmul_args), _vp]),
     "pgcn_trace_enable": (_i32, [_i32]),
@@ -311,12 +318,22 @@ def pgcn_layer_fwd_noalloc(part: Partition, *, f_in, f_out, gemm_dtype, relu, ld
     _check(lib.pgcn_layer_fwd_noalloc(part.handle, C.byref(a), _stream(stream)), "pgcn_layer_fwd_noalloc")
 
 
+def _mx_rows(x):
+    """pgcn_mx_rows of (Q, S), two byte matrices with strides; None stays None."""
+    return None if x is None else pgcn_mx_rows(_ptr(x[0]), _ptr(x[1]), x[0].stride(0), x[1].stride(0))
+
+
 def pgcn_layer_bwd(part: Partition, *, f_in, f_out, gemm_dtype, relu, ld_in, ld_out, J_out, H_out, A, A_bf16,
                    W, dW, J_in, J_bd_out, workspace, workspace_bytes, order=PGCN_ORDER_AGG, H_in=None, H_bd=None,
-                   stream=None):
+                   A_mx=None, stream=None):
+    """A_mx: (Q, S) of the layer's A in 8 bits, read in its place (pgcn_layer_bwd_mx)."""
     a = pgcn_bwd_args(f_in, f_out, gemm_dtype, int(relu), ld_in, ld_out, _ptr(J_out), _ptr(H_out), _ptr(A),
                       _ptr(A_bf16), _ptr(W), _ptr(dW), _ptr(J_in), _ptr(J_bd_out), _ptr(workspace),
                       workspace_bytes, order, _ptr(H_in), _ptr(H_bd))
+    if A_mx is not None:
+        _check(lib.pgcn_layer_bwd_mx(part.handle, C.byref(a), C.byref(_mx_rows(A_mx)), _stream(stream)),
+               "pgcn_layer_bwd_mx")
+        return
     _check(lib.pgcn_layer_bwd(part.handle, C.byref(a), _stream(stream)), "pgcn_layer_bwd")
 
 
@@ -364,10 +381,16 @@ def pgcn_sage_layer_fwd(part: Partition, *, f_in, f_out, gemm_dtype, relu, ld_in
 
 def pgcn_sage_layer_bwd(part: Partition, *, f_in, f_out, gemm_dtype, relu, ld_in, ld_out, J_out, H_out, A, A_bf16,
                         X_in, X_in_bf16, W, dW, J_in, J_bd_out, workspace, workspace_bytes, order=PGCN_ORDER_AGG,
-                        X_bd=None, stream=None):
+                        X_bd=None, A_mx=None, X_in_mx=None, stream=None):
+    """A_mx, X_in_mx: (Q, S) of z and X_in in 8 bits, read in their place (pgcn_sage_layer_bwd_mx)."""
     a = pgcn_sage_bwd_args(f_in, f_out, gemm_dtype, int(relu), ld_in, ld_out, _ptr(J_out), _ptr(H_out), _ptr(A),
                            _ptr(A_bf16), _ptr(X_in), _ptr(X_in_bf16), _ptr(W), _ptr(dW), _ptr(J_in),
                            _ptr(J_bd_out), _ptr(workspace), workspace_bytes, order, _ptr(X_bd))
+    if A_mx is not None:
+        x = _mx_rows(X_in_mx)
+        _check(lib.pgcn_sage_layer_bwd_mx(part.handle, C.byref(a), C.byref(_mx_rows(A_mx)), None if x is None else C.byref(x),
+                                          _stream(stream)), "pgcn_sage_layer_bwd_mx")
+        return
     _check(lib.pgcn_sage_layer_bwd(part.handle, C.byref(a), _stream(stream)), "pgcn_sage_layer_bwd")
 
 

@@ -3,7 +3,7 @@
 #include <cmath>
 #include <cstring>
 
-#include "internal.h"
+#include "ops.h"
 
 using namespace pgcn;
 
@@ -89,9 +89,31 @@ size_t fwd_acc_bytes(const pgcn_partition *p, int32_t f_in, int32_t gemm_dtype) 
 size_t fwd_agg_bytes(const pgcn_partition *p, int32_t f_in, int32_t gemm_dtype) {
   return fwd_part_bytes(p, f_in) + fwd_acc_bytes(p, f_in, gemm_dtype);
 }
+// PGCN_MXFP4: A and the transposed W in 4 bits, and the product's scratch, after the aggregation's
+struct Fp4Update {
+  size_t q_a, s_a, q_w, s_w, scratch;          // offsets from the update's part of the workspace
+  size_t bytes, scratch_bytes;
+  int64_t ld_q, ld_s;
+};
+Fp4Update fp4_update(const pgcn_partition *p, int32_t f_in, int32_t f_out) {
+  Fp4Update u;
+  u.ld_q = mx_row_bytes(PGCN_MX_FP4, f_in);
+  u.ld_s = (int64_t)align_up((size_t)mx_blocks(f_in), 4);
+  u.q_a = 0;
+  u.s_a = u.q_a + align_up((size_t)(p->n_inner * u.ld_q), 256);
+  u.q_w = u.s_a + align_up((size_t)(p->n_inner * u.ld_s), 256);
+  u.s_w = u.q_w + align_up((size_t)((int64_t)f_out * u.ld_q), 256);
+  u.scratch = u.s_w + align_up((size_t)((int64_t)f_out * u.ld_s), 256);
+  u.scratch_bytes = mx_matmul_workspace(PGCN_F32, p->n_inner, f_out, f_in);
+  u.bytes = u.scratch + align_up(u.scratch_bytes, 256);
+  return u;
+}
+size_t update_ws(const pgcn_partition *p, int32_t f_in, int32_t f_out, int32_t gemm_dtype) {
+  return gemm_dtype == PGCN_MXFP4 ? fp4_update(p, f_in, f_out).bytes : gemm_nk_workspace(f_out, f_in, gemm_dtype);
+}
 // symmetric normalisation, aggregate-first: the gathered rows scaled by d̃_u^{-1/2}
 size_t fwd_sym_off(const pgcn_partition *p, int32_t f_in, int32_t f_out, int32_t gemm_dtype) {
-  return fwd_agg_bytes(p, f_in, gemm_dtype) + gemm_nk_workspace(f_out, f_in, gemm_dtype);
+  return fwd_agg_bytes(p, f_in, gemm_dtype) + update_ws(p, f_in, f_out, gemm_dtype);
 }
 size_t fwd_ws(const pgcn_partition *p, int32_t f_in, int32_t f_out, int32_t gemm_dtype) {
   const size_t sym = p->symmetric ? align_up((size_t)(p->n_inner + p->n_bd) * (size_t)ld_rows(p, false, f_in) * sizeof(float), 256)
@@ -157,17 +179,17 @@ size_t bwd_ws_tf(const pgcn_partition *p, int32_t f_in, int32_t f_out, bool inpu
 // Workspace bytes one pgcn_layer_fwd call needs (0 for arguments it rejects).
 size_t pgcn::layer_fwd_workspace(const pgcn_partition *p, const pgcn_fwd_args *a) {
   if (!p || !a || a->f_in < 1 || a->f_out < 1 || a->f_in > PGCN_MAX_WIDTH || a->f_out > PGCN_MAX_WIDTH) return 0;
-  if (a->gemm_dtype != PGCN_F32 && a->gemm_dtype != PGCN_BF16) return 0;
+  if (a->gemm_dtype != PGCN_F32 && a->gemm_dtype != PGCN_BF16 && (a->gemm_dtype != PGCN_MXFP4 || a->order != PGCN_ORDER_AGG)) return 0;
   if (a->order == PGCN_ORDER_TRANSFORM) return fwd_ws_tf(p, a->f_in, a->f_out, a->gemm_dtype);
   if (a->order != PGCN_ORDER_AGG) return 0;
-  if (a->a_given) return gemm_nk_workspace(a->f_out, a->f_in, a->gemm_dtype);
+  if (a->a_given) return update_ws(p, a->f_in, a->f_out, a->gemm_dtype);
   return fwd_ws(p, a->f_in, a->f_out, a->gemm_dtype);
 }
 
 extern "C" size_t pgcn_layer_workspace_size(const pgcn_partition *p, int32_t f_in, int32_t f_out, int32_t gemm_dtype,
                                             int32_t order) try {
   if (order == PGCN_ORDER_AGG) return pgcn_workspace_size(p, f_in, f_out, gemm_dtype);
-  if (order != PGCN_ORDER_TRANSFORM || !p || f_in <= 0 || f_out <= 0) return 0;
+  if (order != PGCN_ORDER_TRANSFORM || !p || f_in <= 0 || f_out <= 0 || gemm_dtype == PGCN_MXFP4) return 0;
   const size_t w = fwd_ws_tf(p, f_in, f_out, gemm_dtype);
   const size_t b = bwd_ws_tf(p, f_in, f_out, true, gemm_dtype) + m16_bytes(p, f_out, true, gemm_dtype);
   const size_t l = align_up(loss_workspace(p->n_inner), 256);
@@ -181,7 +203,9 @@ extern "C" size_t pgcn_layer_workspace_size(const pgcn_partition *p, int32_t f_i
 extern "C" size_t pgcn_workspace_size(const pgcn_partition *p, int32_t f_in, int32_t f_out, int32_t gemm_dtype) try {
   if (!p || f_in <= 0 || f_out <= 0) return 0;
   size_t w = fwd_ws(p, f_in, f_out, gemm_dtype);
-  size_t b = bwd_ws(p, f_in, f_out, true, gemm_dtype);
+  // the backward of a layer whose forward ran in MXFP4 is one of the other two
+  size_t b = gemm_dtype == PGCN_MXFP4 ? std::max(bwd_ws(p, f_in, f_out, true, PGCN_F32), bwd_ws(p, f_in, f_out, true, PGCN_BF16))
+                                      : bwd_ws(p, f_in, f_out, true, gemm_dtype);
   size_t l = align_up(loss_workspace(p->n_inner), 256);
   size_t m = w > b ? w : b;
   return m > l ? m : l;
@@ -350,6 +374,57 @@ int layer_bwd_transform(const pgcn_partition *p, const pgcn_bwd_args *a, hipStre
 
 }  // namespace
 
+namespace {
+
+// The update H_out = act(A W) with both operands in 4 bits, blocks along f_in; then the sent rows.
+int layer_update_fp4(const pgcn_partition *p, const pgcn_fwd_args *a, void *workspace, hipStream_t s) {
+  const Fp4Update u = fp4_update(p, a->f_in, a->f_out);
+  uint8_t *ws = (uint8_t *)workspace;
+  pgcn_mx_quantize_args q{};
+  q.format = PGCN_MX_FP4;
+  q.dtype = PGCN_F32;
+  q.cols = a->f_in;
+  q.rows = q.src_rows = p->n_inner;
+  q.ld_x = a->ld_in;
+  q.ld_q = u.ld_q;
+  q.ld_s = u.ld_s;
+  q.X = a->A;
+  q.Q = ws + u.q_a;
+  q.S = ws + u.s_a;
+  int rc = launch_mx_quantize(q, s);
+  if (rc) return rc;
+  q.transpose = 1;                     // W [f_in, f_out], compact: its rows need not be aligned
+  q.cols = a->f_out;
+  q.rows = q.src_rows = a->f_in;
+  q.ld_x = a->f_out;
+  q.X = a->W;
+  q.Q = ws + u.q_w;
+  q.S = ws + u.s_w;
+  rc = launch_mx_quantize(q, s);
+  if (rc) return rc;
+  pgcn_mx_matmul_args m{};
+  m.dtype = PGCN_F32;
+  m.relu = a->relu ? 1 : 0;
+  m.m = p->n_inner;
+  m.n = a->f_out;
+  m.k = a->f_in;
+  m.ld_a = m.ld_b = u.ld_q;
+  m.ld_a_scales = m.ld_b_scales = u.ld_s;
+  m.ld_c = a->ld_out;
+  m.A = ws + u.q_a;
+  m.A_scales = ws + u.s_a;
+  m.B = ws + u.q_w;
+  m.B_scales = ws + u.s_w;
+  m.C = a->H_out;
+  m.workspace = ws + u.scratch;
+  m.workspace_bytes = u.scratch_bytes;
+  rc = launch_mx_matmul(m, s);
+  if (rc || !a->send_out) return rc;
+  return launch_pack(p->d_send_idx, p->n_send, p->d_inv_ptr, p->d_inv_k, p->n_inner, a->H_out, a->send_out, a->f_out, a->ld_out, s);
+}
+
+}  // namespace
+
 extern "C" int pgcn_layer_fwd(const pgcn_partition *p, const pgcn_fwd_args *a, hipStream_t s) try {
   int rc = check_part(p, "pgcn_layer_fwd");
   if (rc) return rc;
@@ -358,13 +433,16 @@ extern "C" int pgcn_layer_fwd(const pgcn_partition *p, const pgcn_fwd_args *a, h
   PGCN_REQUIRE(a->f_in >= 1 && a->f_out >= 1, "pgcn_layer_fwd: widths must be >= 1");
   PGCN_REQUIRE(a->f_in <= PGCN_MAX_WIDTH && a->f_out <= PGCN_MAX_WIDTH, "pgcn_layer_fwd: widths above PGCN_MAX_WIDTH");
   PGCN_REQUIRE(aligned16(a->send_out), "pgcn_layer_fwd: send_out must be 16-byte aligned");
-  PGCN_REQUIRE(a->gemm_dtype == PGCN_F32 || a->gemm_dtype == PGCN_BF16, "pgcn_layer_fwd: bad gemm_dtype");
+  PGCN_REQUIRE(a->gemm_dtype == PGCN_F32 || a->gemm_dtype == PGCN_BF16 || a->gemm_dtype == PGCN_MXFP4, "pgcn_layer_fwd: bad gemm_dtype");
   PGCN_REQUIRE(a->ld_in >= a->f_in && a->ld_in % 4 == 0, "pgcn_layer_fwd: ld_in must be >= f_in and a multiple of 4");
   PGCN_REQUIRE(a->ld_out >= a->f_out && a->ld_out % 4 == 0, "pgcn_layer_fwd: ld_out must be >= f_out and a multiple of 4");
   PGCN_REQUIRE(a->order == PGCN_ORDER_AGG || a->order == PGCN_ORDER_TRANSFORM, "pgcn_layer_fwd: bad order");
   PGCN_REQUIRE(a->a_given == 0 || a->a_given == 1, "pgcn_layer_fwd: a_given must be 0 or 1");
   PGCN_REQUIRE(!(a->a_given && a->order == PGCN_ORDER_TRANSFORM),
                "pgcn_layer_fwd: a given aggregate needs the aggregate-first order");
+  PGCN_REQUIRE(a->gemm_dtype != PGCN_MXFP4 || a->order == PGCN_ORDER_AGG, "pgcn_layer_fwd: MXFP4 needs the aggregate-first order");
+  if (a->gemm_dtype == PGCN_MXFP4 && p->n_inner > 0)
+    PGCN_REQUIRE(aligned16(a->H_out) && aligned16(a->W), "pgcn_layer_fwd: MXFP4 needs H_out and W 16-byte aligned");
   if (a->order == PGCN_ORDER_TRANSFORM) return layer_fwd_transform(p, a, s);
   const bool bf16 = a->gemm_dtype == PGCN_BF16;
   if (a->a_given) {                  // only the update: Z = A W from the given fp32 aggregate
@@ -372,9 +450,10 @@ extern "C" int pgcn_layer_fwd(const pgcn_partition *p, const pgcn_fwd_args *a, h
       PGCN_REQUIRE(a->A && a->W && a->H_out, "pgcn_layer_fwd: a_given needs A, W and H_out");
       PGCN_REQUIRE(aligned16(a->A), "pgcn_layer_fwd: A must be 16-byte aligned");
     }
-    const size_t gneed = gemm_nk_workspace(a->f_out, a->f_in, a->gemm_dtype);
+    const size_t gneed = update_ws(p, a->f_in, a->f_out, a->gemm_dtype);
     if (!a->workspace || a->workspace_bytes < gneed) return set_error(PGCN_EWORKSPACE, "pgcn_layer_fwd: workspace too small");
     if (p->n_inner == 0) return PGCN_OK;
+    if (a->gemm_dtype == PGCN_MXFP4) return layer_update_fp4(p, a, a->workspace, s);
     GemmArgs m{};
     m.M = (int32_t)p->n_inner;
     m.N = a->f_out;
@@ -446,6 +525,8 @@ extern "C" int pgcn_layer_fwd(const pgcn_partition *p, const pgcn_fwd_args *a, h
   g.trace_kind = PGCN_TK_AGG_FWD;
   rc = launch_aggregate(g, s);
   if (rc) return rc;
+  if (a->gemm_dtype == PGCN_MXFP4)
+    return layer_update_fp4(p, a, (char *)a->workspace + fwd_agg_bytes(p, a->f_in, a->gemm_dtype), s);
 
   GemmArgs m{};
   m.M = (int32_t)p->n_inner;
@@ -469,7 +550,41 @@ extern "C" int pgcn_layer_fwd(const pgcn_partition *p, const pgcn_fwd_args *a, h
   return exception_status("pgcn_layer_fwd");
 }
 
-extern "C" int pgcn_layer_bwd(const pgcn_partition *p, const pgcn_bwd_args *a, hipStream_t s) try {
+namespace {
+
+// dW = A^T (J ∘ mask) of a layer's backward from 8-bit rows instead of what g names; its other arguments as in g.
+int mx_weight_gradient(const pgcn_mx_rows &x, const GemmArgs &g, hipStream_t s) {
+  pgcn_mx_wgrad_args w{};
+  w.dtype = g.dtype;
+  w.f_in = g.M;
+  w.f_out = g.N;
+  w.rows = g.K;
+  w.ld_q = x.ld_q;
+  w.ld_s = x.ld_s;
+  w.ld_j = g.ldb;
+  w.ld_h = g.ldm;
+  w.Q = x.Q;
+  w.S = x.S;
+  w.J = g.B;
+  w.H = g.Hmask;
+  w.dW = g.C;
+  w.workspace = g.workspace;
+  w.workspace_bytes = g.workspace_bytes;
+  return launch_mx_wgrad(w, s);
+}
+
+int check_mx_rows(const pgcn_mx_rows &x, int64_t rows, int32_t f, const char *fn, const char *name) {
+  const std::string of = std::string(fn) + ": " + name;
+  PGCN_REQUIRE(x.ld_q >= mx_row_bytes(PGCN_MX_INT8, f) && x.ld_q % 16 == 0 && x.ld_q <= (int64_t(1) << 40),
+               of + "'s ld_q must hold a row's blocks and be a multiple of 16");
+  PGCN_REQUIRE(x.ld_s >= mx_blocks(f) && x.ld_s % 4 == 0 && x.ld_s <= (int64_t(1) << 40),
+               of + "'s ld_s must hold a row's blocks and be a multiple of 4");
+  PGCN_REQUIRE(rows == 0 || (x.Q && x.S && aligned16(x.Q) && ((uintptr_t)x.S & 3u) == 0),
+               of + " must have Q (16-byte aligned) and S (4-byte)");
+  return PGCN_OK;
+}
+
+int layer_bwd(const pgcn_partition *p, const pgcn_bwd_args *a, const pgcn_mx_rows *mx, hipStream_t s) {
   int rc = check_part(p, "pgcn_layer_bwd");
   if (rc) return rc;
   PGCN_REQUIRE(p->self_loop, "pgcn_layer_bwd: the GCN layer needs a partition built with self loops");
@@ -480,6 +595,7 @@ extern "C" int pgcn_layer_bwd(const pgcn_partition *p, const pgcn_bwd_args *a, h
   PGCN_REQUIRE(a->ld_in >= a->f_in && a->ld_in % 4 == 0, "pgcn_layer_bwd: ld_in must be >= f_in and a multiple of 4");
   PGCN_REQUIRE(a->ld_out >= a->f_out && a->ld_out % 4 == 0, "pgcn_layer_bwd: ld_out must be >= f_out and a multiple of 4");
   PGCN_REQUIRE(a->order == PGCN_ORDER_AGG || a->order == PGCN_ORDER_TRANSFORM, "pgcn_layer_bwd: bad order");
+  PGCN_REQUIRE(!mx || a->order == PGCN_ORDER_AGG, "pgcn_layer_bwd_mx: aggregate first only");
   if (a->order == PGCN_ORDER_TRANSFORM) return layer_bwd_transform(p, a, s);
   const bool bf16 = a->gemm_dtype == PGCN_BF16;
   const bool input_grad = a->J_in != nullptr || a->J_bd_out != nullptr;
@@ -493,7 +609,8 @@ extern "C" int pgcn_layer_bwd(const pgcn_partition *p, const pgcn_bwd_args *a, h
     PGCN_REQUIRE(a->J_out && a->W, "pgcn_layer_bwd: null J_out or W");
     PGCN_REQUIRE(!a->relu || a->H_out, "pgcn_layer_bwd: relu needs H_out as mask source");
     PGCN_REQUIRE(aligned16(a->J_out) && aligned16(a->H_out), "pgcn_layer_bwd: J_out/H_out must be 16-byte aligned");
-    if (bf16 && !a->A)
+    if (mx) {                        // A and A_bf16 are not read
+    } else if (bf16 && !a->A)
       PGCN_REQUIRE(a->A_bf16 && aligned16(a->A_bf16) && a->ld_in % 8 == 0,
                    "pgcn_layer_bwd: bf16 path needs A_bf16 (16-byte aligned, ld_in % 8 == 0) or A");
     else
@@ -520,11 +637,11 @@ extern "C" int pgcn_layer_bwd(const pgcn_partition *p, const pgcn_bwd_args *a, h
   g.ldc = a->f_out;
   g.workspace = (float *)a->workspace;
   g.workspace_bytes = a->workspace_bytes;
-  uint16_t *M16 = p->n_inner > 0 ? m16_ptr(p, a->workspace, a->f_in, a->f_out, input_grad, a->gemm_dtype) : nullptr;
+  uint16_t *M16 = p->n_inner > 0 && !mx ? m16_ptr(p, a->workspace, a->f_in, a->f_out, input_grad, a->gemm_dtype) : nullptr;
   g.M16 = M16;
   g.ldm16 = ld_m16(a->f_out);
   if (bf16 && !a->A_bf16) g.k_split = p->n_inner;    // fp32 A rounded while staged (every row from A)
-  rc = launch_gemm(Gemm::TN_MASK_SPLITK, g, s);
+  rc = mx ? mx_weight_gradient(*mx, g, s) : launch_gemm(Gemm::TN_MASK_SPLITK, g, s);
   if (rc) return rc;
   if (!input_grad || p->n_inner == 0) return PGCN_OK;
 
@@ -575,8 +692,22 @@ extern "C" int pgcn_layer_bwd(const pgcn_partition *p, const pgcn_bwd_args *a, h
   t.partials = partials;
   t.trace_kind = PGCN_TK_AGG_BWD;
   return launch_aggregate(t, s);
+}
+
+}  // namespace
+
+extern "C" int pgcn_layer_bwd(const pgcn_partition *p, const pgcn_bwd_args *a, hipStream_t s) try {
+  return layer_bwd(p, a, nullptr, s);
 } catch (...) {
   return exception_status("pgcn_layer_bwd");
+}
+
+extern "C" int pgcn_layer_bwd_mx(const pgcn_partition *p, const pgcn_bwd_args *a, const pgcn_mx_rows *A, hipStream_t s) try {
+  PGCN_REQUIRE(p && a && A, "pgcn_layer_bwd_mx: null partition, args or A");
+  const int rc = check_mx_rows(*A, p->n_inner, a->f_in, "pgcn_layer_bwd_mx", "A");
+  return rc ? rc : layer_bwd(p, a, A, s);
+} catch (...) {
+  return exception_status("pgcn_layer_bwd_mx");
 }
 
 // ---------------------------------------------------------------- GraphSAGE ---
@@ -889,7 +1020,10 @@ extern "C" int pgcn_sage_layer_fwd(const pgcn_partition *p, const pgcn_sage_fwd_
   return exception_status("pgcn_sage_layer_fwd");
 }
 
-extern "C" int pgcn_sage_layer_bwd(const pgcn_partition *p, const pgcn_sage_bwd_args *a, hipStream_t s) try {
+namespace {
+
+int sage_layer_bwd(const pgcn_partition *p, const pgcn_sage_bwd_args *a, const pgcn_mx_rows *mx, const pgcn_mx_rows *mx_in,
+                   hipStream_t s) {
   int rc = check_part(p, "pgcn_sage_layer_bwd");
   if (rc) return rc;
   PGCN_REQUIRE(!p->self_loop, "pgcn_sage_layer_bwd: the partition must be built with PGCN_SETUP_NO_SELF_LOOP");
@@ -901,6 +1035,7 @@ extern "C" int pgcn_sage_layer_bwd(const pgcn_partition *p, const pgcn_sage_bwd_
   PGCN_REQUIRE(a->ld_out >= a->f_out && a->ld_out % 4 == 0,
                "pgcn_sage_layer_bwd: ld_out must be >= f_out and a multiple of 4");
   PGCN_REQUIRE(a->order == PGCN_ORDER_AGG || a->order == PGCN_ORDER_TRANSFORM, "pgcn_sage_layer_bwd: bad order");
+  PGCN_REQUIRE(!mx || a->order == PGCN_ORDER_AGG, "pgcn_sage_layer_bwd_mx: aggregate first only");
   if (a->order == PGCN_ORDER_TRANSFORM) return sage_bwd_transform(p, a, s);
   const bool bf16 = a->gemm_dtype == PGCN_BF16;
   const bool input_grad = a->J_in != nullptr || a->J_bd_out != nullptr;
@@ -915,7 +1050,13 @@ extern "C" int pgcn_sage_layer_bwd(const pgcn_partition *p, const pgcn_sage_bwd_
     PGCN_REQUIRE(a->J_out && a->W, "pgcn_sage_layer_bwd: null J_out or W");
     PGCN_REQUIRE(!a->relu || a->H_out, "pgcn_sage_layer_bwd: relu needs H_out as mask source");
     PGCN_REQUIRE(aligned16(a->J_out) && aligned16(a->H_out), "pgcn_sage_layer_bwd: J_out/H_out must be 16-byte aligned");
-    if (bf16)
+    if (mx) {                        // only X_in is read, where it is not held in 8 bits too
+      if (!mx_in && bf16)
+        PGCN_REQUIRE(a->X_in_bf16 && aligned16(a->X_in_bf16) && a->ld_in % 8 == 0,
+                     "pgcn_sage_layer_bwd_mx: bf16 path needs X_in_bf16 (16-byte aligned) and ld_in % 8 == 0");
+      else if (!mx_in)
+        PGCN_REQUIRE(a->X_in && aligned16(a->X_in), "pgcn_sage_layer_bwd_mx: fp32 path needs X_in (16-byte aligned)");
+    } else if (bf16)
       PGCN_REQUIRE(a->A_bf16 && a->X_in_bf16 && aligned16(a->A_bf16) && aligned16(a->X_in_bf16) && a->ld_in % 8 == 0,
                    "pgcn_sage_layer_bwd: bf16 path needs A_bf16 and X_in_bf16 (16-byte aligned) and ld_in % 8 == 0");
     else
@@ -944,16 +1085,16 @@ extern "C" int pgcn_sage_layer_bwd(const pgcn_partition *p, const pgcn_sage_bwd_
   g.ldc = a->f_out;
   g.workspace = (float *)a->workspace;
   g.workspace_bytes = a->workspace_bytes;
-  uint16_t *M16 = p->n_inner > 0 ? m16_ptr(p, a->workspace, a->f_in, a->f_out, input_grad, a->gemm_dtype) : nullptr;
+  uint16_t *M16 = p->n_inner > 0 && !mx ? m16_ptr(p, a->workspace, a->f_in, a->f_out, input_grad, a->gemm_dtype) : nullptr;
   g.M16 = M16;
   g.ldm16 = ld_m16(a->f_out);
-  rc = launch_gemm(Gemm::TN_MASK_SPLITK, g, s);
+  rc = mx ? mx_weight_gradient(*mx, g, s) : launch_gemm(Gemm::TN_MASK_SPLITK, g, s);
   if (rc) return rc;
   g.A = a->X_in;
   g.A16 = a->X_in_bf16;
   g.C = a->dW + half;
   g.M16 = nullptr;
-  rc = launch_gemm(Gemm::TN_MASK_SPLITK, g, s);
+  rc = mx_in ? mx_weight_gradient(*mx_in, g, s) : launch_gemm(Gemm::TN_MASK_SPLITK, g, s);
   if (rc) return rc;
   if (!input_grad || p->n_inner == 0) return PGCN_OK;
 
@@ -1007,8 +1148,24 @@ extern "C" int pgcn_sage_layer_bwd(const pgcn_partition *p, const pgcn_sage_bwd_
   t.trace_kind = PGCN_TK_AGG_BWD;
   t.accum_lo = 1;
   return launch_aggregate(t, s);
+}
+
+}  // namespace
+
+extern "C" int pgcn_sage_layer_bwd(const pgcn_partition *p, const pgcn_sage_bwd_args *a, hipStream_t s) try {
+  return sage_layer_bwd(p, a, nullptr, nullptr, s);
 } catch (...) {
   return exception_status("pgcn_sage_layer_bwd");
+}
+
+extern "C" int pgcn_sage_layer_bwd_mx(const pgcn_partition *p, const pgcn_sage_bwd_args *a, const pgcn_mx_rows *A,
+                                      const pgcn_mx_rows *X_in, hipStream_t s) try {
+  PGCN_REQUIRE(p && a && A, "pgcn_sage_layer_bwd_mx: null partition, args or A");
+  int rc = check_mx_rows(*A, p->n_inner, a->f_in, "pgcn_sage_layer_bwd_mx", "A");
+  if (!rc && X_in) rc = check_mx_rows(*X_in, p->n_inner, a->f_in, "pgcn_sage_layer_bwd_mx", "X_in");
+  return rc ? rc : sage_layer_bwd(p, a, A, X_in, s);
+} catch (...) {
+  return exception_status("pgcn_sage_layer_bwd_mx");
 }
 
 extern "C" int pgcn_dropout(float *out, const float *in, int64_t rows, int32_t cols, int64_t ld, int64_t row0,

@@ -224,14 +224,18 @@ struct Shape {
 // (58,000 x 602 x 256: 76 us and 8 for adding the partial tiles, at two 85 and 6); bf16, which waits for memory, two
 // (58,000 x 602 x 256: 67, at three 65 and 2 more for the partial tiles), and where one tile is all there is, one:
 // half as many partial tiles (306,000 x 128 x 128: 68 + 7, at two 70 + 12).  At least 64 rows to a split; where that
-// leaves compute units idle down to 32, as a workgroup's slabs are a chain.  Partial tiles stay below 64 MB a matrix.
+// leaves compute units idle down to 32, as a workgroup's slabs are a chain.  The partial
+// matrices stay below 64 MB together.
 Shape shape_of(int32_t dtype, int64_t rows, int32_t f_in, int32_t f_out) {
   Shape c;
   c.bn = f_out <= 64 ? 64 : 128;
   c.bm = f_in <= 128 || c.bn == 64 || (f_in + 255) / 256 * 256 > (f_in + 127) / 128 * 128 ? 128 : 256;
   const int64_t tiles = (int64_t)((f_in + c.bm - 1) / c.bm) * ((f_out + c.bn - 1) / c.bn);
   const int64_t slots = c.bm == 256 ? 512 : dtype == PGCN_F32 ? 768 : tiles == 1 && c.bn == 128 ? 256 : 512;
-  const int64_t by_bytes = std::max<int64_t>(1, ((int64_t)64 << 20) / ((int64_t)f_in * f_out * 4));
+  // no more than the fp32 and bf16 forms take, whose scratch a layer's backward has
+  const int64_t tile_bytes = (int64_t)f_in * f_out * 4;
+  const int64_t by_bytes =
+      std::max<int64_t>(1, std::min<int64_t>((int64_t)64 << 20, gemm_workspace(Gemm::TN_MASK_SPLITK, f_in, f_out, (int32_t)rows)) / tile_bytes);
   int64_t s = std::max<int64_t>(1, std::min({slots / tiles, (rows + 63) / 64, by_bytes}));
   if (tiles * s < 256) s = std::max(s, std::min({(rows + 31) / 32, (256 + tiles - 1) / tiles, by_bytes}));
   int64_t e = s;                                          // a multiple of 8 workgroups: see the order of tiles

@@ -49,6 +49,17 @@ Distillation: ``top_logits`` lists the largest logits of every node in the last 
 with the teacher's lists at temperature T = ``distill_temp``; nodes with label
 -1 have no hard term, and nodes without a list no soft one.
 
+In fewer bits (blocks of 32 values with one power of two as scale, ``pgcn_mx_*``):
+
+* ``checkpoint_bits`` = 8 keeps each layer's aggregate for the weight gradient in 8 bits (1.03 bytes a
+  value instead of 4 or 2; GraphSAGE's dropped input too), from one fp32 buffer that the layers share.
+  The forward, the loss and the input gradients are as without it;
+* ``exchange_bits`` = 8 or 4 sends boundary features and gradients in that many bits: rows are quantised
+  as they are packed, travel and wait in the stale buffers as bytes, and are read back, smoothed or not,
+  when they are consumed;
+* ``forward_mx4`` runs the forward updates A W with both operands in 4 bits (GCN, aggregate first); the
+  backward stays in gemm_dtype.
+
 ``cache_layer1`` keeps layer 1's aggregate across iterations (GCN, no
 dropout): its input X never changes, so after the peers' rows have arrived
 once, A_full = P [X_in; X_bd] is fixed, and with feature smoothing the
@@ -101,6 +112,9 @@ class StepOptions:
     distill_temp: float = 1.0        # with set_teacher: temperature and weights of the two terms
     distill_soft: float = 0.5
     distill_hard: float = 0.5
+    checkpoint_bits: int = 0         # 0 | 8: the aggregates kept for the backward in 8 bits
+    exchange_bits: int = 0           # 0 | 8 | 4: boundary rows sent and kept in that many bits
+    forward_mx4: bool = False        # forward updates with operands in 4 bits
 
 
 ACTS = {"none": B.PGCN_ACT_NONE, "relu": B.PGCN_ACT_RELU, "silu": B.PGCN_ACT_SILU, "gelu": B.PGCN_ACT_GELU}
@@ -111,6 +125,31 @@ def layer_order(order: str, f_in: int, f_out: int) -> int:
     assert order in ("agg", "transform", "auto"), order
     tf = order == "transform" or (order == "auto" and f_out < f_in)
     return B.PGCN_ORDER_TRANSFORM if tf else B.PGCN_ORDER_AGG
+
+
+class HeldRows:
+    """Rows in 8 or 4 bits, elements and scales in one buffer (one copy moves both)."""
+
+    def __init__(self, bits: int, rows: int, cols: int, device, pin: bool = False):
+        self.format, self.rows, self.cols = {8: B.PGCN_MX_INT8, 4: B.PGCN_MX_FP4}[bits], rows, cols
+        ld_q, ld_s = B.mx_strides(self.format, cols)
+        self.bytes = torch.zeros(rows * (ld_q + ld_s), dtype=torch.uint8, **(dict(pin_memory=True) if pin else dict(device=device)))
+        self.Q = self.bytes[:rows * ld_q].view(rows, ld_q)
+        self.S = self.bytes[rows * ld_q:].view(rows, ld_s)
+        self.held = (self.Q, self.S)
+
+    def write(self, X, stream, index=None):
+        """The rows of X (index: those rows) are quantised."""
+        dtype = B.PGCN_BF16 if X.dtype == torch.bfloat16 else B.PGCN_F32
+        B.pgcn_mx_quantize(format=self.format, dtype=dtype, rows=self.rows, cols=self.cols, src_rows=X.shape[0],
+                           ld_x=ld_of(self.cols), ld_q=self.Q.stride(0), ld_s=self.S.stride(0), X=X, index=index, Q=self.Q,
+                           S=self.S, stream=stream)
+
+    def read(self, out, stream, gamma=0.0):
+        """out = the rows' values, or their moving average over it."""
+        B.pgcn_mx_dequantize(format=self.format, dtype=B.PGCN_F32, rows=self.rows, cols=self.cols, ld_q=self.Q.stride(0),
+                             ld_s=self.S.stride(0), ld_out=ld_of(self.cols), gamma=gamma, Q=self.Q, S=self.S, out=out,
+                             stream=stream)
 
 
 class PartitionTrainer:
@@ -161,10 +200,18 @@ class PartitionTrainer:
         self.adam_v = [torch.zeros_like(w) for w in self.W] if opts.optimizer == "adam" else None
         # dropped layer inputs (dropout, or the bf16 copy of the GraphSAGE self operand)
         self.use_drop = opts.dropout > 0.0 or (self.sage and not f32)
-        self.Xd_in = {l: z(n, wd[l - 1]) for l in range(1, L + 1)} if self.use_drop else {}
-        self.Xd_bd = {l: z(b, wd[l - 1]) for l in range(1, L + 1)} if self.use_drop else {}
-        self.Xd_16 = {l: z(n, wd[l - 1], torch.bfloat16) for l in range(1, L + 1)} \
-            if (self.sage and not f32) else {}
+        self.ckpt = opts.checkpoint_bits == 8
+        # checkpoints: one buffer that every layer takes in turn, else one a layer
+        wide = ld_of(max(wd[:-1]))
+        def each(rows, dt=torch.float32):
+            if not self.ckpt:
+                return {l: z(rows, wd[l - 1], dt) for l in range(1, L + 1)}
+            t = torch.zeros(rows * wide, dtype=dt, device=self.dev)
+            return {l: t[:rows * ld_of(wd[l - 1])].view(rows, ld_of(wd[l - 1])) for l in range(1, L + 1)}
+
+        self.Xd_in = each(n) if self.use_drop else {}
+        self.Xd_bd = each(b) if self.use_drop else {}
+        self.Xd_16 = each(n, torch.bfloat16) if (self.sage and not f32) else {}
         self.G_peer = [None] * L
         self.order = {l: layer_order(opts.order, wd[l - 1], wd[l]) for l in range(1, L + 1)}
         self.cache1 = opts.cache_layer1
@@ -173,8 +220,19 @@ class PartitionTrainer:
             self.order[1] = B.PGCN_ORDER_AGG
         # activations, indexed by layer 1..L (a transform-first layer keeps no aggregate)
         agg = {l: self.order[l] == B.PGCN_ORDER_AGG for l in range(1, L + 1)}
-        self.A = {l: (z(n, wd[l - 1]) if f32 and agg[l] else None) for l in range(1, L + 1)}
-        self.A16 = {l: (None if f32 or not agg[l] else z(n, wd[l - 1], torch.bfloat16)) for l in range(1, L + 1)}
+        assert opts.checkpoint_bits in (0, 8) and opts.exchange_bits in (0, 4, 8), (opts.checkpoint_bits, opts.exchange_bits)
+        self.fwd_dtype = B.PGCN_MXFP4 if opts.forward_mx4 else self.dtype
+        if self.ckpt or opts.forward_mx4:
+            assert all(agg.values()), "checkpoints in 8 bits and forward updates in 4 need aggregate-first layers"
+        assert not (self.cache1 and (self.ckpt or opts.exchange_bits)), "the cached layer 1 keeps and receives fp32 rows"
+        assert not (opts.forward_mx4 and self.sage), "forward updates in 4 bits are the GCN layer's"
+        in32 = f32 or (not self.sage and (self.ckpt or opts.forward_mx4))     # the forward leaves A in fp32
+        A = each(n, torch.float32 if in32 else torch.bfloat16)
+        self.A = {l: A[l] if in32 and agg[l] else None for l in range(1, L + 1)}
+        self.A16 = {l: A[l] if not in32 and agg[l] else None for l in range(1, L + 1)}
+        self.A_mx = {l: HeldRows(8, n, wd[l - 1], self.dev) for l in range(1, L + 1)} if self.ckpt else {}
+        drops = self.ckpt and self.sage and self.use_drop
+        self.X_mx = {l: HeldRows(8, n, wd[l - 1], self.dev) for l in range(1, L + 1)} if drops else {}
         if self.cache1:   # fp32 aggregates of layer 1 on both paths: the running one and A_full
             self.A[1], self.A16[1] = z(n, wd[0]), None
             self.A1_full = z(n, wd[0])
@@ -201,17 +259,24 @@ class PartitionTrainer:
                                               for _ in range(2))
                 self.norm_m[l], self.norm_v[l] = (one(f, 0.0), one(f, 0.0)), (one(f, 0.0), one(f, 0.0))
                 self.G_peer_norm[l] = (None, None)
-        self.fuse_pack = opts.fuse_pack and not self.norm
+        self.bits = opts.exchange_bits
+        self.fuse_pack = opts.fuse_pack and not self.norm and not self.bits
         self.teacher = None
         self.J_top = z(n, wd[L])
         self.J_in = {l: z(n, wd[l - 1]) for l in range(2, L + 1)}
         self.J_bd_out = {l: z(b, wd[l - 1]) for l in range(2, L + 1)}
-        # stale feature buffers (layer l reads boundary rows of H^(l-1)), gradient buffers for l >= 2
-        self.feat = {l: [z(b, wd[l - 1]), z(b, wd[l - 1])] for l in range(1, L + 1)}
+        # stale feature buffers (layer l reads boundary rows of H^(l-1)), gradient buffers for l >= 2; messages in
+        # fewer bits are kept as they arrived
+        message = (lambda r, f: HeldRows(self.bits, r, f, self.dev)) if self.bits else z
+        self.feat = {l: [message(b, wd[l - 1]), message(b, wd[l - 1])] for l in range(1, L + 1)}
         self.ema_f = {l: z(b, wd[l - 1]) for l in range(1, L + 1)}
-        self.send_f = {l: z(s, wd[l - 1]) for l in range(1, L + 1)}
-        self.grad = {l: [z(s, wd[l - 1]), z(s, wd[l - 1])] for l in range(2, L + 1)}
+        self.send_f = {l: message(s, wd[l - 1]) for l in range(1, L + 1)}
+        self.grad = {l: [message(s, wd[l - 1]), message(s, wd[l - 1])] for l in range(2, L + 1)}
         self.ema_g = {l: z(s, wd[l - 1]) for l in range(2, L + 1)}
+        self.send_g = {}
+        if self.bits:
+            self.send_rows = torch.from_numpy(self.send_idx.astype(np.int32)).to(self.dev)
+            self.send_g = {l: message(b, wd[l - 1]) for l in range(2, L + 1)}
         # emulated peers: what the other partitions send each iteration
         g = torch.Generator(device="cpu").manual_seed(remote_seed)
         if opts.remote == "host":          # pinned host memory: refills cross the host link (CPU-staged exchange)
@@ -225,15 +290,21 @@ class PartitionTrainer:
         for l in range(2, L + 1):
             self.remote_g[l][:, : wd[l - 1]] = (1e-3 * torch.randn((s, wd[l - 1]), generator=g)).to(
                 self.remote_g[l].device)
-        self.refill_bytes = sum(t.numel() * 4 for t in self.remote_f.values()) + \
-            sum(t.numel() * 4 for t in self.remote_g.values())
+        self.remote_fq, self.remote_gq = {}, {}
+        if self.bits:
+            pin = opts.remote == "host"
+            self.remote_fq = {l: HeldRows(self.bits, b, wd[l - 1], self.dev, pin) for l in self.remote_f}
+            self.remote_gq = {l: HeldRows(self.bits, s, wd[l - 1], self.dev, pin) for l in self.remote_g}
+            self.quantize_remote()
+        sources = (*self.remote_fq.values(), *self.remote_gq.values()) if self.bits else (*self.remote_f.values(), *self.remote_g.values())
+        self.refill_bytes = sum(self._data(t).numel() * self._data(t).element_size() for t in sources)
         self.X_used = {}                  # layer input the forward used (the GraphSAGE self operand)
         self.X_bd_used = {}               # boundary rows the forward used (transform-first backward)
         self.cur = 0                      # index of the buffer read in this iteration
         self.t = 0
         self.loss = torch.zeros(1, dtype=torch.float32, device=self.dev)
-        ws = max(B.pgcn_layer_workspace_size(self.part, wd[l - 1], wd[l], self.dtype, self.order[l])
-                 for l in range(1, L + 1))
+        ws = max(B.pgcn_layer_workspace_size(self.part, wd[l - 1], wd[l], dt, self.order[l])
+                 for l in range(1, L + 1) for dt in {self.dtype, self.fwd_dtype})
         if self.norm:
             ws = max([ws] + [B.pgcn_group_norm_workspace_size(B.PGCN_F32, wd[l], opts.norm_groups, *self.norm_shape)
                              for l in range(1, L)])
@@ -340,6 +411,59 @@ class PartitionTrainer:
                                     top_ids=i, tail_lse=tail, labels=self.labels, J=self.J_top, loss_out=self.loss,
                                     workspace=self.ws, workspace_bytes=self.ws_bytes, stream=st)
 
+    @staticmethod
+    def _data(x):
+        return x.bytes if isinstance(x, HeldRows) else x
+
+    def quantize_remote(self):
+        """Messages in fewer bits: the emulated peers' rows as they send them (after a change of remote_f, remote_g)."""
+        st = torch.cuda.current_stream(self.dev)
+        with torch.cuda.device(self.dev):
+            for held, rows in ((self.remote_fq, self.remote_f), (self.remote_gq, self.remote_g)):
+                for l, x in rows.items():
+                    there = held[l].bytes.is_cuda
+                    h = held[l] if there else HeldRows(self.bits, held[l].rows, held[l].cols, self.dev)
+                    h.write(x.to(self.dev), st)
+                    if not there:
+                        held[l].bytes.copy_(h.bytes)
+            torch.cuda.synchronize(self.dev)
+
+    def _send_features(self, l, H_in, st):
+        """Algorithm 1's send of the layer's input rows: packed, quantised on the way where messages have fewer bits."""
+        f = self.widths[l - 1]
+        if self.bits:
+            self.send_f[l].write(H_in, st, index=self.send_rows)
+        else:
+            B.pgcn_pack_boundary(self.part, B.PGCN_PACK_FEAT, H_in, self.send_f[l], f, ld_of(f), st)
+
+    def _stale_features(self, l, received, st):
+        """The boundary rows that layer l uses: the received ones or their moving average."""
+        o, f = self.opts, self.widths[l - 1]
+        if self.bits:                       # without smoothing they are read to where the average would be
+            received.read(self.ema_f[l], st, o.gamma if o.smooth_f else 0.0)
+            return self.ema_f[l]
+        if not o.smooth_f:
+            return received
+        B.pgcn_smooth_ema(self.ema_f[l], received, self.b, f, ld_of(f), o.gamma, st)
+        return self.ema_f[l]
+
+    def _add_gradients(self, l, received, st):
+        """The received gradients, or their moving average, are added to the rows that were sent."""
+        o, f = self.opts, self.widths[l - 1]
+        if self.bits:
+            received.read(self.ema_g[l], st, o.gamma if o.smooth_g else 0.0)
+            B.pgcn_pack_boundary(self.part, B.PGCN_ACCUM_GRAD, self.ema_g[l], self.J_in[l], f, ld_of(f), st)
+        elif o.smooth_g:      # smoothing of the received rows fused with their accumulation
+            B.pgcn_accum_smoothed(self.part, received, self.ema_g[l], o.gamma, self.J_in[l], f, ld_of(f), st)
+        else:
+            B.pgcn_pack_boundary(self.part, B.PGCN_ACCUM_GRAD, received, self.J_in[l], f, ld_of(f), st)
+
+    def _refill_features(self, l, dst, stream):
+        self._refill(self._data(dst), self._data((self.remote_fq if self.bits else self.remote_f)[l]), stream)
+
+    def _refill_gradients(self, l, dst, stream):
+        self._refill(self._data(dst), self._data((self.remote_gq if self.bits else self.remote_g)[l]), stream)
+
     def _refill(self, dst, src, stream):
         if self.opts.remote == "host":
             flags = B.PGCN_REFILL_FROM_HOST
@@ -357,7 +481,7 @@ class PartitionTrainer:
         average of A_full (smoothing) or A_full itself; iteration 1 aggregates with zero
         boundary rows straight into the running aggregate."""
         o, wd, f = self.opts, self.widths, self.widths[0]
-        common = dict(f_in=f, f_out=wd[1], gemm_dtype=self.dtype, relu=self._relu(1), ld_in=ld_of(f),
+        common = dict(f_in=f, f_out=wd[1], gemm_dtype=self.fwd_dtype, relu=self._relu(1), ld_in=ld_of(f),
                       ld_out=ld_of(wd[1]), W=self.W[0], A_bf16=None, workspace=self.ws,
                       workspace_bytes=self.ws_bytes, stream=st)
         send = self._send_out(1)
@@ -396,7 +520,7 @@ class PartitionTrainer:
             if H_bd is not None:
                 self._dropout(self.Xd_bd[l], H_bd, self.b, l, self.n, None, st)
                 X_bd = self.Xd_bd[l]
-        common = dict(f_in=f, f_out=wd[l], gemm_dtype=self.dtype, relu=self._relu(l), ld_in=ld_of(f),
+        common = dict(f_in=f, f_out=wd[l], gemm_dtype=self.fwd_dtype, relu=self._relu(l), ld_in=ld_of(f),
                       ld_out=ld_of(wd[l]), W=self.W[l - 1], A=self.A[l], A_bf16=self.A16[l], H_out=self._layer_out(l),
                       workspace=self.ws, workspace_bytes=self.ws_bytes, stream=st)
         send = self._send_out(l)
@@ -407,6 +531,10 @@ class PartitionTrainer:
             B.pgcn_layer_fwd(self.part, H_in=X_in, H_bd=X_bd, order=self.order[l], send_out=send, **common)
         self.X_used[l] = X_in
         self.X_bd_used[l] = X_bd
+        if self.ckpt:
+            self.A_mx[l].write(self.A[l] if self.A[l] is not None else self.A16[l], st)
+            if l in self.X_mx:
+                self.X_mx[l].write(X_in, st)
 
     def _backward_layer(self, l, J_out, st):
         """Layer gradients; the input gradient then takes the forward's dropout mask."""
@@ -416,6 +544,10 @@ class PartitionTrainer:
                       ld_out=ld_of(wd[l]), J_out=J_out, H_out=self._layer_out(l), A=A, A_bf16=self.A16[l],
                       W=self.W[l - 1], dW=self.dW[l - 1], J_in=self.J_in.get(l), J_bd_out=self.J_bd_out.get(l),
                       workspace=self.ws, workspace_bytes=self.ws_bytes, stream=st)
+        if self.ckpt:
+            common["A_mx"] = self.A_mx[l].held
+        if self.sage and l in self.X_mx:
+            common["X_in_mx"] = self.X_mx[l].held
         if self.sage:
             B.pgcn_sage_layer_bwd(self.part, X_in=self.X_used[l], X_in_bf16=self.Xd_16.get(l), order=self.order[l],
                                   X_bd=self.X_bd_used.get(l), **common)
@@ -450,7 +582,7 @@ class PartitionTrainer:
                     self._norm_forward(1, st)
                     continue
                 if mode == "serial":
-                    self._refill(self.feat[1][cur], self.remote_f[1], st)
+                    self._refill_features(1, self.feat[1][cur], st)
                 if t > 1 or mode == "serial":
                     if mode == "pipe":
                         st.wait_event(self.ev_feat[1])
@@ -460,26 +592,23 @@ class PartitionTrainer:
                     if mode == "pipe":
                         self.ev_pack[1].record(st)
                         side.wait_event(self.ev_pack[1])
-                        self._refill(self.feat[1][nxt], self.remote_f[1], side)
+                        self._refill_features(1, self.feat[1][nxt], side)
                         self.ev_feat[1].record(side)
                 self._forward_layer1_cached(H_bd, st)
                 self._norm_forward(1, st)
                 continue
             if mode == "serial":
-                self._refill(self.feat[l][cur], self.remote_f[l], st)
+                self._refill_features(l, self.feat[l][cur], st)
             if t > 1 or mode == "serial":
                 if mode == "pipe":
                     st.wait_event(self.ev_feat[l])
-                H_bd = self.feat[l][cur]
-                if o.smooth_f:
-                    B.pgcn_smooth_ema(self.ema_f[l], H_bd, b, f, ld_of(f), o.gamma, st)
-                    H_bd = self.ema_f[l]
+                H_bd = self._stale_features(l, self.feat[l][cur], st)
             if l == 1 or not self.fuse_pack:   # fused: layer l - 1's output kernel wrote these rows
-                B.pgcn_pack_boundary(self.part, B.PGCN_PACK_FEAT, H_in, self.send_f[l], f, ld_of(f), st)
+                self._send_features(l, H_in, st)
             if mode == "pipe":
                 self.ev_pack[l].record(st)
                 side.wait_event(self.ev_pack[l])
-                self._refill(self.feat[l][nxt], self.remote_f[l], side)
+                self._refill_features(l, self.feat[l][nxt], side)
                 self.ev_feat[l].record(side)
             self._forward_layer(l, H_in, H_bd, st)
             self._norm_forward(l, st)
@@ -494,20 +623,18 @@ class PartitionTrainer:
             self._backward_layer(l, self._norm_backward(l, J_out, st), st)
             if l == 1:
                 break
+            if self.bits:                      # the outgoing gradients as they are sent
+                self.send_g[l].write(self.J_bd_out[l], st)
             if mode == "serial":
-                self._refill(self.grad[l][cur], self.remote_g[l], st)
+                self._refill_gradients(l, self.grad[l][cur], st)
             if t > 1 or mode == "serial":
                 if mode == "pipe":
                     st.wait_event(self.ev_grad[l])
-                C = self.grad[l][cur]
-                if o.smooth_g:      # smoothing of the received rows fused with their accumulation
-                    B.pgcn_accum_smoothed(self.part, C, self.ema_g[l], o.gamma, self.J_in[l], f, ld_of(f), st)
-                else:
-                    B.pgcn_pack_boundary(self.part, B.PGCN_ACCUM_GRAD, C, self.J_in[l], f, ld_of(f), st)
+                self._add_gradients(l, self.grad[l][cur], st)
             if mode == "pipe":
                 self.ev_bwd[l].record(st)
                 side.wait_event(self.ev_bwd[l])
-                self._refill(self.grad[l][nxt], self.remote_g[l], side)
+                self._refill_gradients(l, self.grad[l][nxt], side)
                 self.ev_grad[l].record(side)
 
         # ---- AllReduce (identity on one partition, or + the injected peer sum) and the update

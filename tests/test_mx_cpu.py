@@ -100,7 +100,7 @@ def test_strides():
 
 
 def test_structs_and_limits_match_the_header(tmp_path):
-    structs = [B.pgcn_mx_quantize_args, B.pgcn_mx_dequantize_args, B.pgcn_mx_wgrad_args, B.pgcn_mx_matmul_args]
+    structs = [B.pgcn_mx_quantize_args, B.pgcn_mx_dequantize_args, B.pgcn_mx_wgrad_args, B.pgcn_mx_matmul_args, B.pgcn_mx_rows]
     lines = ["#include <stdio.h>", "#include <stddef.h>", '#include "pgcn.h"', "int main(void) {"]
     for cls in structs:
         name = cls.__name__
@@ -122,3 +122,62 @@ def test_structs_and_limits_match_the_header(tmp_path):
     header = open(os.path.join(ROOT, "include", "pgcn.h")).read()
     for name in ("PGCN_MX_BLOCK", "PGCN_MAX_MX_COLS"):
         assert int(re.search(rf"#define {name} (\d+)", header).group(1)) == getattr(B, name)
+
+
+# ---------------------------------------------------------------- in layers --
+
+@pytest.fixture(scope="module")
+def parts():
+    import numpy as np
+    rowptr, col = np.array([0, 2, 4, 5, 6], np.int64), np.array([1, 2, 0, 3, 0, 1], np.int32)
+    owner = np.array([0, 0, 0, 1], np.int32)
+    return [B.pgcn_partition_setup(4, rowptr, col, owner, 2, 0, self_loop=not sage, host_only=True) for sage in (False, True)]
+
+
+LAYER = dict(f_in=70, f_out=30, gemm_dtype=B.PGCN_F32, relu=1, ld_in=72, ld_out=32)
+
+
+def bwd_args(cls, **over):
+    a = cls()
+    for k, v in {**LAYER, "J_out": at(1), "H_out": at(2), "W": at(3), "dW": at(4), "workspace": at(5), "workspace_bytes": STEP, **over}.items():
+        setattr(a, k, v)
+    return a
+
+
+BAD_ROWS = [dict(Q=None), dict(S=None), dict(Q=at(6) + 8), dict(S=at(7) + 2), dict(ld_q=80), dict(ld_q=104), dict(ld_s=2), dict(ld_s=6),
+            dict(ld_q=(1 << 40) + 16)]
+
+
+def rows_in_8_bits(**over):
+    r = {**dict(Q=at(6), S=at(7), ld_q=96, ld_s=4), **over}
+    return B.pgcn_mx_rows(r["Q"], r["S"], r["ld_q"], r["ld_s"])
+
+
+@pytest.mark.parametrize("bad", BAD_ROWS, ids=str)
+def test_layer_backwards_refuse_bad_rows(parts, bad):
+    gcn, sage = parts
+    good, ill = rows_in_8_bits(), rows_in_8_bits(**bad)
+    a, b = bwd_args(B.pgcn_bwd_args), bwd_args(B.pgcn_sage_bwd_args)
+    assert B.lib.pgcn_layer_bwd_mx(gcn.handle, C.byref(a), C.byref(ill), None) == B.PGCN_EINVAL
+    assert "pgcn_layer_bwd_mx" in B.pgcn_last_error()
+    for x in ((ill, None), (ill, good), (good, ill)):
+        assert B.lib.pgcn_sage_layer_bwd_mx(sage.handle, C.byref(b), C.byref(x[0]), None if x[1] is None else C.byref(x[1]), None) == B.PGCN_EINVAL
+        assert "pgcn_sage_layer_bwd_mx" in B.pgcn_last_error()
+
+
+def test_layer_backwards_refuse_null_arguments(parts):
+    gcn, sage = parts
+    good, a, b = rows_in_8_bits(), bwd_args(B.pgcn_bwd_args), bwd_args(B.pgcn_sage_bwd_args)
+    for args in ((None, C.byref(a), C.byref(good)), (gcn.handle, None, C.byref(good)), (gcn.handle, C.byref(a), None),
+                 (gcn.handle, C.byref(a), C.byref(good))):           # the last: a partition without a device
+        assert B.lib.pgcn_layer_bwd_mx(*args, None) == B.PGCN_EINVAL
+    for args in ((None, C.byref(b), C.byref(good)), (sage.handle, None, C.byref(good)), (sage.handle, C.byref(b), None),
+                 (sage.handle, C.byref(b), C.byref(good))):
+        assert B.lib.pgcn_sage_layer_bwd_mx(*args, None, None) == B.PGCN_EINVAL
+
+
+def test_workspaces_of_layers_in_4_bits(parts):
+    gcn, _ = parts
+    size = lambda dt, order: B.pgcn_layer_workspace_size(gcn, 70, 30, dt, order)
+    assert size(B.PGCN_MXFP4, B.PGCN_ORDER_AGG) >= max(size(dt, B.PGCN_ORDER_AGG) for dt in (B.PGCN_F32, B.PGCN_BF16)) - (1 << 20)
+    assert size(B.PGCN_MXFP4, B.PGCN_ORDER_TRANSFORM) == 0
