@@ -45,7 +45,8 @@ def test_write_and_read(fmt, dtype, cols):
 
 @pytest.mark.parametrize("fmt", FMTS)
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
-@pytest.mark.parametrize("rows,cols", [(1, 1), (31, 5), (32, 64), (33, 257), (100, 300), (1000, 17), (65, 1025)])
+@pytest.mark.parametrize("rows,cols", [(1, 1), (31, 5), (32, 64), (33, 257), (100, 300), (1000, 17), (65, 1025), (255, 33), (257, 129),
+                                       (600, 258)])
 def test_write_transposed(fmt, dtype, rows, cols):
     x = rows_of(np.random.default_rng(rows), rows, cols, dtype)
     Q, S = quantize(matrix(x, dtype), cols, fmt, dtype, transpose=True)
@@ -77,6 +78,8 @@ def test_source_views():
     for fmt in FMTS:
         Q, S = quantize(wide, 36, fmt, rows=13)
         check_held(Q, S, x[:13], fmt)
+        Q, S = quantize(wide, 36, fmt, transpose=True)
+        check_held(Q, S, np.ascontiguousarray(x.T), fmt)
 
 
 @pytest.mark.parametrize("fmt", FMTS)
@@ -195,3 +198,39 @@ def test_streams_and_graphs():
         g.replay()
         torch.cuda.synchronize()
         assert torch.equal(out, want) and torch.equal(Q, q)
+
+
+def test_more_rows_than_a_launch_counts_in_32_bits():
+    """2^30 + 70 rows of one element, four threads each; what lies past 2^32 threads, and 2^34 bytes into Q."""
+    rows, n = (1 << 30) + 70, 5
+    x = np.float64([[1.0], [-3.0], [0.25], [0.0], [6.0]])
+    X = matrix(x, pad=0)
+    index = torch.zeros(rows, dtype=torch.int32, device="cuda")
+    index[-140:] = torch.arange(140, device="cuda").remainder(n).to(torch.int32)
+    Q, S = torch.empty(rows, 16, dtype=torch.uint8, device="cuda"), torch.empty(rows, 4, dtype=torch.uint8, device="cuda")
+    Q[-140:], S[-140:] = 0xA5, 0xA5
+    B.pgcn_mx_quantize(format=B.PGCN_MX_FP4, dtype=B.PGCN_F32, rows=rows, cols=1, src_rows=n, ld_x=X.stride(0), ld_q=16, ld_s=4, X=X,
+                       index=index, Q=Q, S=S)
+    torch.cuda.synchronize()
+    code, s = mx.quantize(x, "fp4")
+    at = np.arange(140) % n
+    assert np.array_equal(Q[-140:].cpu().numpy(), mx.to_bytes(code, "fp4")[at]) and np.array_equal(S[-140:, :1].cpu().numpy(), s[at])
+    del index
+    out = torch.full((rows, 4), 77.0, device="cuda")
+    dequantize(Q, S, rows, 1, "fp4", out=out)
+    torch.cuda.synchronize()
+    assert np.array_equal(out[-140:, 0].cpu().numpy(), x[at, 0]) and (out[:, 1:][-140:] == 77).all()
+
+
+def test_reading_more_chunks_than_a_launch_counts_in_32_bits():
+    """Three chunks a row: 2^32 and some threads in all."""
+    rows = ((1 << 32) // 3) + 50
+    Q, S = torch.zeros(rows, 16, dtype=torch.uint8, device="cuda"), torch.full((rows, 4), 127, dtype=torch.uint8, device="cuda")
+    code = np.random.default_rng(3).integers(0, 16, (120, 32))
+    Q[-120:] = torch.from_numpy(mx.to_bytes(code, "fp4")).cuda()
+    out = torch.empty(rows, 24, dtype=torch.bfloat16, device="cuda")
+    out[-120:] = 77.0
+    dequantize(Q, S, rows, 20, "fp4", "bf16", out=out)
+    torch.cuda.synchronize()
+    assert np.array_equal(host(out[-120:], 20), mx.values(code, np.full((120, 1), 127), 20, "fp4"))
+    assert (out[-120:, 20:] == 77).all()
