@@ -9,6 +9,7 @@ import torch
 
 from mx_helpers import U, host, matmul, quantize, matrix, upload
 from oracle import mx
+from paper_2203_10428_amd import binding as B
 
 pytestmark = pytest.mark.gpu
 
@@ -47,6 +48,27 @@ def test_product(m, n, k, dtype):
 def test_many_tiles(m, n, k, dtype):
     """Enough rows and columns for the larger tiles, with ragged edges; an even and an odd number of slabs, part of one."""
     test_product(m, n, k, dtype)
+
+
+@pytest.mark.parametrize("k", [32, 256, 257, 500, 512, 600, 768, 1000, 1024, 1030, 1280, 1500, 1800, 2048, 2100, 2400])
+@pytest.mark.parametrize("m,n", [(70, 3), (1, 90), (16, 16)])
+def test_every_number_of_slabs(m, n, k):
+    """One slab to more than all stages hold, with whole and part last ones; groups for one wave to more than all."""
+    test_product(m, n, k, "f32")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("m,n,k", [(1, 40, 20000), (1, 1, 70000), (9, 130, 9001), (16, 33, 16384), (100, 90, 9000), (17, 5, 40000), (129, 200, 4100),
+                                   (64, 64, 2048)])
+def test_long_rows_in_parts(m, n, k, dtype):
+    """Blocks split among workgroups, the last part shorter; one part fewer than asked for."""
+    assert B.pgcn_mx_matmul_workspace_size(B.PGCN_F32, m, n, k) >= 2 * 4 * m * n
+    test_product(m, n, k, dtype)
+
+
+@pytest.mark.parametrize("m,n,k", [(4100, 4000, 600), (4090, 4200, 1100), (2050, 2100, 600), (2049, 2176, 1200), (16400, 4100, 40)])
+def test_many_tiles_of_more_slabs(m, n, k):
+    test_product(m, n, k, "bf16")
 
 
 @pytest.mark.parametrize("m", [1, 20, 300])
