@@ -64,9 +64,9 @@ __device__ __forceinline__ bf16x8 transposed(const uint16_t *lo, const uint16_t 
 template <int BM, int BN, int kParts, bool kMasked>
 __global__ __launch_bounds__(256, 2) void wgrad(WgradArgs p) {
   constexpr int LA = BM + kPad, LB = BN + kPad;
-  constexpr int CA = BM / 8, CB = BN / 4, RA = 256 / CA, RB = 256 / CB, VA = kSlab / RA, VB = kSlab / RB;
+  constexpr int CA = BM / 8, CB = BN / 4, RB = 256 / CB, VA = (kSlab * CA + 255) / 256, VB = kSlab / RB;
   constexpr int WM = BM / 2, WN = BN / 2, TM = WM / 32, TN = WN / 32;
-  static_assert(VA >= 1 && VB >= 1, "a slab holds an item for every thread");
+  static_assert(kSlab * CA % 64 == 0 && VB >= 1, "whole waves have an item");
   __shared__ __attribute__((aligned(16))) uint16_t As[2][kSlab * LA];
   __shared__ __attribute__((aligned(16))) uint16_t Bs[2][kParts][kSlab * LB];
 
@@ -77,22 +77,33 @@ __global__ __launch_bounds__(256, 2) void wgrad(WgradArgs p) {
   const int m0 = (int)(tile / p.tiles_n) * BM, n0 = (int)(tile % p.tiles_n) * BN;
   const int64_t begin = split * p.chunk, end = min(p.rows, begin + p.chunk);
 
-  // staging: row ra + RA i and eight features of v, row rb + RB i and four of J
-  const int ca = 8 * (t % CA), ra = t / CA, cb = 4 * (t % CB), rb = t / CB;
+  // staging: items t + 256 i of v, a row's eight features, the last for some waves alone; row rb + RB i and four of J
+  const int cb = 4 * (t % CB), rb = t / CB;
+  int ca[VA], ra[VA];
+#pragma unroll
+  for (int i = 0; i < VA; ++i) ca[i] = 8 * ((t + 256 * i) % CA), ra[i] = (t + 256 * i) / CA;
+  auto has = [&](int i) __attribute__((always_inline)) { return (i + 1) * 256 <= kSlab * CA || 64 * wave + 256 * i < kSlab * CA; };
   struct Regs {
     op_u32x2 q[VA];
     uint32_t s[VA];
     op_f32x4 j[VB], h[VB];
   };
   // Columns past the matrix read its first ones: their products are not stored.
-  const int64_t col_q = m0 + ca < p.f_in ? m0 + ca : 0, col_j = n0 + cb < p.f_out ? n0 + cb : 0;
-  const int64_t off_q = ra * p.ld_q + col_q, off_s = ra * p.ld_s + col_q / 32, off_j = rb * p.ld_j + col_j, off_h = rb * p.ld_h + col_j;
+  const int64_t col_j = n0 + cb < p.f_out ? n0 + cb : 0, off_j = rb * p.ld_j + col_j, off_h = rb * p.ld_h + col_j;
+  int64_t off_q[VA], off_s[VA];
+#pragma unroll
+  for (int i = 0; i < VA; ++i) {
+    const int64_t col = m0 + ca[i] < p.f_in ? m0 + ca[i] : 0;
+    off_q[i] = ra[i] * p.ld_q + col;
+    off_s[i] = ra[i] * p.ld_s + col / 32;
+  }
   auto load = [&](Regs &R, int64_t k) __attribute__((always_inline)) {
 #pragma unroll
-    for (int i = 0; i < VA; ++i) {
-      R.q[i] = *reinterpret_cast<const op_u32x2 *>(p.Q + (k + RA * i) * p.ld_q + off_q);
-      R.s[i] = (p.S + (k + RA * i) * p.ld_s)[off_s];
-    }
+    for (int i = 0; i < VA; ++i)
+      if (has(i)) {
+        R.q[i] = *reinterpret_cast<const op_u32x2 *>(p.Q + k * p.ld_q + off_q[i]);
+        R.s[i] = (p.S + k * p.ld_s)[off_s[i]];
+      }
 #pragma unroll
     for (int i = 0; i < VB; ++i) {
       R.j[i] = *reinterpret_cast<const op_f32x4 *>(p.J + (k + RB * i) * p.ld_j + off_j);
@@ -102,10 +113,9 @@ __global__ __launch_bounds__(256, 2) void wgrad(WgradArgs p) {
   auto load_last = [&](Regs &R, int64_t k) __attribute__((always_inline)) {      // zeros for rows past the last one
 #pragma unroll
     for (int i = 0; i < VA; ++i) {
-      const int64_t row = k + ra + RA * i;
-      const bool in = row < p.rows;
-      R.q[i] = in ? *reinterpret_cast<const op_u32x2 *>(p.Q + row * p.ld_q + col_q) : op_u32x2{0u, 0u};
-      R.s[i] = in ? p.S[row * p.ld_s + col_q / 32] : 0u;
+      const bool in = has(i) && k + ra[i] < p.rows;
+      R.q[i] = in ? *reinterpret_cast<const op_u32x2 *>(p.Q + k * p.ld_q + off_q[i]) : op_u32x2{0u, 0u};
+      R.s[i] = in ? (p.S + k * p.ld_s)[off_s[i]] : 0u;
     }
 #pragma unroll
     for (int i = 0; i < VB; ++i) {
@@ -118,7 +128,7 @@ __global__ __launch_bounds__(256, 2) void wgrad(WgradArgs p) {
   auto store = [&](const Regs &R, int buf) __attribute__((always_inline)) {
 #pragma unroll
     for (int i = 0; i < VA; ++i)
-      *reinterpret_cast<op_u32x4 *>(&As[buf][(ra + RA * i) * LA + ca]) = bf16_of(R.q[i], int8_step(R.s[i]));
+      if (has(i)) *reinterpret_cast<op_u32x4 *>(&As[buf][ra[i] * LA + ca[i]]) = bf16_of(R.q[i], int8_step(R.s[i]));
 #pragma unroll
     for (int i = 0; i < VB; ++i) {
       float x[4];
@@ -217,10 +227,10 @@ struct Shape {
   int64_t chunk;
 };
 
-// Tile: 256 features of v where that fills up no more than 128 do, since a slab's J is split into its parts by
-// every tile row (239,000 x 512 x 512 fp32: 335 us with 256, 353 with 128; 58,000 x 602 x 256, which 256 would
-// fill up to 768: 93 against 76).
-// Splits: as many workgroups as are resident at once.  256-row tiles two to a compute unit, 128-row tiles three
+// Tile: 256 or 192 features of v where that fills up no more than 128 do, since a slab's J is split into its parts by
+// every tile row (fp32: 239,000 x 512 x 512 347 us with 256, 455 with 128; 239,000 x 300 x 512 284 with 192, 348 with 128;
+// 58,000 x 602 x 256, which 256 would fill up to 768: 81 against 76).
+// Splits: as many workgroups as are resident at once.  Tiles of more than 128 two to a compute unit, 128-row tiles three
 // (58,000 x 602 x 256: 76 us and 8 for adding the partial tiles, at two 85 and 6); bf16, which waits for memory, two
 // (58,000 x 602 x 256: 67, at three 65 and 2 more for the partial tiles), and where one tile is all there is, one:
 // half as many partial tiles (306,000 x 128 x 128: 68 + 7, at two 70 + 12).  At least 64 rows to a split; where that
@@ -229,9 +239,10 @@ struct Shape {
 Shape shape_of(int32_t dtype, int64_t rows, int32_t f_in, int32_t f_out) {
   Shape c;
   c.bn = f_out <= 64 ? 64 : 128;
-  c.bm = f_in <= 128 || c.bn == 64 || (f_in + 255) / 256 * 256 > (f_in + 127) / 128 * 128 ? 128 : 256;
+  const auto filled = [&](int bm) { return (f_in + bm - 1) / bm * bm; };
+  c.bm = f_in <= 128 || c.bn == 64 ? 128 : filled(256) <= filled(128) ? 256 : filled(192) <= filled(128) ? 192 : 128;
   const int64_t tiles = (int64_t)((f_in + c.bm - 1) / c.bm) * ((f_out + c.bn - 1) / c.bn);
-  const int64_t slots = c.bm == 256 ? 512 : dtype == PGCN_F32 ? 768 : tiles == 1 && c.bn == 128 ? 256 : 512;
+  const int64_t slots = c.bm > 128 ? 512 : dtype == PGCN_F32 ? 768 : tiles == 1 && c.bn == 128 ? 256 : 512;
   // no more than the fp32 and bf16 forms take, whose scratch a layer's backward has
   const int64_t tile_bytes = (int64_t)f_in * f_out * 4;
   const int64_t by_bytes =
@@ -275,6 +286,7 @@ int launch_mx_wgrad(const pgcn_mx_wgrad_args &x, hipStream_t s) {
     const bool bf16 = x.dtype == PGCN_BF16;
     if (c.bn == 64) launch_tile<128, 64>(a, c.splits, bf16, s);
     else if (c.bm == 128) launch_tile<128, 128>(a, c.splits, bf16, s);
+    else if (c.bm == 192) launch_tile<192, 128>(a, c.splits, bf16, s);
     else launch_tile<256, 128>(a, c.splits, bf16, s);
     PGCN_HIP(hipGetLastError());
   }

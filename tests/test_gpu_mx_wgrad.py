@@ -37,7 +37,8 @@ def check(dW, code, s, J, H, f_in, f_out, dtype):
 
 
 SHAPES = [(1, 1, 1), (1, 33, 7), (2, 64, 64), (15, 5, 100), (16, 32, 16), (17, 129, 65), (33, 96, 128), (100, 602, 41), (257, 256, 256),
-          (1000, 32, 16), (1500, 100, 130), (4099, 300, 47), (3000, 513, 260), (700, 1025, 8), (64, 40, 1500), (20000, 128, 128)]
+          (1000, 32, 16), (1500, 100, 130), (4099, 300, 47), (3000, 513, 260), (700, 1025, 8), (64, 40, 1500), (20000, 128, 128),
+          (2000, 300, 130), (999, 540, 200), (50, 384, 100), (35, 257, 65)]
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
