@@ -51,14 +51,14 @@ with the teacher's lists at temperature T = ``distill_temp``; nodes with label
 
 In fewer bits (blocks of 32 values with one power of two as scale, ``pgcn_mx_*``):
 
-* ``checkpoint_bits`` = 8 keeps each layer's aggregate for the weight gradient in 8 bits (1.03 bytes a
-  value instead of 4 or 2; GraphSAGE's dropped input too), from one fp32 buffer that the layers share.
-  The forward, the loss and the input gradients are as without it;
+* ``checkpoint_bits`` = 8 keeps the aggregate of every aggregate-first layer for the weight gradient in
+  8 bits (1.03 bytes a value instead of 4 or 2; GraphSAGE's dropped input too), from one buffer that
+  these layers share.  The forward, the loss and the input gradients are as without it;
 * ``exchange_bits`` = 8 or 4 sends boundary features and gradients in that many bits: rows are quantised
   as they are packed, travel and wait in the stale buffers as bytes, and are read back, smoothed or not,
   when they are consumed;
-* ``forward_mx4`` runs the forward updates A W with both operands in 4 bits (GCN, aggregate first); the
-  backward stays in gemm_dtype.
+* ``forward_mx4`` runs the forward updates A W of GCN's aggregate-first layers with both operands in
+  4 bits; the backward stays in gemm_dtype.
 
 ``cache_layer1`` keeps layer 1's aggregate across iterations (GCN, no
 dropout): its input X never changes, so after the peers' rows have arrived
@@ -198,41 +198,40 @@ class PartitionTrainer:
         self.dW = [torch.zeros_like(w) for w in self.W]
         self.adam_m = [torch.zeros_like(w) for w in self.W] if opts.optimizer == "adam" else None
         self.adam_v = [torch.zeros_like(w) for w in self.W] if opts.optimizer == "adam" else None
-        # dropped layer inputs (dropout, or the bf16 copy of the GraphSAGE self operand)
-        self.use_drop = opts.dropout > 0.0 or (self.sage and not f32)
-        self.ckpt = opts.checkpoint_bits == 8
-        # checkpoints: one buffer that every layer takes in turn, else one a layer
-        wide = ld_of(max(wd[:-1]))
-        def each(rows, dt=torch.float32):
-            if not self.ckpt:
-                return {l: z(rows, wd[l - 1], dt) for l in range(1, L + 1)}
-            t = torch.zeros(rows * wide, dtype=dt, device=self.dev)
-            return {l: t[:rows * ld_of(wd[l - 1])].view(rows, ld_of(wd[l - 1])) for l in range(1, L + 1)}
-
-        self.Xd_in = each(n) if self.use_drop else {}
-        self.Xd_bd = each(b) if self.use_drop else {}
-        self.Xd_16 = each(n, torch.bfloat16) if (self.sage and not f32) else {}
         self.G_peer = [None] * L
         self.order = {l: layer_order(opts.order, wd[l - 1], wd[l]) for l in range(1, L + 1)}
         self.cache1 = opts.cache_layer1
         if self.cache1:
             assert not self.sage and opts.dropout == 0.0, "layer-1 caching needs a constant layer input"
             self.order[1] = B.PGCN_ORDER_AGG
-        # activations, indexed by layer 1..L (a transform-first layer keeps no aggregate)
         agg = {l: self.order[l] == B.PGCN_ORDER_AGG for l in range(1, L + 1)}
         assert opts.checkpoint_bits in (0, 8) and opts.exchange_bits in (0, 4, 8), (opts.checkpoint_bits, opts.exchange_bits)
-        self.fwd_dtype = B.PGCN_MXFP4 if opts.forward_mx4 else self.dtype
-        if self.ckpt or opts.forward_mx4:
-            assert all(agg.values()), "checkpoints in 8 bits and forward updates in 4 need aggregate-first layers"
+        # layers whose aggregate (and dropped input) is kept in 8 bits, and whose update runs in 4
+        self.ckpt = {l for l in agg if agg[l] and opts.checkpoint_bits == 8}
+        self.mx4 = {l for l in agg if agg[l] and opts.forward_mx4}
+        assert (self.ckpt or not opts.checkpoint_bits) and (self.mx4 or not opts.forward_mx4), "no layer aggregates first"
         assert not (self.cache1 and (self.ckpt or opts.exchange_bits)), "the cached layer 1 keeps and receives fp32 rows"
-        assert not (opts.forward_mx4 and self.sage), "forward updates in 4 bits are the GCN layer's"
-        in32 = f32 or (not self.sage and (self.ckpt or opts.forward_mx4))     # the forward leaves A in fp32
-        A = each(n, torch.float32 if in32 else torch.bfloat16)
-        self.A = {l: A[l] if in32 and agg[l] else None for l in range(1, L + 1)}
-        self.A16 = {l: A[l] if not in32 and agg[l] else None for l in range(1, L + 1)}
-        self.A_mx = {l: HeldRows(8, n, wd[l - 1], self.dev) for l in range(1, L + 1)} if self.ckpt else {}
-        drops = self.ckpt and self.sage and self.use_drop
-        self.X_mx = {l: HeldRows(8, n, wd[l - 1], self.dev) for l in range(1, L + 1)} if drops else {}
+        assert not (self.mx4 and self.sage), "forward updates in 4 bits are the GCN layer's"
+        wide = max([ld_of(wd[l - 1]) for l in self.ckpt], default=0)
+
+        def each(rows, dt=torch.float32, layers=range(1, L + 1)):
+            """Buffers of the layers' input widths: one that the layers in 8 bits take in turn, one for each other."""
+            t = torch.zeros(rows * wide if self.ckpt & set(layers) else 0, dtype=dt, device=self.dev)
+            return {l: t[:rows * ld_of(wd[l - 1])].view(rows, ld_of(wd[l - 1])) if l in self.ckpt else z(rows, wd[l - 1], dt)
+                    for l in layers}
+
+        # dropped layer inputs (dropout, or the bf16 copy of the GraphSAGE self operand)
+        self.use_drop = opts.dropout > 0.0 or (self.sage and not f32)
+        self.Xd_in = each(n) if self.use_drop else {}
+        self.Xd_bd = each(b) if self.use_drop else {}
+        self.Xd_16 = each(n, torch.bfloat16) if (self.sage and not f32) else {}
+        # activations, indexed by layer 1..L (a transform-first layer keeps no aggregate)
+        in32 = [l for l in agg if agg[l] and (f32 or (not self.sage and l in self.ckpt | self.mx4))]   # the forward leaves A in fp32
+        in16 = [l for l in agg if agg[l] and l not in in32]
+        self.A = {**dict.fromkeys(agg), **each(n, layers=in32)}
+        self.A16 = {**dict.fromkeys(agg), **each(n, torch.bfloat16, in16)}
+        self.A_mx = {l: HeldRows(8, n, wd[l - 1], self.dev) for l in sorted(self.ckpt)}
+        self.X_mx = {l: HeldRows(8, n, wd[l - 1], self.dev) for l in sorted(self.ckpt) if self.sage and self.use_drop}
         if self.cache1:   # fp32 aggregates of layer 1 on both paths: the running one and A_full
             self.A[1], self.A16[1] = z(n, wd[0]), None
             self.A1_full = z(n, wd[0])
@@ -304,7 +303,7 @@ class PartitionTrainer:
         self.t = 0
         self.loss = torch.zeros(1, dtype=torch.float32, device=self.dev)
         ws = max(B.pgcn_layer_workspace_size(self.part, wd[l - 1], wd[l], dt, self.order[l])
-                 for l in range(1, L + 1) for dt in {self.dtype, self.fwd_dtype})
+                 for l in range(1, L + 1) for dt in {self.dtype, self._fwd_dtype(l)})
         if self.norm:
             ws = max([ws] + [B.pgcn_group_norm_workspace_size(B.PGCN_F32, wd[l], opts.norm_groups, *self.norm_shape)
                              for l in range(1, L)])
@@ -321,6 +320,9 @@ class PartitionTrainer:
     # ------------------------------------------------------------------
     def _relu(self, l):
         return (l < self.L and not self.norm) or self.opts.relu_last
+
+    def _fwd_dtype(self, l):
+        return B.PGCN_MXFP4 if l in self.mx4 else self.dtype
 
     def _layer_out(self, l):
         """Where layer l's product goes: H, or Z where a group norm follows."""
@@ -481,7 +483,7 @@ class PartitionTrainer:
         average of A_full (smoothing) or A_full itself; iteration 1 aggregates with zero
         boundary rows straight into the running aggregate."""
         o, wd, f = self.opts, self.widths, self.widths[0]
-        common = dict(f_in=f, f_out=wd[1], gemm_dtype=self.fwd_dtype, relu=self._relu(1), ld_in=ld_of(f),
+        common = dict(f_in=f, f_out=wd[1], gemm_dtype=self._fwd_dtype(1), relu=self._relu(1), ld_in=ld_of(f),
                       ld_out=ld_of(wd[1]), W=self.W[0], A_bf16=None, workspace=self.ws,
                       workspace_bytes=self.ws_bytes, stream=st)
         send = self._send_out(1)
@@ -520,7 +522,7 @@ class PartitionTrainer:
             if H_bd is not None:
                 self._dropout(self.Xd_bd[l], H_bd, self.b, l, self.n, None, st)
                 X_bd = self.Xd_bd[l]
-        common = dict(f_in=f, f_out=wd[l], gemm_dtype=self.fwd_dtype, relu=self._relu(l), ld_in=ld_of(f),
+        common = dict(f_in=f, f_out=wd[l], gemm_dtype=self._fwd_dtype(l), relu=self._relu(l), ld_in=ld_of(f),
                       ld_out=ld_of(wd[l]), W=self.W[l - 1], A=self.A[l], A_bf16=self.A16[l], H_out=self._layer_out(l),
                       workspace=self.ws, workspace_bytes=self.ws_bytes, stream=st)
         send = self._send_out(l)
@@ -531,7 +533,7 @@ class PartitionTrainer:
             B.pgcn_layer_fwd(self.part, H_in=X_in, H_bd=X_bd, order=self.order[l], send_out=send, **common)
         self.X_used[l] = X_in
         self.X_bd_used[l] = X_bd
-        if self.ckpt:
+        if l in self.ckpt:
             self.A_mx[l].write(self.A[l] if self.A[l] is not None else self.A16[l], st)
             if l in self.X_mx:
                 self.X_mx[l].write(X_in, st)
@@ -544,7 +546,7 @@ class PartitionTrainer:
                       ld_out=ld_of(wd[l]), J_out=J_out, H_out=self._layer_out(l), A=A, A_bf16=self.A16[l],
                       W=self.W[l - 1], dW=self.dW[l - 1], J_in=self.J_in.get(l), J_bd_out=self.J_bd_out.get(l),
                       workspace=self.ws, workspace_bytes=self.ws_bytes, stream=st)
-        if self.ckpt:
+        if l in self.ckpt:
             common["A_mx"] = self.A_mx[l].held
         if self.sage and l in self.X_mx:
             common["X_in_mx"] = self.X_mx[l].held

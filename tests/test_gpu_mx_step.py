@@ -82,6 +82,31 @@ def test_checkpoints_in_8_bits(dt, model, dropout):
                 assert torch.equal(tr.dW[l - 1][f:], plain.dW[l - 1][f:])
 
 
+@pytest.mark.parametrize("dropout", [0.0, 0.3])
+def test_only_layers_that_aggregate_first_are_held(dropout):
+    """One layer of three narrows and transforms first: it keeps what it keeps without the options."""
+    w = configs.TINY
+    widths = (32, 48, 16, 8)                                  # auto: the first aggregates first
+    g = configs.make_graph(w)
+    d = configs.make_dense(w, g.n)
+    rng = np.random.default_rng(2)
+    W = [rng.uniform(-0.2, 0.2, (a, b)).astype(np.float32) for a, b in zip(widths, widths[1:])]
+    make = lambda **kw: PartitionTrainer(g, d.X, d.labels, W, widths, w.loss, w.loss_scale, "f32",
+                                         StepOptions(gamma=w.gamma, eta=w.eta, copy_mode="pipe", order="auto", dropout=dropout, seed=5, **kw))
+    plain, tr, both = make(), make(checkpoint_bits=8), make(checkpoint_bits=8, forward_mx4=True)
+    assert set(tr.A_mx) == tr.ckpt == both.mx4 == {1}
+    for t in range(3):
+        for a, c, b in zip(tr.W, both.W, plain.W):
+            a.copy_(b)
+            c.copy_(b)
+        step(plain, tr, both)
+        assert torch.equal(tr.loss, plain.loss) and np.isfinite(both.loss.item())
+        for l in (2, 3):
+            assert torch.equal(tr.dW[l - 1], plain.dW[l - 1]) and torch.equal(tr.J_in[l], plain.J_in[l])
+        v = mx.values(*mx.quantize(get(plain.A[1], 32), "int8"), 32, "int8")
+        check_dw(tr.dW[0], v, get(plain.J_in[2], 48), get(plain.H[1], 48), "f32", True)
+
+
 def test_checkpoints_take_less_memory():
     """The aggregates that stay between forward and backward: 8 bits and a scale to 32 elements, against 32 bits."""
     w, tr = trainer(checkpoint_bits=8)
@@ -136,15 +161,16 @@ def test_boundary_rows_in_fewer_bits(bits, mode, remote, smooth):
 
 
 @pytest.mark.parametrize("dt", ["f32", "bf16"])
-def test_forward_updates_in_4_bits(dt):
-    w, tr = trainer(dt=dt, forward_mx4=True)
+@pytest.mark.parametrize("cache", [False, True])
+def test_forward_updates_in_4_bits(dt, cache):
+    w, tr = trainer(dt=dt, forward_mx4=True, cache_layer1=cache)
     for t in range(3):
         W = [x.cpu().numpy().astype(np.float64) for x in tr.W]
         step(tr)
         assert np.isfinite(tr.loss.item())
         for l in range(1, w.layers + 1):
             f = w.widths[l - 1]
-            A = get(tr.A[l], f)
+            A = get(tr.A1_used if cache and l == 1 else tr.A[l], f)
             a, b = mx.values(*mx.quantize(A, "fp4"), f, "fp4"), mx.values(*mx.quantize(np.ascontiguousarray(W[l - 1].T), "fp4"), f, "fp4")
             tol = 2 * (f + 64) * U * (np.abs(a) @ np.abs(b).T) + 2.0 ** -120
             assert (np.abs(get(tr.H[l], w.widths[l]) - mx.product(a, b, l < w.layers)) <= tol).all()
@@ -186,7 +212,7 @@ def test_two_trainers_at_once_keep_their_own():
 
 
 @pytest.mark.parametrize("kw", [dict(checkpoint_bits=4), dict(exchange_bits=16), dict(checkpoint_bits=8, order="transform"),
-                                dict(forward_mx4=True, order="transform"), dict(forward_mx4=True, model="sage"),
+                                dict(forward_mx4=True, order="auto"), dict(forward_mx4=True, model="sage"),
                                 dict(checkpoint_bits=8, cache_layer1=True), dict(exchange_bits=8, cache_layer1=True)])
 def test_refused_options(kw):
     with pytest.raises(AssertionError):
