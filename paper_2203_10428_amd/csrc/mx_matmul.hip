@@ -427,6 +427,7 @@ int launch_mx_matmul(const pgcn_mx_matmul_args &x, hipStream_t s) {
   a.m = x.m, a.ld_a = x.ld_a, a.ld_sa = x.ld_a_scales, a.ld_b = x.ld_b, a.ld_sb = x.ld_b_scales, a.ld_c = x.ld_c;
   a.n = x.n, a.n4 = (x.n + 3) / 4 * 4, a.blocks = (int32_t)mx_blocks(x.k), a.relu = x.relu;
   TraceScope ts(PGCN_TK_MX_MATMUL, s);
+  if (c.splits > 1) ts.set_launches(2);
   if (x.dtype == PGCN_BF16) launch<BF16>(a, c, s);
   else launch<F32>(a, c, s);
   PGCN_HIP(hipGetLastError());

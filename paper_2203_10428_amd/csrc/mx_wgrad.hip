@@ -29,9 +29,18 @@ struct WgradArgs {
   int32_t f_in, f_out, tiles_n, tiles;
 };
 
-// Eight INT8 elements as bf16: (u - 128) step, u = q + 128, is exact, so its high half is the value.
+// Eight INT8 elements as bf16: (u - 128) step, u = q + 128, is exact, so its high half is the value.  One product-sum,
+// but for the largest scale, with which 128 step is no float.
 __device__ __forceinline__ op_u32x4 bf16_of(const op_u32x2 &q, float step) {
   op_u32x4 w;
+  if (step > 0x1p120f) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t u = q[i / 2] >> (16 * (i % 2));
+      w[i] = __builtin_amdgcn_perm(__float_as_uint((float)(int8_t)(u >> 8) * step), __float_as_uint((float)(int8_t)u * step), 0x07060302u);
+    }
+    return w;
+  }
   const float off = -128.f * step;
 #pragma unroll
   for (int i = 0; i < 2; ++i) {

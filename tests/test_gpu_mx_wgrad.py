@@ -98,6 +98,25 @@ def test_scales_far_apart(dtype):
     check(wgrad(Q, S, matrix(J), None, 64, 40, 24, dtype), code, s, J, None, 40, 24, dtype)
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("scale", [0, 1, 6, 133, 253, 254])
+def test_every_element_at_the_ends_of_the_scales(dtype, scale):
+    """Elements -128 .. 127 with the smallest and largest scales; J brings the products to where floats are."""
+    rows, f_in, f_out = 40, 256, 8
+    code = np.tile(np.arange(-128, 128), (rows, 1))
+    if scale == 254:
+        code = np.maximum(code, -127)                      # -128 with the largest scale is no float
+    s = np.full((rows, 8), scale)
+    J = np.zeros((rows, f_out))
+    J[np.arange(rows), np.arange(rows) % f_out] = np.ldexp(1.0 + np.arange(rows) / 64.0, -60 if scale > 133 else 60)
+    Q, S = upload(code, s, "int8")
+    dW = wgrad(Q, S, matrix(J), None, rows, f_in, f_out, dtype)
+    if scale >= 6:                                         # below, values are less than 2^-126
+        check(dW, code, s, J, None, f_in, f_out, dtype)
+    torch.cuda.synchronize()
+    assert torch.isfinite(dW).all()
+
+
 def test_the_same_bits_every_time_and_from_a_graph():
     code, s, J, H = inputs(6, 5000, 100, 72, True)
     Q, S = upload(code, s, "int8")
