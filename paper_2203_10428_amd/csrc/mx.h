@@ -114,17 +114,24 @@ struct Bits8<Fp4> {
 };
 
 // n (may be <= 0 or > 8) of eight neighbouring elements from a 16-byte aligned place, zeros for the rest; no
-// vector is read that holds none of them.
+// vector is read that holds none of them.  kOnce: the line is read once and need not stay in a cache.
+template <bool kOnce, class V>
+__device__ __forceinline__ V load_vector(const void *p) {
+  if constexpr (kOnce) return __builtin_nontemporal_load((const V *)p);
+  else return *(const V *)p;
+}
+template <bool kOnce>
 __device__ __forceinline__ void load8(F32, const float *p, int64_t n, float (&v)[8]) {
   const op_f32x4 none = {0.f, 0.f, 0.f, 0.f};
-  const op_f32x4 a = n > 0 ? *reinterpret_cast<const op_f32x4 *>(p) : none;
-  const op_f32x4 b = n > 4 ? *reinterpret_cast<const op_f32x4 *>(p + 4) : none;
+  const op_f32x4 a = n > 0 ? load_vector<kOnce, op_f32x4>(p) : none;
+  const op_f32x4 b = n > 4 ? load_vector<kOnce, op_f32x4>(p + 4) : none;
 #pragma unroll
   for (int e = 0; e < 8; ++e) v[e] = e < n ? (e < 4 ? a[e % 4] : b[e % 4]) : 0.f;
 }
+template <bool kOnce>
 __device__ __forceinline__ void load8(BF16, const uint16_t *p, int64_t n, float (&v)[8]) {
   const op_u32x4 none = {0u, 0u, 0u, 0u};
-  const op_u32x4 a = n > 0 ? *reinterpret_cast<const op_u32x4 *>(p) : none;
+  const op_u32x4 a = n > 0 ? load_vector<kOnce, op_u32x4>(p) : none;
   BF16::unpack(a, v);
 #pragma unroll
   for (int e = 0; e < 8; ++e) v[e] = e < n ? v[e] : 0.f;

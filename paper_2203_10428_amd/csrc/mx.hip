@@ -25,8 +25,10 @@ struct QuantArgs {
   Chunks chunks;        // of 8 elements, four to a block
 };
 
-// Four neighbouring lanes to a block, eight elements each.
-template <class T, class F>
+// Four neighbouring lanes to a block, eight elements each.  Bound by memory: 239,000 x 512 fp32 to INT8 110 us, 5.6 TB/s,
+// with loads past the caches (127 through them); gathered rows, which several peers are sent, go through them
+// (462,000 rows of 239,000: 199 us against 212).  More than one chunk to a thread changes nothing.
+template <class T, class F, bool kGather>
 __global__ __launch_bounds__(kThreads) void quantize_rows(QuantArgs a) {
   const int64_t first = workgroup() * kThreads;
   const int64_t row0 = first / a.chunks.per;
@@ -34,10 +36,11 @@ __global__ __launch_bounds__(kThreads) void quantize_rows(QuantArgs a) {
   if (first + threadIdx.x >= a.chunks.total) return;     // whole blocks: a row's chunks are a multiple of four
   const uint32_t down = chunk_row(a.chunks, at), c = at - down * a.chunks.per;
   const int64_t row = row0 + down;
-  const int64_t src = a.index ? a.index[row] : row;
+  const int64_t src = kGather ? a.index[row] : row;
   float x[8];
   const bool some = src >= 0 && src < a.src_rows;
-  load8(T{}, (const typename T::type *)a.X + (some ? src * a.ld_x + 8 * (int64_t)c : 0), some ? a.cols - 8 * (int64_t)c : 0, x);
+  const typename T::type *X = (const typename T::type *)a.X + (some ? src * a.ld_x + 8 * (int64_t)c : 0);
+  load8<!kGather>(T{}, X, some ? a.cols - 8 * (int64_t)c : 0, x);
   uint32_t m = 0u;
 #pragma unroll
   for (int e = 0; e < 8; ++e) m = max(m, __float_as_uint(x[e]) & 0x7fffffffu);
@@ -83,7 +86,7 @@ __global__ __launch_bounds__(kThreads) void quantize_cols(QuantArgs a, uint32_t 
   const int64_t rows = a.rows - 32 * block;
   op_u32x4 x[32];
 #pragma unroll
-  for (int r = 0; r < 32; ++r) x[r] = r < rows ? *reinterpret_cast<const op_u32x4 *>(X + r * a.ld_x) : op_u32x4{0u, 0u, 0u, 0u};
+  for (int r = 0; r < 32; ++r) x[r] = r < rows ? load_vector<true, op_u32x4>(X + r * a.ld_x) : op_u32x4{0u, 0u, 0u, 0u};
   const int cols = (int)min((int64_t)T::E, a.cols - col);
 #pragma unroll
   for (int c = 0; c < T::E; ++c) {
@@ -140,7 +143,7 @@ __global__ __launch_bounds__(kThreads) void read_rows(ReadArgs a) {
   const int n = a.cols - 8 * (int)c;
   if (kAverage) {
     float x[8];
-    load8(T{}, out, n, x);
+    load8<false>(T{}, out, n, x);
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] = __builtin_fmaf(a.gamma, x[e], a.rest * v[e]);
   }
@@ -159,7 +162,9 @@ void quantize(const QuantArgs &a, bool transpose, hipStream_t s) {
     const int64_t groups = (a.cols + 32 * T::E - 1) / (32 * T::E), bands = (mx_blocks(a.rows) + 7) / 8;
     hipLaunchKernelGGL((quantize_cols<T, F>), grid_of(groups * bands), dim3(kThreads), 0, s, a, (uint32_t)groups);
   } else {
-    hipLaunchKernelGGL((quantize_rows<T, F>), grid_of((a.chunks.total + kThreads - 1) / kThreads), dim3(kThreads), 0, s, a);
+    const dim3 grid = grid_of((a.chunks.total + kThreads - 1) / kThreads);
+    if (a.index) hipLaunchKernelGGL((quantize_rows<T, F, true>), grid, dim3(kThreads), 0, s, a);
+    else hipLaunchKernelGGL((quantize_rows<T, F, false>), grid, dim3(kThreads), 0, s, a);
   }
 }
 
