@@ -88,19 +88,31 @@ __device__ __forceinline__ uint32_t pack8(Fp4, const float (&x)[8], uint32_t s) 
   return v;
 }
 
-__device__ __forceinline__ void unpack8(Int8, const op_u32x2 &q, uint32_t s, float (&v)[8]) {
+// Four elements of a block from their bytes, in the low ones of q.
+__device__ __forceinline__ void unpack4(Int8, uint32_t q, uint32_t s, float *v) {
   const float step = int8_step(s);
 #pragma unroll
-  for (int e = 0; e < 8; ++e) v[e] = (float)(int)(int8_t)(q[e / 4] >> (8 * (e % 4))) * step;
+  for (int e = 0; e < 4; ++e) v[e] = (float)(int)(int8_t)(q >> (8 * e)) * step;
 }
-__device__ __forceinline__ void unpack8(Fp4, uint32_t q, uint32_t s, float (&v)[8]) {
+__device__ __forceinline__ void unpack4(Fp4, uint32_t q, uint32_t s, float *v) {
   typedef float f2 __attribute__((ext_vector_type(2)));
   const float f = scale_of(s);
   const f2 a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(q, f, 0), b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(q, f, 1);
-  const f2 c = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(q, f, 2), d = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(q, f, 3);
-  const float w[8] = {a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+  const float w[4] = {a[0], a[1], b[0], b[1]};
 #pragma unroll
-  for (int e = 0; e < 8; ++e) v[e] = s == 255u ? __uint_as_float(0x7fc00000u) : w[e];
+  for (int e = 0; e < 4; ++e) v[e] = s == 255u ? __uint_as_float(0x7fc00000u) : w[e];
+}
+// Four or eight of them from memory.
+template <int E>
+__device__ __forceinline__ void unpack(Int8, const uint8_t *q, uint32_t s, float (&v)[E]) {
+#pragma unroll
+  for (int i = 0; i < E / 4; ++i) unpack4(Int8{}, reinterpret_cast<const uint32_t *>(q)[i], s, v + 4 * i);
+}
+template <int E>
+__device__ __forceinline__ void unpack(Fp4, const uint8_t *q, uint32_t s, float (&v)[E]) {
+  const uint32_t bits = E == 4 ? *reinterpret_cast<const uint16_t *>(q) : *reinterpret_cast<const uint32_t *>(q);
+#pragma unroll
+  for (int i = 0; i < E / 4; ++i) unpack4(Fp4{}, bits >> (16 * i), s, v + 4 * i);
 }
 template <class F>
 struct Bits8;      // the bytes of eight elements

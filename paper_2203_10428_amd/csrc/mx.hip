@@ -125,35 +125,30 @@ struct ReadArgs {
   int64_t ld_q, ld_s, ld_out;
   int32_t cols;
   float gamma, rest;       // rest = 1 - gamma
-  Chunks chunks;           // of 8 elements that hold some of a row's
+  Chunks chunks;           // of 16 bytes of out that hold some of a row's
 };
 
+// A thread to 16 bytes of out, so that a wave writes whole lines.
 template <class T, class F, bool kAverage>
 __global__ __launch_bounds__(kThreads) void read_rows(ReadArgs a) {
+  constexpr int E = T::E;
   const int64_t first = workgroup() * kThreads;
   const int64_t row0 = first / a.chunks.per;
   const uint32_t at = (uint32_t)(first - row0 * a.chunks.per) + threadIdx.x;
   if (first + threadIdx.x >= a.chunks.total) return;
   const uint32_t down = chunk_row(a.chunks, at), c = at - down * a.chunks.per;
   const int64_t row = row0 + down;
-  float v[8];
-  unpack8(F{}, *reinterpret_cast<const typename Bits8<F>::type *>(a.Q + row * a.ld_q + (int64_t)c * (F::kBytes / 4)),
-          a.S[row * a.ld_s + c / 4], v);
-  typename T::type *out = (typename T::type *)a.out + row * a.ld_out + 8 * (int64_t)c;
-  const int n = a.cols - 8 * (int)c;
-  if (kAverage) {
-    float x[8];
-    load8<false>(T{}, out, n, x);
+  float v[E];
+  unpack<E>(F{}, a.Q + row * a.ld_q + (int64_t)c * (F::kBytes * E / 32), a.S[row * a.ld_s + c / (32 / E)], v);
+  typename T::type *out = (typename T::type *)a.out + row * a.ld_out + E * (int64_t)c;
+  const int n = a.cols - E * (int)c;
+  if constexpr (kAverage) {
+    const typename T::raw x = *reinterpret_cast<const typename T::raw *>(out);
+    static_assert(E == 4, "a moving average is kept in fp32");
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = __builtin_fmaf(a.gamma, x[e], a.rest * v[e]);
+    for (int e = 0; e < E; ++e) v[e] = __builtin_fmaf(a.gamma, x[e], a.rest * v[e]);
   }
-#pragma unroll
-  for (int i = 0; i < 8 / T::E; ++i) {
-    float w[T::E];
-#pragma unroll
-    for (int e = 0; e < T::E; ++e) w[e] = v[i * T::E + e];
-    if (n > i * T::E) store_some<T>(out + i * T::E, w, n - i * T::E);
-  }
+  store_some<T>(out, v, n);
 }
 
 template <class T, class F>
@@ -187,7 +182,7 @@ int launch_mx_quantize(const pgcn_mx_quantize_args &x, hipStream_t s) {
 }
 
 int launch_mx_dequantize(const pgcn_mx_dequantize_args &x, hipStream_t s) {
-  const ReadArgs a{x.Q, x.S, x.out, x.ld_q, x.ld_s, x.ld_out, x.cols, x.gamma, 1.f - x.gamma, chunks_of(x.rows, (x.cols + 7) / 8)};
+  const ReadArgs a{x.Q, x.S, x.out, x.ld_q, x.ld_s, x.ld_out, x.cols, x.gamma, 1.f - x.gamma, chunks_of(x.rows, x.dtype == PGCN_BF16 ? (x.cols + 7) / 8 : (x.cols + 3) / 4)};
   const dim3 grid = grid_of((a.chunks.total + kThreads - 1) / kThreads), block(kThreads);
   TraceScope ts(PGCN_TK_MX_DEQUANTIZE, s);
   const bool int8 = x.format == PGCN_MX_INT8;
