@@ -31,7 +31,7 @@ struct MatmulArgs {
 __device__ __forceinline__ i32x8 wide(const op_u32x4 &q) { return i32x8{(int)q[0], (int)q[1], (int)q[2], (int)q[3], 0, 0, 0, 0}; }
 
 // 16 bytes or one dword a lane from memory to LDS, place + lane size, without a register between.  Written out, so that
-// the compiler does not wait for it before every LDS read: landed() does, once a slab.
+// the compiler does not wait for it before every LDS read: landed() does, once a slab.  No register is written.
 template <int kBytes>
 __device__ __forceinline__ void to_lds(const void *src, uint32_t place) {
   if constexpr (kBytes == 16)

@@ -101,7 +101,7 @@ def test_zero_rows():
     assert (C[:5, :6] == 0).all()
 
 
-@pytest.mark.parametrize("m,n,k", [(1, 600, 2000), (40, 300, 515), (600, 520, 700)])
+@pytest.mark.parametrize("m,n,k", [(1, 600, 2000), (40, 300, 515), (600, 520, 700), (2, 90, 20000), (100, 90, 9000), (2100, 2060, 1100)])
 def test_the_same_bits_every_time_and_from_a_graph(m, n, k):
     """Quantised activations times held weights, on another stream, replayed with eager calls between."""
     rng = np.random.default_rng(4)
