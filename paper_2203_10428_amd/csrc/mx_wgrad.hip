@@ -239,19 +239,22 @@ struct Shape {
 // Tile: 256 or 192 features of v where that fills up no more than 128 do, since a slab's J is split into its parts by
 // every tile row (fp32: 239,000 x 512 x 512 347 us with 256, 455 with 128; 239,000 x 300 x 512 284 with 192, 348 with 128;
 // 58,000 x 602 x 256, which 256 would fill up to 768: 81 against 76).
-// Splits: as many workgroups as are resident at once.  Tiles of more than 128 two to a compute unit, 128-row tiles three
-// (58,000 x 602 x 256: 76 us and 8 for adding the partial tiles, at two 85 and 6); bf16, which waits for memory, two
-// (58,000 x 602 x 256: 67, at three 65 and 2 more for the partial tiles), and where one tile is all there is, one:
-// half as many partial tiles (306,000 x 128 x 128: 68 + 7, at two 70 + 12).  At least 64 rows to a split; where that
-// leaves compute units idle down to 32, as a workgroup's slabs are a chain.  The partial
-// matrices stay below 64 MB together.
+// Splits: as many workgroups as are resident at once, or fewer where their partial tiles cost more than they bring.  fp32
+// 128-row tiles three to a compute unit (58,000 x 602 x 256: 76 us and 8 for adding the partial tiles, at two 83 and 6), with
+// two tiles two, with one one (306,000 x 128 x 128: 75 us with the adding, at three 93; 306,000 x 128 x 256: 135 at two, 148 at
+// three); larger tiles two.  bf16, which waits for memory, two, with up to two tiles one (306,000 x 128 x 256: 126, at two
+// 135; 100,000 x 400 x 128: 55 and 71).  Tiles of 64 columns two (306,000 x 100 x 47 fp32: 39, at one 49, at three 47).
+// At least 64 rows to a split; where that leaves compute units idle down to 32, as a workgroup's slabs are a chain.
+// The partial matrices stay below 64 MB together.
 Shape shape_of(int32_t dtype, int64_t rows, int32_t f_in, int32_t f_out) {
   Shape c;
   c.bn = f_out <= 64 ? 64 : 128;
   const auto filled = [&](int bm) { return (f_in + bm - 1) / bm * bm; };
   c.bm = f_in <= 128 || c.bn == 64 ? 128 : filled(256) <= filled(128) ? 256 : filled(192) <= filled(128) ? 192 : 128;
   const int64_t tiles = (int64_t)((f_in + c.bm - 1) / c.bm) * ((f_out + c.bn - 1) / c.bn);
-  const int64_t slots = c.bm > 128 ? 512 : dtype == PGCN_F32 ? 768 : tiles == 1 && c.bn == 128 ? 256 : 512;
+  int64_t slots = 512;
+  if (c.bn == 128 && dtype == PGCN_BF16 && tiles <= 2) slots = 256;
+  if (c.bn == 128 && dtype == PGCN_F32 && c.bm == 128) slots = std::min<int64_t>(256 * tiles, 768);
   // no more than the fp32 and bf16 forms take, whose scratch a layer's backward has
   const int64_t tile_bytes = (int64_t)f_in * f_out * 4;
   const int64_t by_bytes =
