@@ -65,6 +65,7 @@ __device__ __forceinline__ void finish4(const MatmulArgs &p, int64_t row, int co
       if (col + e < p.n) T::put(out + e, v[e]);
   }
 }
+
 // One stage of LDS: a slab's eight blocks of every row, block c at place c ^ (row % 8), so that neighbouring lanes' reads
 // of one block touch all banks.
 template <int BM, int BN>
