@@ -269,8 +269,8 @@ size_t pgcn_layer_workspace_size(const pgcn_partition *part, int32_t f_in, int32
  * a_given == 1 (aggregate first only) skips the aggregation: A is an input
  * holding P_i [H_in ; H_bd], e.g. a layer-1 aggregate kept across iterations
  * (the input features are constant); H_in / H_bd are then not read.
- * With PGCN_MXFP4, A is required, A_bf16 ignored, H_out and W are 16-byte
- * aligned, and the sent rows are copied after the product.
+ * With PGCN_MXFP4, A is required, A_bf16 ignored, H_out, W and the workspace
+ * are 16-byte aligned, and the sent rows are copied after the product.
  */
 typedef struct {
   int32_t f_in, f_out;         /* 1 .. PGCN_MAX_WIDTH                            */

@@ -442,7 +442,8 @@ extern "C" int pgcn_layer_fwd(const pgcn_partition *p, const pgcn_fwd_args *a, h
                "pgcn_layer_fwd: a given aggregate needs the aggregate-first order");
   PGCN_REQUIRE(a->gemm_dtype != PGCN_MXFP4 || a->order == PGCN_ORDER_AGG, "pgcn_layer_fwd: MXFP4 needs the aggregate-first order");
   if (a->gemm_dtype == PGCN_MXFP4 && p->n_inner > 0)
-    PGCN_REQUIRE(aligned16(a->H_out) && aligned16(a->W), "pgcn_layer_fwd: MXFP4 needs H_out and W 16-byte aligned");
+    PGCN_REQUIRE(aligned16(a->H_out) && aligned16(a->W) && aligned16(a->workspace),
+                 "pgcn_layer_fwd: MXFP4 needs H_out, W and the workspace 16-byte aligned");
   if (a->order == PGCN_ORDER_TRANSFORM) return layer_fwd_transform(p, a, s);
   const bool bf16 = a->gemm_dtype == PGCN_BF16;
   if (a->a_given) {                  // only the update: Z = A W from the given fp32 aggregate

@@ -237,6 +237,7 @@ def test_forward_in_4_bits_refuses():
     for over in (dict(order=B.PGCN_ORDER_TRANSFORM), dict(A=None), dict(H_out=H[1:]), dict(W=g.W.view(-1)[1:]), dict(gemm_dtype=3), dict(ld_out=40)):
         refused(lambda: B.pgcn_layer_fwd(g.part, **{**args, **over}))
     refused(lambda: B.pgcn_layer_fwd(g.part, **{**args, "workspace_bytes": 256}), B.PGCN_EWORKSPACE)
+    refused(lambda: B.pgcn_layer_fwd(g.part, **{**args, "workspace": args["workspace"][8:], "workspace_bytes": 1 << 40}))
     s = Layer(sage=True)
     refused(lambda: B.pgcn_sage_layer_fwd(s.part, X_in=s.X, X_in_bf16=None, X_bd=s.X_bd, A=torch.zeros_like(s.X), A_bf16=None, H_out=H,
                                           **{**s.common(B.PGCN_F32), "gemm_dtype": B.PGCN_MXFP4}))
