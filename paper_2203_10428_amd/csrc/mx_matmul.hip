@@ -275,6 +275,7 @@ __global__ __launch_bounds__(256) void matmul_tile(MatmulArgs p) {
           if constexpr (kElem == 4) *reinterpret_cast<op_f32x4 *>(to) = op_f32x4{v[0], v[1], v[2], v[3]};
           else *reinterpret_cast<op_u32x2 *>(to) = op_u32x2{BF16::two(v[0], v[1]), BF16::two(v[2], v[3])};
         }
+      wave_sync();                                        // lanes read what others wrote
 #pragma unroll
       for (int pass = 0; pass < kChunks / 2; ++pass) {
         const int down = pass * (64 / kChunks) + lane / kChunks, col = j0 + wn0 + lane % kChunks * O::E;
@@ -293,6 +294,7 @@ __global__ __launch_bounds__(256) void matmul_tile(MatmulArgs p) {
             }
         }
       }
+      wave_sync();                                        // the next rows are written after these reads
     }
   };
   if (BM == 64 && p.parts) write(F32{}, p.parts + (int64_t)part * p.m * p.n4, p.n4, (int)p.n4, false);

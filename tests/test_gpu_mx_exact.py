@@ -68,3 +68,22 @@ def test_every_block_counts_once(m, n, k):
 def test_every_block_of_a_long_row_counts_once(m, n, k, signed, dtype):
     assert B.pgcn_mx_matmul_workspace_size(B.PGCN_F32, m, n, k) >= 2 * 4 * m * n
     check_product(m, n, k, dtype, signed, False)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("m,n", [(64, 64), (200, 100), (2100, 2050), (2048, 2176), (4096, 4096), (4100, 4090)])
+def test_results_of_every_tile_are_in_their_place(m, n, dtype):
+    """Rows of a tile go through LDS, which one lane writes and another reads, and the next rows after them: products of
+    one term, a sign and a power of two that tell neighbouring rows and columns apart, several times over the same output."""
+    rng = np.random.default_rng(m)
+    side = lambda rows: (np.concatenate((rng.choice([1, 2, 4, 10], (rows, 1)), np.zeros((rows, 31), np.int64)), axis=1),
+                         rng.integers(100, 150, (rows, 1)))
+    a, b = side(m), side(n)
+    held = upload(*a, "fp4"), upload(*b, "fp4")
+    want = torch.from_numpy(mx.product(mx.values(*a, 1, "fp4"), mx.values(*b, 1, "fp4"))).cuda()
+    C = None
+    for _ in range(5):
+        C = matmul(*held[0], *held[1], m, n, 1, dtype, out=C)
+        torch.cuda.synchronize()
+        assert torch.equal(C[:m, :n].double(), want)
+        C[:m, :n] = 5.0
