@@ -52,8 +52,10 @@ with the teacher's lists at temperature T = ``distill_temp``; nodes with label
 In fewer bits (blocks of 32 values with one power of two as scale, ``pgcn_mx_*``):
 
 * ``checkpoint_bits`` = 8 keeps the aggregate of every aggregate-first layer for the weight gradient in
-  8 bits (1.03 bytes a value instead of 4 or 2; GraphSAGE's dropped input too), from one buffer that
-  these layers share.  The forward, the loss and the input gradients are as without it;
+  8 bits (1.03 bytes a value instead of 4 or 2; GraphSAGE's dropped input too).  The layers take turns in one
+  buffer in full precision, which lies where the backward's gradients do and takes more only as far as the widest
+  of them needs more than these (more than is saved where that is nearly the whole of the model: one layer alone, or
+  bf16 layers 602-64-16).  The forward, the loss and the input gradients are as without it;
 * ``exchange_bits`` = 8 or 4 sends boundary features and gradients in that many bits: rows are quantised
   as they are packed, travel and wait in the stale buffers as bytes, and are read back, smoothed or not,
   when they are consumed;
@@ -152,6 +154,17 @@ class HeldRows:
                              stream=stream)
 
 
+class Space:
+    """A byte buffer handed out in matrices, one behind the other; with at = 0 from its start again."""
+
+    def __init__(self, nbytes: int, device):
+        self.bytes, self.at = torch.zeros(nbytes, dtype=torch.uint8, device=device), 0
+
+    def take(self, rows: int, ld: int, dtype):
+        first, self.at = self.at, self.at + rows * ld * dtype.itemsize
+        return self.bytes[first:self.at].view(dtype).view(rows, ld)
+
+
 class PartitionTrainer:
     """Device state of one partition and its training step."""
 
@@ -213,23 +226,27 @@ class PartitionTrainer:
         assert not (self.cache1 and (self.ckpt or opts.exchange_bits)), "the cached layer 1 keeps and receives fp32 rows"
         assert not (self.mx4 and self.sage), "forward updates in 4 bits are the GCN layer's"
         wide = max([ld_of(wd[l - 1]) for l in self.ckpt], default=0)
-
-        def each(rows, dt=torch.float32, layers=range(1, L + 1)):
-            """Buffers of the layers' input widths: one that the layers in 8 bits take in turn, one for each other."""
-            t = torch.zeros(rows * wide if self.ckpt & set(layers) else 0, dtype=dt, device=self.dev)
-            return {l: t[:rows * ld_of(wd[l - 1])].view(rows, ld_of(wd[l - 1])) if l in self.ckpt else z(rows, wd[l - 1], dt)
-                    for l in layers}
-
         # dropped layer inputs (dropout, or the bf16 copy of the GraphSAGE self operand)
         self.use_drop = opts.dropout > 0.0 or (self.sage and not f32)
-        self.Xd_in = each(n) if self.use_drop else {}
-        self.Xd_bd = each(b) if self.use_drop else {}
-        self.Xd_16 = each(n, torch.bfloat16) if (self.sage and not f32) else {}
         # activations, indexed by layer 1..L (a transform-first layer keeps no aggregate)
-        in32 = [l for l in agg if agg[l] and (f32 or (not self.sage and l in self.ckpt | self.mx4))]   # the forward leaves A in fp32
+        in32 = [l for l in agg if agg[l] and (f32 or l in self.mx4)]            # the forward leaves A in fp32
         in16 = [l for l in agg if agg[l] and l not in in32]
+        # what the layers in 8 bits take turns in is not used past the forward pass, and the gradients J not before it ends
+        turns = [t for t, some in ((4, self.ckpt & set(in32)), (2, self.ckpt & set(in16)), (4, self.use_drop),
+                                   (2, self.sage and not f32)) if some]
+        shared = Space(n * max(wide * sum(turns), 4 * sum(ld_of(f) for f in wd[1:])), self.dev) if self.ckpt else None
+
+        def each(rows, dt=torch.float32, layers=range(1, L + 1), space=shared):
+            """Buffers of the layers' input widths: one that the layers in 8 bits take in turn, one for each other."""
+            turn = self.ckpt & set(layers) and (space.take(rows, wide, dt) if space else z(rows, wide, dt)).view(-1)
+            return {l: turn[:rows * ld_of(wd[l - 1])].view(rows, ld_of(wd[l - 1])) if l in self.ckpt else z(rows, wd[l - 1], dt)
+                    for l in layers}
+
         self.A = {**dict.fromkeys(agg), **each(n, layers=in32)}
         self.A16 = {**dict.fromkeys(agg), **each(n, torch.bfloat16, in16)}
+        self.Xd_in = each(n) if self.use_drop else {}
+        self.Xd_bd = each(b, space=None) if self.use_drop else {}
+        self.Xd_16 = each(n, torch.bfloat16) if (self.sage and not f32) else {}
         self.A_mx = {l: HeldRows(8, n, wd[l - 1], self.dev) for l in sorted(self.ckpt)}
         self.X_mx = {l: HeldRows(8, n, wd[l - 1], self.dev) for l in sorted(self.ckpt) if self.sage and self.use_drop}
         if self.cache1:   # fp32 aggregates of layer 1 on both paths: the running one and A_full
@@ -261,8 +278,11 @@ class PartitionTrainer:
         self.bits = opts.exchange_bits
         self.fuse_pack = opts.fuse_pack and not self.norm and not self.bits
         self.teacher = None
-        self.J_top = z(n, wd[L])
-        self.J_in = {l: z(n, wd[l - 1]) for l in range(2, L + 1)}
+        if shared:
+            shared.at = 0
+        gradient = lambda f: shared.take(n, ld_of(f), torch.float32) if shared else z(n, f)
+        self.J_top = gradient(wd[L])
+        self.J_in = {l: gradient(wd[l - 1]) for l in range(2, L + 1)}
         self.J_bd_out = {l: z(b, wd[l - 1]) for l in range(2, L + 1)}
         # stale feature buffers (layer l reads boundary rows of H^(l-1)), gradient buffers for l >= 2; messages in
         # fewer bits are kept as they arrived
@@ -541,9 +561,11 @@ class PartitionTrainer:
     def _backward_layer(self, l, J_out, st):
         """Layer gradients; the input gradient then takes the forward's dropout mask."""
         wd, f = self.widths, self.widths[l - 1]
-        A = self.A1_used if (self.cache1 and l == 1) else self.A[l]
+        A, A16 = self.A1_used if (self.cache1 and l == 1) else self.A[l], self.A16[l]
+        if l in self.ckpt:
+            A = A16 = None
         common = dict(f_in=f, f_out=wd[l], gemm_dtype=self.dtype, relu=self._relu(l), ld_in=ld_of(f),
-                      ld_out=ld_of(wd[l]), J_out=J_out, H_out=self._layer_out(l), A=A, A_bf16=self.A16[l],
+                      ld_out=ld_of(wd[l]), J_out=J_out, H_out=self._layer_out(l), A=A, A_bf16=A16,
                       W=self.W[l - 1], dW=self.dW[l - 1], J_in=self.J_in.get(l), J_bd_out=self.J_bd_out.get(l),
                       workspace=self.ws, workspace_bytes=self.ws_bytes, stream=st)
         if l in self.ckpt:
