@@ -807,7 +807,7 @@ int pgcn_mx_matmul(const pgcn_mx_matmul_args *args, hipStream_t stream);
  * them on a second stream): an asynchronous copy of `bytes` bytes into device
  * memory `dst`, enqueued on `stream`.  flags = 0: device-to-device on the
  * compute units; copies of at least 4 MiB between 16-byte-aligned device
- * buffers (`bytes` a multiple of 16) by the library's copy kernel with
+ * buffers by the library's copy kernel with
  * non-temporal loads and stores (the copied rows are read in the next
  * iteration, so they bypass the caches the current one uses), others by
  * the runtime's copy; PGCN_REFILL_DMA:

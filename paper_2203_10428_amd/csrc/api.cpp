@@ -1307,7 +1307,7 @@ extern "C" int pgcn_refill_async(void *dst, const void *src, size_t bytes, uint3
   // pointers itself; small copies skip the pointer lookups (microseconds each) that the
   // kernel path needs.
   constexpr size_t kRefillKernelMin = size_t(4) << 20;
-  const bool vec = (bytes % 16) == 0 && ((reinterpret_cast<uintptr_t>(dst) | reinterpret_cast<uintptr_t>(src)) & 15) == 0;
+  const bool vec = ((reinterpret_cast<uintptr_t>(dst) | reinterpret_cast<uintptr_t>(src)) & 15) == 0;
   if (!(flags & PGCN_REFILL_DMA) && vec && bytes >= kRefillKernelMin && is_device_memory(dst) && is_device_memory(src))
     return launch_refill_copy(dst, src, bytes, s);
   PGCN_HIP(hipMemcpyAsync(dst, src, bytes, (flags & PGCN_REFILL_DMA) ? hipMemcpyDeviceToDeviceNoCU : hipMemcpyDeviceToDevice, s));

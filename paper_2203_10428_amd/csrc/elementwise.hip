@@ -151,9 +151,13 @@ __global__ __launch_bounds__(256) void pack_rows_kernel(const int64_t *__restric
 // 16 KB (four vectors per thread, loads issued together): the copy runs on a
 // side stream beside the compute kernels, and workgroups that retire often
 // let the dispatcher interleave theirs (a grid-stride copy that holds every
-// wave slot until it ends starves a compute kernel launched meanwhile).
+// wave slot until it ends starves a compute kernel launched meanwhile).  The
+// bytes behind the last vector, fewer than 16, go one to a thread of the first
+// workgroup.
 constexpr int kRefillVec = 4;
-__global__ __launch_bounds__(256) void refill_copy_kernel(const ew_f32x4 *src, ew_f32x4 *dst, int64_t n16) {
+__global__ __launch_bounds__(256) void refill_copy_kernel(const ew_f32x4 *src, ew_f32x4 *dst, int64_t n16, int rest) {
+  if (blockIdx.x == 0 && (int)threadIdx.x < rest)
+    reinterpret_cast<uint8_t *>(dst + n16)[threadIdx.x] = reinterpret_cast<const uint8_t *>(src + n16)[threadIdx.x];
   const int64_t base = (int64_t)blockIdx.x * (256 * kRefillVec) + threadIdx.x;
   ew_f32x4 v[kRefillVec];
 #pragma unroll
@@ -169,7 +173,7 @@ int launch_refill_copy(void *dst, const void *src, size_t bytes, hipStream_t s) 
   const int64_t blocks = (n16 + 256 * kRefillVec - 1) / (256 * kRefillVec);
   PGCN_REQUIRE(blocks <= 0x7fffffff, "pgcn_refill_async: copy too large for one launch");
   hipLaunchKernelGGL(refill_copy_kernel, dim3((unsigned)blocks), dim3(256), 0, s,
-                     reinterpret_cast<const ew_f32x4 *>(src), reinterpret_cast<ew_f32x4 *>(dst), n16);
+                     reinterpret_cast<const ew_f32x4 *>(src), reinterpret_cast<ew_f32x4 *>(dst), n16, (int)(bytes % 16));
   PGCN_HIP(hipGetLastError());
   return PGCN_OK;
 }
