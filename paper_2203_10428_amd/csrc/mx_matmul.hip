@@ -378,7 +378,8 @@ struct Shape {
 
 // Up to 16 rows on their own: 16 x 8192 x 8192 13 us, in 64 x 64 tiles 14 and 3 to join them.  Otherwise the largest tile
 // of which there is one for every compute unit: it brings the fewest bytes to a product (8192 x 8192 x 8192: 268 us in
-// tiles of 256; 3500 x 3000 x 4096, half as many of them as units: 37 in tiles of 128).  More stages than two help where a
+// tiles of 256; 3500 x 3000 x 4096, half as many of them as units: 37 in tiles of 128).  The count does not see tiles that
+// are mostly filled up, where one side is short: 306,000 x 47 x 128 takes 88 us, 32 x 65,536 x 4096 39.  More stages than two help where a
 // compute unit has one small tile (777 x 1000 x 5000: 11.4 us with four, 15.8 with two), not where others fill it
 // (58,000 x 256 x 602 in tiles of 128: 21.6 with two, 31.7 with four).
 // Where units are left without a tile, the blocks are split among as many workgroups as there are units (two a unit for
